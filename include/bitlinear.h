@@ -52,7 +52,10 @@ enum {
     BITLINEAR_ERR_TIMEOUT = -7,   /* a bounded device-side wait expired (device status) */
     BITLINEAR_ERR_RANGE = -8,     /* a weight was non-finite or >= 2^24 in magnitude (reported on the device, as
                                      gamma = NaN; no call returns this code) */
-    BITLINEAR_ERR_BADCODE = -9    /* bitlinear_validate_packed found the 2-bit code 3, which no weight has */
+    BITLINEAR_ERR_BADCODE = -9,   /* bitlinear_validate_packed found the 2-bit code 3, which no weight has */
+    BITLINEAR_ERR_PAGE = -10      /* a page number, a sequence length or a position outside what the cache, the page table
+                                     or the rotary table holds (reported on the device, in bitlinear_kv_cache.status; no
+                                     call returns this code) */
 };
 
 /* Matmul code paths selectable through the test hook bitlinear_matmul_i32. */
@@ -303,6 +306,105 @@ bitlinear_status bitlinear_forward_sequence_stage(const bitlinear_sequence *seq,
 
 /* Frees the host object (no device work, no device memory involved).  NULL is allowed. */
 void bitlinear_sequence_destroy(bitlinear_sequence *seq);
+
+/*
+ * What stands between the projections of a decoder layer: the rotary embedding (Section 2, "LLaMA-alike Components",
+ * names it and gives no formula; this is the textbook one), a paged cache of keys and values, in bf16 or in 8 bits (the
+ * outlook of Section 4 on long sequences expects 8-bit activations and with them a cache of half the size), and the softmax
+ * attention over it.  Queries, keys and values are what the BitLinear projections wrote: bf16 [tokens, heads, head_dim]
+ * with any row stride (a multiple of 8 elements, at least heads * head_dim), e.g. slices of one fused q/k/v output.
+ *
+ * The cache.  Row (page, h, slot) of `k` and `v` holds the key and the value of one token for kv head h: W = head_dim
+ * rounded up to a multiple of 16 elements (the elements behind head_dim are 0: bitlinear_kv_append writes them so, and
+ * bitlinear_attend_* rely on it), stored [n_pages][kv_heads][page_size][W].
+ *   bits 16: bf16.  bits 8: int8 codes and, in k_scale and v_scale [n_pages][kv_heads][page_size], one fp32 per row: the
+ *   row stands for code * scale.
+ * Position p of sequence b stands in page page_table[b * table_stride + p / page_size], slot p % page_size.  A page may
+ * serve several sequences (a shared prefix) as long as nothing is appended to it for one of them.
+ *   head_dim a multiple of 4, 4 .. 128;  kv_heads 1 .. 1024;  page_size 16, 32, 64, 128 or 256;  n_pages >= 1 with
+ *   n_pages * kv_heads * page_size < 2^31
+ * `status` (device, one int32, set to 0 by the owner) receives BITLINEAR_ERR_PAGE when a call met a page number outside
+ * 0 .. n_pages - 1, a length beyond table_pages * page_size, or a position beyond the rotary table: nothing is read or
+ * written there (what that does to the results is said at each call), and the word keeps the code until the owner clears it.
+ */
+typedef struct {
+    void *k, *v;             /* device, bitlinear_kv_cache_bytes(...) bytes each, 16-byte aligned */
+    float *k_scale, *v_scale; /* device, fp32 [n_pages][kv_heads][page_size], 16-byte aligned; NULL for bits = 16 */
+    int32_t *status;         /* device */
+    int64_t n_pages;
+    int32_t kv_heads, head_dim, page_size, bits;
+} bitlinear_kv_cache;
+
+/*
+ * The sequences of a call.  kv_lens[b] is the length of sequence b WITH the call's new tokens: the i-th of its n new tokens
+ * has position kv_lens[b] - n + i.  cu_tokens [n_seqs + 1] holds the rows of the new tokens: those of sequence b are
+ * cu_tokens[b] .. cu_tokens[b + 1] - 1 (0 <= cu_tokens[b] <= cu_tokens[b + 1]); NULL: one token per sequence, row b.  Rows
+ * behind cu_tokens[n_seqs] (a padded batch) are left as they are.  A token whose position is negative (kv_lens[b] < n:
+ * 0 for an empty slot of a batch) is not stored and sees nothing.  All three arrays are read on the device, so a captured
+ * graph follows their contents.
+ *   0 <= n_seqs <= 2^20;  1 <= table_pages <= table_stride;  table_pages * page_size <= 2^30
+ */
+typedef struct {
+    const int32_t *page_table; /* device, [n_seqs][table_stride], the first table_pages of a row are used */
+    const int32_t *kv_lens;    /* device, [n_seqs] */
+    const int32_t *cu_tokens;  /* device, [n_seqs + 1], or NULL */
+    int64_t n_seqs, table_stride, table_pages;
+} bitlinear_kv_batch;
+
+/* Bytes of `k` (and of `v`) of a cache; the scale arrays have n_pages * kv_heads * page_size floats each.  0 for shapes the
+ * library rejects. (host) */
+size_t bitlinear_kv_cache_bytes(int64_t n_pages, int kv_heads, int head_dim, int page_size, int bits);
+
+/* Fills the rotary table: fp32 [n_pos][head_dim / 2][2], (cos, sin) of pos * base^(-2 i / head_dim), the angle computed in
+ * double.  Models with scaled angles fill their own table.  1 <= n_pos <= 2^24, head_dim as above, base > 0 and finite. */
+bitlinear_status bitlinear_rope_table(float *table, int64_t n_pos, int head_dim, double base, void *stream);
+
+/*
+ * Appends the keys and values of new tokens to the cache, rotated on the way, and rotates their queries.
+ *   k, v       in   bf16 [T, kv_heads, head_dim], row strides in elements
+ *   q          in   bf16 [T, heads, head_dim], or NULL (then heads, q_out and the two strides are not looked at)
+ *   q_out      out  the rotated queries; may be q itself (with the same stride), else must not overlap it
+ *   rope       in   fp32 [rope_positions][head_dim / 2][2] as bitlinear_rope_table writes it, or NULL: no rotation
+ *   interleaved     0: the pairs (x_i, x_{i + head_dim/2});  1: the pairs (x_2i, x_2i+1)
+ *   T               rows of k, v and q (T = n_seqs when cu_tokens is NULL), 0 <= T <= 2^20
+ * A pair (a, b) becomes (a c - b s, b c + a s), rounded once to bf16 for q_out and for a bf16 cache.  8-bit cache: with
+ * x the rotated key (or the value), beta = max(max |x_i|, 1e-5), code_i = round(127 x_i / beta) (half to even) and scale =
+ * beta / 127, all in double (x itself is exact up to 2^-53), so that values half way between two codes, frequent among
+ * quotients of bf16 numbers, go where exact arithmetic sends them.  A row that holds a NaN or an infinity gets scale = NaN
+ * and codes 0.
+ * A token whose position lies beyond the rotary table or the page table is skipped, and one with a bad page is rotated but
+ * not stored; both set the status.
+ */
+bitlinear_status bitlinear_kv_append(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *k,
+                                     int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                                     int64_t T, int heads, const float *rope, int64_t rope_positions, int interleaved,
+                                     void *q_out, int64_t q_out_stride, void *stream);
+
+/* Bytes of workspace of bitlinear_attend_decode (prompt = 0) or bitlinear_attend_prompt (prompt = 1) for these heads,
+ * whatever the batch.  0 for rejected shapes. (host) */
+size_t bitlinear_attend_workspace_bytes(int heads, int kv_heads, int head_dim, int prompt);
+
+/*
+ * Softmax attention over the cache: of the one new token of each sequence (decode, cu_tokens must be NULL), or of the new
+ * tokens of prompts and prompt chunks (prompt, cu_tokens must not be NULL), each over the positions up to its own:
+ *   out_t,h = sum_j p_j v_j,  p = softmax_j(softmax_scale * q_t,h . k_j),  j = 0 .. position of t,  kv head h / (heads / kv_heads)
+ *   q     in   bf16 [T, heads, head_dim] (rotated), row stride in elements;  T = n_seqs for decode
+ *   out   out  bf16 [T, heads, head_dim], row stride in elements; must not overlap q
+ *   heads      a multiple of kv_heads, heads <= 4096
+ *   softmax_scale  > 0 and finite; usually 1 / sqrt(head_dim)
+ *   workspace  >= bitlinear_attend_workspace_bytes(...), 256-byte aligned, filled with zeros by the caller once before its
+ *              first use; every call leaves it fit for the next.  Two calls that may run at the same time must not
+ *              share a workspace.
+ * Sums, maxima and the softmax's denominators are fp32; weights are rounded to bf16 before they meet the values in the
+ * prompt kernel.  A token that sees nothing (an empty slot) gets zeros.  Keys on a bad page, or behind the page table, take
+ * no part and the status is set.  Calls with the same arguments on the same contents give the same bits.
+ */
+bitlinear_status bitlinear_attend_decode(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q,
+                                         int64_t q_stride, int heads, float softmax_scale, void *out, int64_t out_stride,
+                                         void *workspace, size_t workspace_bytes, void *stream);
+bitlinear_status bitlinear_attend_prompt(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q,
+                                         int64_t q_stride, int64_t T, int heads, float softmax_scale, void *out,
+                                         int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Test hooks.

@@ -17,6 +17,7 @@ LIB_PATH = _PKG / "libbitlinear_b200.so"
 
 OK = 0
 ERR_ARG, ERR_SHAPE, ERR_ALIGN, ERR_WORKSPACE, ERR_ARCH, ERR_CUDA, ERR_TIMEOUT, ERR_RANGE, ERR_BADCODE = range(-1, -10, -1)
+ERR_PAGE = -10
 PATH_AUTO, PATH_DP4A, PATH_MMA, PATH_TCGEN05 = 0, 1, 2, 3
 
 EXPORTS = [
@@ -49,6 +50,12 @@ EXPORTS = [
     "bitlinear_sequence_create_trits",
     "bitlinear_matmul_i32_trits",
     "bitlinear_unpack_weights_trits",
+    "bitlinear_kv_cache_bytes",
+    "bitlinear_rope_table",
+    "bitlinear_kv_append",
+    "bitlinear_attend_workspace_bytes",
+    "bitlinear_attend_decode",
+    "bitlinear_attend_prompt",
     "bitlinear_probe_int8_peak",
     "bitlinear_test_expire_next_wait",
     "bitlinear_poll_status",
@@ -70,6 +77,32 @@ class LayerDesc(ctypes.Structure):
         ("M", ctypes.c_int64),
         ("K", ctypes.c_int64),
         ("N", ctypes.c_int64),
+    ]
+
+
+class KVCacheDesc(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("status", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int64),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("bits", ctypes.c_int32),
+    ]
+
+
+class KVBatchDesc(ctypes.Structure):
+    _fields_ = [
+        ("page_table", ctypes.c_void_p),
+        ("kv_lens", ctypes.c_void_p),
+        ("cu_tokens", ctypes.c_void_p),
+        ("n_seqs", ctypes.c_int64),
+        ("table_stride", ctypes.c_int64),
+        ("table_pages", ctypes.c_int64),
     ]
 
 
@@ -128,6 +161,15 @@ def load_library() -> ctypes.CDLL:
     L.bitlinear_probe_int8_peak.argtypes = [ci, vp, ctypes.POINTER(i64), vp]
     L.bitlinear_test_expire_next_wait.argtypes = [ctypes.c_uint32, ci]
     L.bitlinear_test_expire_next_wait.restype = None
+    # (the two descriptors travel as addresses: KVCache and KVBatch keep them)
+    L.bitlinear_kv_cache_bytes.argtypes = [i64, ci, ci, ci, ci]
+    L.bitlinear_kv_cache_bytes.restype = sz
+    L.bitlinear_rope_table.argtypes = [vp, i64, ci, ctypes.c_double, vp]
+    L.bitlinear_kv_append.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, i64, ci, vp, i64, ci, vp, i64, vp]
+    L.bitlinear_attend_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    L.bitlinear_attend_workspace_bytes.restype = sz
+    L.bitlinear_attend_decode.argtypes = [vp, vp, vp, i64, ci, cf, vp, i64, vp, sz, vp]
+    L.bitlinear_attend_prompt.argtypes = [vp, vp, vp, i64, i64, ci, cf, vp, i64, vp, sz, vp]
     _lib = L
     return L
 
@@ -462,3 +504,215 @@ class Sequence:
             self.close()
         except Exception:
             pass
+
+
+def _refuse(where: str, why: str, status: int = ERR_ARG):
+    error = BitLinearError(status, where)
+    error.args = (f"{error.args[0]}: {why}",)
+    raise error
+
+
+def kv_cache_bytes(n_pages: int, kv_heads: int, head_dim: int, page_size: int, bits: int) -> int:
+    return int(load_library().bitlinear_kv_cache_bytes(n_pages, kv_heads, head_dim, page_size, bits))
+
+
+class KVCache:
+    """bitlinear_kv_cache: a paged cache of keys and values, bf16 (bits 16) or int8 codes with a scale per row (bits 8).
+
+    `k`, `v`: [n_pages, kv_heads, page_size, head_dim rounded up to 16]; `k_scale`, `v_scale`: fp32
+    [n_pages, kv_heads, page_size] or None; `status`: int32[1], see check().
+    """
+
+    def __init__(self, n_pages: int, kv_heads: int, head_dim: int, page_size: int = 16, bits: int = 16, device="cuda"):
+        if kv_cache_bytes(n_pages, kv_heads, head_dim, page_size, bits) == 0:
+            raise BitLinearError(ERR_SHAPE, "bitlinear_kv_cache_bytes")
+        shape = (n_pages, kv_heads, page_size, (head_dim + 15) // 16 * 16)
+        dtype = torch.bfloat16 if bits == 16 else torch.int8
+        scales = [None, None] if bits == 16 else [torch.zeros(shape[:3], dtype=torch.float32, device=device) for _ in range(2)]
+        self._set(torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device), head_dim, *scales)
+
+    @classmethod
+    def from_tensors(cls, k: torch.Tensor, v: torch.Tensor, head_dim: int, k_scale: torch.Tensor | None = None,
+                     v_scale: torch.Tensor | None = None) -> "KVCache":
+        """A cache over tensors that the caller allocated."""
+        self = cls.__new__(cls)
+        self._set(k, v, head_dim, k_scale, v_scale)
+        return self
+
+    def _set(self, k, v, head_dim, k_scale, v_scale):
+        where = "bitlinear_kv_cache"
+        if k.dim() != 4 or k.shape != v.shape or k.shape[3] != (head_dim + 15) // 16 * 16:
+            _refuse(where, "k and v are [n_pages, kv_heads, page_size, head_dim rounded up to 16]", ERR_SHAPE)
+        if k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.int8):
+            _refuse(where, "k and v are both bf16 or both int8")
+        bits = 16 if k.dtype == torch.bfloat16 else 8
+        for s in (k_scale, v_scale):
+            if (s is None) != (bits == 16) or (s is not None and (s.shape != k.shape[:3] or s.dtype != torch.float32)):
+                _refuse(where, "an int8 cache has fp32 scales [n_pages, kv_heads, page_size], a bf16 cache has none")
+        if not all(t is None or (t.is_cuda and t.device == k.device and t.is_contiguous()) for t in (k, v, k_scale, v_scale)):
+            _refuse(where, "the tensors are contiguous and on one CUDA device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.kv_heads, self.page_size = k.shape[:3]
+        self.head_dim, self.bits, self.device = head_dim, bits, k.device
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._desc = KVCacheDesc(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(self.status), self.n_pages, self.kv_heads,
+                                 head_dim, self.page_size, bits)
+        self._address = ctypes.addressof(self._desc)
+
+    def check(self):
+        """Waits for the device and raises if a call met a bad page, length or position; clears the status."""
+        status = int(self.status.item())
+        if status != OK:
+            self.status.zero_()
+            raise BitLinearError(status, "bitlinear_kv_cache")
+
+
+class KVBatch:
+    """bitlinear_kv_batch: the sequences of a call.  page_table int32 [n_seqs, pages], kv_lens int32 [n_seqs] (with the new
+    tokens), cu_tokens int32 [n_seqs + 1] or None (one token per sequence).  The tensors are kept, not copied: a program
+    that writes new lengths and pages into them uses the same object again, in a captured graph too."""
+
+    def __init__(self, page_table: torch.Tensor, kv_lens: torch.Tensor, cu_tokens: torch.Tensor | None = None):
+        where = "bitlinear_kv_batch"
+        n = kv_lens.numel()
+        if page_table.dim() != 2 or page_table.shape[0] != n or kv_lens.dim() != 1 or \
+                (cu_tokens is not None and (cu_tokens.dim() != 1 or cu_tokens.numel() != n + 1)):
+            _refuse(where, "page_table is [n_seqs, pages], kv_lens [n_seqs], cu_tokens [n_seqs + 1]", ERR_SHAPE)
+        for t in (page_table, kv_lens, cu_tokens):
+            if t is not None and (t.dtype != torch.int32 or not t.is_cuda or t.device != kv_lens.device):
+                _refuse(where, "page_table, kv_lens and cu_tokens are int32 and on one CUDA device")
+        if (page_table.shape[1] > 1 and page_table.stride(1) != 1) or (n > 1 and kv_lens.stride(0) != 1) or \
+                (cu_tokens is not None and n > 0 and cu_tokens.stride(0) != 1):
+            _refuse(where, "kv_lens, cu_tokens and the rows of page_table are contiguous")
+        self.page_table, self.kv_lens, self.cu_tokens, self.n_seqs, self.device = page_table, kv_lens, cu_tokens, n, kv_lens.device
+        pages = page_table.shape[1]
+        stride = page_table.stride(0) if n > 1 else pages
+        self._desc = KVBatchDesc(_ptr(page_table), _ptr(kv_lens), _ptr(cu_tokens), n, stride, pages)
+        self._address = ctypes.addressof(self._desc)
+
+
+def rope_table(n_pos: int, head_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
+    """bitlinear_rope_table: -> fp32 [n_pos, head_dim / 2, 2], (cos, sin) of every position and pair."""
+    table = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=device)
+    if torch.cuda.current_device() != table.device.index:
+        with torch.cuda.device(table.device):
+            st = load_library().bitlinear_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(stream))
+    else:
+        st = load_library().bitlinear_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(stream))
+    _check(st, "bitlinear_rope_table")
+    return table
+
+
+def _row_stride(t: torch.Tensor, heads: int, head_dim: int, rows: int, device, where: str) -> int:
+    """Row stride of bf16 [rows, heads, head_dim] in elements; refuses what the kernels cannot address."""
+    if t.shape != (rows, heads, head_dim) or t.dtype != torch.bfloat16 or t.device != device:
+        _refuse(where, f"expected bf16 [{rows}, {heads}, {head_dim}] on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    s = t.stride()
+    if (head_dim > 1 and s[2] != 1) or (heads > 1 and s[1] != head_dim):
+        _refuse(where, "the heads of a row are contiguous")
+    return s[0] if rows > 1 else (heads * head_dim + 7) // 8 * 8
+
+
+def _empty_rows(rows: int, heads: int, head_dim: int, device) -> torch.Tensor:
+    """bf16 [rows, heads, head_dim] whose rows start on 16-byte boundaries."""
+    n = heads * head_dim
+    t = torch.empty((rows, (n + 7) // 8 * 8), dtype=torch.bfloat16, device=device)
+    return t.as_strided((rows, heads, head_dim), (t.shape[1], head_dim, 1))
+
+
+def _same_device(cache: KVCache, batch: KVBatch, where: str):
+    if batch.device != cache.device:
+        _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
+
+
+def kv_append(cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor | None = None,
+              rope: torch.Tensor | None = None, interleaved: bool = False, q_out: torch.Tensor | None = None, stream=None):
+    """bitlinear_kv_append: rotates k [T, kv_heads, head_dim] and stores it with v in the cache; rotates q [T, heads, head_dim]
+    into q_out (allocated if not given, may be q itself) and returns it (None without q)."""
+    where = "bitlinear_kv_append"
+    device = cache.device
+    _same_device(cache, batch, where)
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return kv_append(cache, batch, k, v, q, rope, interleaved, q_out, stream)
+    T, D = k.shape[0], cache.head_dim
+    ks = _row_stride(k, cache.kv_heads, D, T, device, where)
+    vs = _row_stride(v, cache.kv_heads, D, T, device, where)
+    heads = qs = os_ = positions = 0
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else 0
+        qs = _row_stride(q, heads, D, T, device, where)
+        if q_out is None:
+            q_out = _empty_rows(T, heads, D, device)
+        os_ = _row_stride(q_out, heads, D, T, device, where)
+    elif q_out is not None:
+        _refuse(where, "q_out without q")
+    if rope is not None:
+        positions = rope.shape[0]
+        if rope.shape != (positions, D // 2, 2) or rope.dtype != torch.float32 or not rope.is_contiguous() or rope.device != device:
+            _refuse(where, f"rope is a contiguous fp32 [positions, {D // 2}, 2] on {device}")
+    st = (_lib or load_library()).bitlinear_kv_append(
+        cache._address, batch._address, k.data_ptr(), ks, v.data_ptr(), vs, 0 if q is None else q.data_ptr(), qs, T, heads,
+        0 if rope is None else rope.data_ptr(), positions, 1 if interleaved else 0, 0 if q_out is None else q_out.data_ptr(), os_,
+        _stream(stream))
+    _check(st, where)
+    return q_out
+
+
+def attend_workspace_bytes(heads: int, kv_heads: int, head_dim: int, prompt: bool) -> int:
+    return int(load_library().bitlinear_attend_workspace_bytes(heads, kv_heads, head_dim, 1 if prompt else 0))
+
+
+def alloc_attend_workspace(heads: int, kv_heads: int, head_dim: int, prompt: bool, device="cuda") -> torch.Tensor:
+    """A workspace for attend_decode (prompt False) or attend_prompt (prompt True), zeroed as its first use needs it."""
+    n = attend_workspace_bytes(heads, kv_heads, head_dim, prompt)
+    if n == 0:
+        raise BitLinearError(ERR_SHAPE, "bitlinear_attend_workspace_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def _attend(prompt: bool, cache: KVCache, batch: KVBatch, q, scale, out, workspace, stream):
+    where = "bitlinear_attend_prompt" if prompt else "bitlinear_attend_decode"
+    device = cache.device
+    _same_device(cache, batch, where)
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _attend(prompt, cache, batch, q, scale, out, workspace, stream)
+    if q.dim() != 3:
+        _refuse(where, "q is [tokens, heads, head_dim]", ERR_SHAPE)
+    T, heads, D = q.shape[0], q.shape[1], cache.head_dim
+    if not prompt and T != batch.n_seqs:
+        _refuse(where, f"{batch.n_seqs} sequences and {T} tokens", ERR_SHAPE)
+    qs = _row_stride(q, heads, D, T, device, where)
+    if out is None:
+        out = _empty_rows(T, heads, D, device)
+    os_ = _row_stride(out, heads, D, T, device, where)
+    if workspace is None:
+        workspace = alloc_attend_workspace(heads, cache.kv_heads, D, prompt, device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        _refuse(where, f"the workspace is contiguous and on {device}")
+    scale = D ** -0.5 if scale is None else float(scale)
+    nbytes = workspace.numel() * workspace.element_size()
+    L = _lib or load_library()
+    if prompt:
+        st = L.bitlinear_attend_prompt(cache._address, batch._address, q.data_ptr(), qs, T, heads, scale, out.data_ptr(), os_,
+                                       workspace.data_ptr(), nbytes, _stream(stream))
+    else:
+        st = L.bitlinear_attend_decode(cache._address, batch._address, q.data_ptr(), qs, heads, scale, out.data_ptr(), os_,
+                                       workspace.data_ptr(), nbytes, _stream(stream))
+    _check(st, where)
+    return out
+
+
+def attend_decode(cache: KVCache, batch: KVBatch, q: torch.Tensor, scale: float | None = None, out: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """bitlinear_attend_decode: attention of the one new token of each sequence, bf16 [n_seqs, heads, head_dim] -> the same.
+    scale: 1 / sqrt(head_dim) if not given."""
+    return _attend(False, cache, batch, q, scale, out, workspace, stream)
+
+
+def attend_prompt(cache: KVCache, batch: KVBatch, q: torch.Tensor, scale: float | None = None, out: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """bitlinear_attend_prompt: causal attention of the new tokens of prompts and prompt chunks, bf16 [T, heads, head_dim] ->
+    the same; rows of out behind the last sequence keep what they held."""
+    return _attend(True, cache, batch, q, scale, out, workspace, stream)

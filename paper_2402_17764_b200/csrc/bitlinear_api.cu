@@ -37,8 +37,6 @@ int sm_count()
     return cached[dev];
 }
 
-namespace {
-
 bool device_is_sm100()
 {
     static int cached[64] = {0}; // 0 unknown, 1 yes, 2 no
@@ -52,7 +50,7 @@ bool device_is_sm100()
     return cached[dev] == 1;
 }
 
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+namespace {
 
 bitlinear_status check_shape(int64_t M, int64_t N, int64_t K)
 {
@@ -209,6 +207,7 @@ const char *bitlinear_status_string(bitlinear_status s)
     case BITLINEAR_ERR_CUDA: return "CUDA call failed";
     case BITLINEAR_ERR_TIMEOUT: return "device-side wait timed out";
     case BITLINEAR_ERR_RANGE: return "weight out of range";
+    case BITLINEAR_ERR_PAGE: return "page, length or position out of range";
     case BITLINEAR_ERR_BADCODE: return "packed weights hold the unused 2-bit code";
     default: return "unknown status";
     }

@@ -164,5 +164,7 @@ WaitHooks take_wait_hooks();
 cudaError_t launch_int8_issue_probe(int iters, int32_t *status, int *ctas, cudaStream_t stream);
 
 int sm_count();
+bool device_is_sm100(); // of the current device
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 } // namespace bitlinear

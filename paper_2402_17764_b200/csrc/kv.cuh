@@ -1,0 +1,108 @@
+// What the kernels around the paged key-value cache share: the views of the cache and of a call's sequences, and the
+// look-ups into them.  Nothing that comes from device memory (lengths, page numbers) is used as an index unchecked.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "internal.cuh"
+
+namespace bitlinear {
+
+constexpr int kMaxHeadDim = 128;
+constexpr int kMaxKvHeads = 1024;
+constexpr int kMaxHeads = 4096;
+
+// Elements of a cache row: the head padded to 16 elements (a whole 32-byte sector in bf16, a 16-byte piece in int8).
+__host__ __device__ inline int kv_row_width(int head_dim) { return (head_dim + 15) / 16 * 16; }
+
+struct KvCache {
+    void *k, *v;            // bf16 or int8 [n_pages][kv_heads][page_size][width]
+    float *k_scale, *v_scale; // null for bf16
+    int32_t *status;
+    int32_t n_pages, kv_heads, head_dim, width, page_shift;
+};
+
+struct KvBatch {
+    const int32_t *page_table, *kv_lens, *cu_tokens;
+    int32_t n_seqs;
+    int32_t capacity; // positions a row of the page table covers
+    int64_t table_stride;
+};
+
+// Reports a bad page, length or position.
+__device__ __forceinline__ void kv_report(const KvCache &c) { *c.status = BITLINEAR_ERR_PAGE; }
+
+// The length of sequence b, cut to what its row of the page table covers; over_long: it was cut.
+__host__ __device__ __forceinline__ int kv_length(const KvBatch &s, int b, bool &over_long)
+{
+    const int n = s.kv_lens[b];
+    over_long = n > s.capacity;
+    return n < 0 ? 0 : (over_long ? s.capacity : n);
+}
+
+// Page of a position inside the capacity; -1 if the table holds a number the cache does not have.
+__host__ __device__ __forceinline__ int kv_page(const KvCache &c, const KvBatch &s, int b, int pos)
+{
+    const int page = s.page_table[(int64_t)b * s.table_stride + (pos >> c.page_shift)];
+    return (uint32_t)page < (uint32_t)c.n_pages ? page : -1;
+}
+
+// Row of the cache, counted over all pages, heads and slots (less than 2^31 of them).
+__host__ __device__ __forceinline__ int kv_row(const KvCache &c, int page, int head, int pos)
+{
+    return ((page * c.kv_heads + head) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
+}
+
+// Sequence of token row t, or -1 if it has none; `first` and `count`: its token rows.
+__host__ __device__ __forceinline__ int kv_sequence_of(const KvBatch &s, int t, int &first, int &count)
+{
+    if (!s.cu_tokens) {
+        first = t;
+        count = 1;
+        return t < s.n_seqs ? t : -1;
+    }
+    int lo = 0, hi = s.n_seqs; // the first b whose rows end behind t
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (s.cu_tokens[mid + 1] > t)
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    if (lo >= s.n_seqs) return -1;
+    first = s.cu_tokens[lo];
+    count = s.cu_tokens[lo + 1] - first;
+    return first <= t ? lo : -1;
+}
+
+// ---- launchers -----------------------------------------------------------------------------------------
+
+cudaError_t launch_rope_table(float *table, int64_t n_pos, int head_dim, double base, cudaStream_t stream);
+
+struct AppendArgs {
+    KvCache cache;
+    KvBatch batch;
+    const __nv_bfloat16 *k, *v, *q;
+    __nv_bfloat16 *q_out;
+    int64_t k_stride, v_stride, q_stride, q_out_stride;
+    const float2 *rope;
+    int32_t rope_positions, T, heads, interleaved;
+};
+cudaError_t launch_kv_append(const AppendArgs &a, cudaStream_t stream);
+
+struct AttendArgs {
+    KvCache cache;
+    KvBatch batch;
+    const __nv_bfloat16 *q;
+    __nv_bfloat16 *out;
+    int64_t q_stride, out_stride;
+    int32_t T, heads;
+    float scale; // of the scores, times log2(e): the kernels work with powers of two
+    void *workspace;
+};
+size_t attend_workspace_bytes(int heads, int kv_heads, int head_dim, bool prompt);
+cudaError_t launch_attend(const AttendArgs &a, bool prompt, cudaStream_t stream);
+
+} // namespace bitlinear
