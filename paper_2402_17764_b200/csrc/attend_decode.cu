@@ -1,0 +1,613 @@
+// Attention of one new token per sequence over the paged cache.
+//
+//   out_h = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m),   s_j = scale log2(e) q_h . k_j,   m = max_j s_j
+//
+// in one pass over the cache: every warp keeps a running maximum, sum and output for its own keys, and partial results join by
+//   m = max(m1, m2),  l = l1 2^(m1 - m) + l2 2^(m2 - m),  o = o1 2^(m1 - m) + o2 2^(m2 - m).
+//
+// What bounds it: reading the cache once (HBM).  So all query heads of a kv head are handled together (8 or 16 columns of
+// a matrix instruction), and the work is cut by bytes, not by sequences: the blocks of all (sequence, kv head) pairs stand
+// in one row, and every CTA takes an equal, contiguous share of it, wherever that begins and ends.  A pair that several
+// CTAs share is joined by whichever of them finishes last, in the order of the shares, so the result does not depend on
+// which one it was.
+//
+// Inside a CTA each of the four warps streams keys of its own through a ring of its own (cp.async, 8 KB per stage, no
+// barrier between warps before the end of a pair): the ring keeps loading the next pair's keys while this one's are
+// finished.  Scores are K Q^T (keys are the 16 rows of the instruction, queries its 8 columns) and the output is
+// V^T P^T (16 elements of the head, 8 queries), so that a group of 1 to 8 query heads wastes at most the columns it does not have;
+// P^T changes from accumulator to operand by movmatrix.  The weights enter as two bf16 parts (value and remainder): the
+// tensor cores have time for it, and the result is as exact as fp32 weights would give.  int8 rows become bf16 exactly
+// (code_pair below); a key's scale multiplies its score, a value's scale its weight.
+#include <algorithm>
+
+#include "internal.cuh"
+#include "kv.cuh"
+#include "ptx.cuh"
+
+namespace bitlinear {
+namespace {
+
+using namespace ptx;
+
+constexpr int kWarps = 4;
+constexpr int kStageBytes = 8192; // keys and values of a stage
+constexpr int kMaxSplits = 2;     // partial results of a CTA: of the pair it begins in the middle of, of the one it ends in the middle of
+
+// WT: elements of a cache row in shared memory (the row's width rounded up to 64 or 128).  NT: 8-query tiles.
+template <bool kInt8, int WT, int NT>
+struct Shape {
+    static constexpr int kRowBytes = WT * (kInt8 ? 1 : 2);
+    static constexpr int kKeys = kStageBytes / 2 / kRowBytes; // of a stage: 16, 32 or 64
+    static constexpr int kChunks = kRowBytes / 16;
+    static constexpr int kScaleBytes = kInt8 ? kKeys * 8 : 0; // fp32 scales of the keys and the values
+    static constexpr int kStage = kStageBytes + kScaleBytes;
+    static constexpr int kStages = 3;
+    static constexpr int kQ = 8 * NT;
+    static constexpr int kSmem = kWarps * kStages * kStage + kWarps * kQ * 8;
+    static_assert(kQ * WT * 4 <= kStageBytes, "a warp's output fits the stage that it has just used up");
+    static constexpr int kPartFloats = kQ * (WT + 2); // a partial result in the workspace
+};
+
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, bool real)
+{
+    const int n = real ? 16 : 0; // 0: the 16 bytes become zero and nothing is read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t movmatrix(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float y;
+    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// Two signed bytes of w as two bf16 numbers, exactly.  0x43 in front of a byte makes the bf16 number 128 + its low seven bits
+// when its top bit is 0; 128 or, with the top bit alone, 256 is then subtracted: b - 0 or b - 256.
+template <uint32_t kSelect>
+__device__ __forceinline__ uint32_t code_pair(uint32_t w)
+{
+    const uint32_t t = __byte_perm(w, 0x43434343u, kSelect);
+    const uint32_t x = t & 0xFF7FFF7Fu, y = t & 0xFF80FF80u;
+    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&d);
+}
+
+// Byte offset of 16-byte piece c of row r of a stage's keys or values: the eight rows that an ldmatrix reads at one
+// c lie in eight different bank groups.
+template <int kRowBytes>
+__device__ __forceinline__ uint32_t piece(int r, int c)
+{
+    const int x = kRowBytes >= 128 ? (r & 7) : ((r >> 1) & 3);
+    return (uint32_t)(r * kRowBytes + ((c ^ x) << 4));
+}
+
+// A place in the row of all blocks: block `blk` of pair `pair` (kv head and chunk of its query heads) of sequence b.
+struct Place {
+    int b, pair, blk, nblk, len;
+};
+
+struct Plan {
+    int64_t total;      // blocks of all pairs
+    int shares;         // CTAs that have work
+    __device__ __forceinline__ int64_t begin_of(int i) const { return total * i / shares; }
+    __device__ __forceinline__ int share_of(int64_t block) const { return (int)(((block + 1) * shares - 1) / total); }
+};
+
+template <bool kInt8, int WT, int NT>
+__global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads)
+{
+    using S = Shape<kInt8, WT, NT>;
+    constexpr int kKeys = S::kKeys, kBlock = kWarps * kKeys, kSteps = WT / 16, kRB = S::kRowBytes;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int64_t scan[kWarps + 1];
+    __shared__ int64_t found_rest;
+    __shared__ int found_b, is_last;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, tq = lane % 4;
+    const int group = a.heads / a.cache.kv_heads, D = a.cache.head_dim, W = a.cache.width;
+    const int pairs = a.cache.kv_heads * chunks, n_seqs = a.batch.n_seqs;
+
+    // ---- the row of all blocks: its length, and where this CTA's share begins --------------------------------
+    const int per_thread = (n_seqs + kWarps * 32 - 1) / (kWarps * 32);
+    const int b0 = min(n_seqs, tid * per_thread), b1 = min(n_seqs, b0 + per_thread);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) {
+        bool over;
+        const int n = kv_length(a.batch, b, over);
+        if (over && blockIdx.x == 0) kv_report(a.cache);
+        mine += (int64_t)((n + kBlock - 1) / kBlock) * pairs;
+    }
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= d) upto += x;
+    }
+    if (lane == 31) scan[warp] = upto;
+    __syncthreads();
+    Plan plan;
+    plan.total = 0;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) upto += scan[w];
+        plan.total += scan[w];
+    }
+    plan.shares = (int)(plan.total < (int64_t)gridDim.x ? plan.total : (int64_t)gridDim.x);
+
+    // empty slots of the batch get zeros
+    for (int b = blockIdx.x; b < n_seqs; b += gridDim.x) {
+        if (a.batch.kv_lens[b] > 0) continue;
+        uint32_t *row = reinterpret_cast<uint32_t *>(a.out + (int64_t)b * a.out_stride);
+        for (int i = tid; i < a.heads * D / 2; i += kWarps * 32) row[i] = 0u;
+    }
+    if ((int)blockIdx.x >= plan.shares) return;
+    const int64_t share_begin = plan.begin_of(blockIdx.x), share_end = plan.begin_of(blockIdx.x + 1);
+    if (share_begin >= upto - mine && share_begin < upto) {
+        int64_t rest = share_begin - (upto - mine);
+        int b = b0;
+        for (;; ++b) {
+            bool over;
+            const int64_t blocks = (int64_t)((kv_length(a.batch, b, over) + kBlock - 1) / kBlock) * pairs;
+            if (rest < blocks) break;
+            rest -= blocks;
+        }
+        found_b = b;
+        found_rest = rest;
+    }
+    __syncthreads();
+
+    auto length = [&](int b) {
+        bool over;
+        return kv_length(a.batch, b, over);
+    };
+    Place first;
+    first.b = found_b;
+    first.len = length(first.b);
+    first.nblk = (first.len + kBlock - 1) / kBlock;
+    first.pair = (int)(found_rest / first.nblk);
+    first.blk = (int)(found_rest - (int64_t)first.pair * first.nblk);
+    auto advance = [&](Place &p) { // only called while blocks are left behind p
+        if (++p.blk < p.nblk) return;
+        p.blk = 0;
+        if (++p.pair < pairs) return;
+        p.pair = 0;
+        do p.len = length(++p.b);
+        while (p.len == 0);
+        p.nblk = (p.len + kBlock - 1) / kBlock;
+    };
+
+    // ---- the ring --------------------------------------------------------------------------------------
+    uint8_t *ring = smem + warp * S::kStages * S::kStage;
+    const uint32_t ring_addr = smem_u32(ring);
+    float2 *join_ml = reinterpret_cast<float2 *>(smem + kWarps * S::kStages * S::kStage); // (m, l) of [warp][query]
+
+    // page numbers of the 16-key groups of this warp's part of a block, one per lane
+    auto pages_of = [&](const Place &p) {
+        int page = -1;
+        if (lane < kKeys / 16) {
+            const int pos = p.blk * kBlock + warp * kKeys + lane * 16;
+            if (pos < p.len) {
+                page = kv_page(a.cache, a.batch, p.b, pos);
+                if (page < 0) kv_report(a.cache);
+            }
+        }
+        return page;
+    };
+    auto fetch = [&](const Place &p, int pages, int stage) {
+        const uint32_t at = ring_addr + stage * S::kStage;
+        const int key0 = p.blk * kBlock + warp * kKeys;
+        const int n = p.len - key0; // keys that exist
+        if (n <= 0) return;
+        const int head = p.pair / chunks;
+        constexpr int kRowsAtOnce = 32 / S::kChunks > 0 ? 32 / S::kChunks : 1;
+        const int c = lane % S::kChunks, r0 = lane / S::kChunks;
+        const bool real_c = c * 16 < W * (kInt8 ? 1 : 2);
+#pragma unroll
+        for (int q = 0; q < kKeys / 16; ++q) {
+            const int page = __shfl_sync(0xFFFFFFFFu, pages, q);
+            const bool have = page >= 0;
+            const int64_t row = have ? kv_row(a.cache, page, head, key0 + q * 16) : 0;
+            const int64_t offset = row * W * (kInt8 ? 1 : 2) + c * 16;
+            const uint8_t *k = reinterpret_cast<const uint8_t *>(a.cache.k) + offset, *v = reinterpret_cast<const uint8_t *>(a.cache.v) + offset;
+#pragma unroll
+            for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+                const int r = q * 16 + i * kRowsAtOnce + r0;
+                const bool real = have && real_c && r < n;
+                const int64_t skip = real ? (int64_t)(r - q * 16) * W * (kInt8 ? 1 : 2) : -c * 16; // (an address that exists in any case)
+                cp_async_16(at + piece<kRB>(r, c), k + skip, real);
+                cp_async_16(at + kStageBytes / 2 + piece<kRB>(r, c), v + skip, real);
+            }
+            if (kInt8 && lane < 8) { // 4 pieces of 4 scales for the keys, 4 for the values
+                const float *src = lane < 4 ? a.cache.k_scale : a.cache.v_scale;
+                cp_async_16(at + kStageBytes + (lane < 4 ? 0 : kKeys * 4) + q * 64 + (lane & 3) * 16, src + (have ? row + (lane & 3) * 4 : 0), have);
+            }
+        }
+    };
+
+    // ---- a pair's state ----------------------------------------------------------------------------------
+    uint32_t qf[NT][kSteps][2];
+    float o[NT][kSteps][4], m[NT][2], l[NT][2];
+    auto begin_pair = [&](const Place &p) {
+        const int head = p.pair / chunks, chunk = p.pair % chunks;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int i = chunk * chunk_heads + t * 8 + g; // query head of the group that is this lane's column
+            const bool have = t * 8 + g < chunk_heads && i < group;
+            const __nv_bfloat16 *q = a.q + (int64_t)p.b * a.q_stride + (int64_t)(head * group + (have ? i : 0)) * D;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                // the instruction's k index runs over the head's elements in the order in which K's registers hold them
+                const int e0 = s * 16 + (kInt8 ? 4 * tq : 2 * tq), e1 = e0 + (kInt8 ? 2 : 8);
+                qf[t][s][0] = have && e0 < D ? *reinterpret_cast<const uint32_t *>(q + e0) : 0u;
+                qf[t][s][1] = have && e1 < D ? *reinterpret_cast<const uint32_t *>(q + e1) : 0u;
+                o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.0f;
+            }
+            m[t][0] = m[t][1] = -INFINITY;
+            l[t][0] = l[t][1] = 0.0f;
+        }
+    };
+
+    // one stage: the scores of its keys, the weights, and their share of the output
+    auto consume = [&](const Place &p, int pages, int stage) {
+        const int key0 = p.blk * kBlock + warp * kKeys;
+        const int n = p.len - key0;
+        if (n <= 0) return;
+        const uint32_t at = ring_addr + stage * S::kStage;
+        const float *scales = reinterpret_cast<const float *>(ring + stage * S::kStage + kStageBytes);
+        constexpr int kGroups = kKeys / 16;
+        float s[kGroups][NT][4];
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[q][t][0] = s[q][t][1] = s[q][t][2] = s[q][t][3] = 0.0f;
+            const int r = q * 16 + (lane & 15);
+            if (!kInt8) {
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    uint32_t k[4];
+                    ldmatrix_x4(at + piece<kRB>(r, 2 * i + (lane >> 4)), k);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) mma_bf16(s[q][t], k, qf[t][i][0], qf[t][i][1]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kSteps; i += 2) {
+                    uint32_t w[4];
+                    ldmatrix_x4(at + piece<kRB>(r, i + (lane >> 4)), w);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t k[4] = {code_pair<0x4140>(w[2 * j]), code_pair<0x4140>(w[2 * j + 1]), code_pair<0x4342>(w[2 * j]),
+                                               code_pair<0x4342>(w[2 * j + 1])};
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) mma_bf16(s[q][t], k, qf[t][i + j][0], qf[t][i + j][1]);
+                    }
+                }
+            }
+        }
+        // scale, mask, running maximum
+        bool bad = false;
+        if (lane < kGroups) bad = pages < 0;
+        const uint32_t bad_groups = __ballot_sync(0xFFFFFFFFu, bad);
+        const bool all = n >= kKeys && bad_groups == 0u;
+        float top[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) top[t][0] = m[t][0], top[t][1] = m[t][1];
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = q * 16 + h * 8 + g;
+                const float f = kInt8 ? a.scale * scales[r] : a.scale;
+                const bool seen = all || (r < n && !((bad_groups >> q) & 1u));
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float &x = s[q][t][2 * h + j];
+                        x = seen ? x * f : -INFINITY;
+                        top[t][j] = fmaxf(top[t][j], x);
+                    }
+            }
+        float base[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) top[t][j] = fmaxf(top[t][j], __shfl_xor_sync(0xFFFFFFFFu, top[t][j], d));
+                base[t][j] = top[t][j] == -INFINITY ? 0.0f : top[t][j];
+                const float keep = exp2_approx(m[t][j] - base[t][j]);
+                m[t][j] = top[t][j];
+                l[t][j] *= keep;
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    o[t][i][j] *= keep;
+                    o[t][i][2 + j] *= keep;
+                }
+            }
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) {
+            uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = q * 16 + h * 8 + g;
+                const bool seen = all || (r < n && !((bad_groups >> q) & 1u));
+                const float vs = kInt8 ? (seen ? scales[kKeys + r] : 0.0f) : 1.0f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    float w[2], rest[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        w[j] = exp2_approx(s[q][t][2 * h + j] - base[t][j]);
+                        l[t][j] += w[j];
+                        if (kInt8) w[j] *= vs;
+                    }
+                    const uint32_t x = pack_bf16(w[0], w[1]);
+                    rest[0] = w[0] - __uint_as_float(x << 16);
+                    rest[1] = w[1] - __uint_as_float(x & 0xFFFF0000u);
+                    hi[t][h] = movmatrix(x);
+                    lo[t][h] = movmatrix(pack_bf16(rest[0], rest[1]));
+                }
+            }
+            if (!kInt8) {
+                // matrices in the order (elements 0-7, keys 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15)
+                const int r = q * 16 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    uint32_t v[4];
+                    ldmatrix_x4_trans(at + kStageBytes / 2 + piece<kRB>(r, 2 * i + ((lane >> 3) & 1)), v);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        mma_bf16(o[t][i], v, hi[t][0], hi[t][1]);
+                        mma_bf16(o[t][i], v, lo[t][0], lo[t][1]);
+                    }
+                }
+            } else {
+                // a 16-bit element of the transposed matrices is two neighbours of the head: rows 0-7 of the instruction take
+                // the even ones, rows 8-15 the odd ones
+                const int r = q * 16 + (lane & 15);
+#pragma unroll
+                for (int i = 0; i < kSteps; i += 2) {
+                    uint32_t w[4];
+                    ldmatrix_x4_trans(at + kStageBytes / 2 + piece<kRB>(r, i + (lane >> 4)), w);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t v[4] = {code_pair<0x4240>(w[2 * j]), code_pair<0x4341>(w[2 * j]), code_pair<0x4240>(w[2 * j + 1]),
+                                               code_pair<0x4341>(w[2 * j + 1])};
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            mma_bf16(o[t][i + j], v, hi[t][0], hi[t][1]);
+                            mma_bf16(o[t][i + j], v, lo[t][0], lo[t][1]);
+                        }
+                    }
+                }
+            }
+        }
+    };
+
+    // ---- the end of a pair, or of this CTA's part of it -----------------------------------------------------
+    char *ws = reinterpret_cast<char *>(a.workspace);
+    uint32_t *counters = reinterpret_cast<uint32_t *>(ws);
+    float *parts = reinterpret_cast<float *>(ws + decode_counter_bytes());
+    auto part_of = [&](int share, int which) { return parts + (int64_t)(share * kMaxSplits + which) * S::kPartFloats; };
+    auto store_out = [&](const Place &p, int q, int e, float x, float y) { // two neighbours of a query head's output
+        const int head = p.pair / chunks, i = (p.pair % chunks) * chunk_heads + q;
+        if (q < chunk_heads && i < group && e < D)
+            *reinterpret_cast<uint32_t *>(a.out + (int64_t)p.b * a.out_stride + (int64_t)(head * group + i) * D + e) = pack_bf16(x, y);
+    };
+    // The warps lay their outputs down as [query][element] in the stage they have just used up (the next fetch into it
+    // comes after this); element e of query q stands at e ^ 8 (q / 2 % 4), so that the lanes of a store hit 32 banks.
+    auto laid = [](int q, int e) { return q * WT + (e ^ (((q >> 1) & 3) << 3)); };
+    auto end_pair = [&](const Place &p, int64_t block, int stage) { // p: the last block of the pair that this CTA has, at `block` in the row
+        __syncwarp();
+        float *own = reinterpret_cast<float *>(ring + stage * S::kStage);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int q = t * 8 + 2 * tq + j;
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[t][j] += __shfl_xor_sync(0xFFFFFFFFu, l[t][j], d);
+                if (g == 0) join_ml[warp * S::kQ + q] = make_float2(m[t][j], l[t][j]);
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    const int e = i * 16 + (kInt8 ? 2 * g : g);
+                    own[laid(q, e)] = o[t][i][j];
+                    own[laid(q, e + (kInt8 ? 1 : 8))] = o[t][i][2 + j];
+                }
+            }
+        __syncthreads();
+        const int64_t pair_begin = block - p.blk, pair_end = pair_begin + p.nblk;
+        const bool whole = pair_begin >= share_begin && pair_end <= share_end;
+        const int which = pair_begin < share_begin ? 0 : 1;
+        float *part = whole ? nullptr : part_of(blockIdx.x, which);
+        for (int i = tid; i < S::kQ * WT / 2; i += kWarps * 32) {
+            const int q = i / (WT / 2), e = i % (WT / 2) * 2;
+            float2 ml[kWarps];
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                ml[w] = join_ml[w * S::kQ + q];
+                M = fmaxf(M, ml[w].x);
+            }
+            const float base = M == -INFINITY ? 0.0f : M;
+            float x = 0.0f, y = 0.0f, L = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = exp2_approx(ml[w].x - base);
+                const float2 v = *reinterpret_cast<const float2 *>(smem + (w * S::kStages + stage) * S::kStage + 4 * laid(q, e));
+                x += f * v.x;
+                y += f * v.y;
+                L += f * ml[w].y;
+            }
+            if (whole) {
+                const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+                store_out(p, q, e, x * inv, y * inv);
+            } else {
+                *reinterpret_cast<float2 *>(part + 2 * S::kQ + q * WT + e) = make_float2(x, y);
+                if (e == 0) *reinterpret_cast<float2 *>(part + 2 * q) = make_float2(M, L);
+            }
+        }
+        if (!whole) {
+            const int from = plan.share_of(pair_begin), to = plan.share_of(pair_end - 1);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                // the counter of the CTA in which the pair begins: at most one shared pair begins in a share
+                const uint32_t before = atomicAdd(counters + from, 1u);
+                is_last = before == (uint32_t)(to - from);
+                if (is_last) counters[from] = 0u; // as the next call expects it
+            }
+            __syncthreads();
+            if (is_last) {
+                __threadfence();
+                for (int i = tid; i < S::kQ * WT / 4; i += kWarps * 32) {
+                    const int q = i / (WT / 4), e = i % (WT / 4) * 4;
+                    float M = -INFINITY;
+                    for (int c = from; c <= to; ++c) M = fmaxf(M, __ldcg(part_of(c, c == from ? 1 : 0) + 2 * q));
+                    const float base = M == -INFINITY ? 0.0f : M;
+                    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    float L = 0.0f;
+#pragma unroll 4
+                    for (int c = from; c <= to; ++c) {
+                        const float *src = part_of(c, c == from ? 1 : 0);
+                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(src + 2 * q));
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(src + 2 * S::kQ + q * WT + e));
+                        const float f = exp2_approx(ml.x - base);
+                        x.x += f * v.x;
+                        x.y += f * v.y;
+                        x.z += f * v.z;
+                        x.w += f * v.w;
+                        L += f * ml.y;
+                    }
+                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+                    store_out(p, q, e, x.x * inv, x.y * inv);
+                    store_out(p, q, e + 2, x.z * inv, x.w * inv);
+                }
+            }
+        }
+        __syncthreads();
+    };
+
+    // ---- the share -----------------------------------------------------------------------------------------
+    // Three places walk along the share: the block whose page numbers are being looked up, the one being fetched (one
+    // block behind it) and the one being consumed (kStages - 1 behind that).
+    constexpr int kAhead = S::kStages - 1;
+    const int64_t blocks = share_end - share_begin;
+    Place now = first, get = first, look = first;
+    int pages_look = pages_of(look), pages_held[kAhead + 1];
+    int64_t fetched = 0;
+    auto fetch_next = [&](int stage) { // returns the page numbers of the block it fetched
+        int pages = -1;
+        if (fetched < blocks) {
+            pages = pages_look;
+            if (fetched + 1 < blocks) {
+                advance(look);
+                pages_look = pages_of(look);
+            }
+            fetch(get, pages, stage);
+            get = look;
+            ++fetched;
+        }
+        cp_async_commit();
+        return pages;
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) pages_held[i] = fetch_next(i);
+    begin_pair(now);
+    int stage = 0;
+    for (int64_t i = 0; i < blocks; ++i) {
+        cp_async_wait<kAhead - 1>();
+        __syncwarp();
+        pages_held[kAhead] = fetch_next(stage == 0 ? kAhead : stage - 1);
+        consume(now, pages_held[0], stage);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) pages_held[j] = pages_held[j + 1];
+        const bool ends = now.blk + 1 == now.nblk;
+        if (ends || i + 1 == blocks) end_pair(now, share_begin + i, stage);
+        stage = stage == kAhead ? 0 : stage + 1;
+        if (i + 1 < blocks) {
+            advance(now);
+            if (ends) begin_pair(now);
+        }
+    }
+    cp_async_wait<0>();
+}
+
+template <bool kInt8, int WT, int NT>
+cudaError_t launch(const AttendArgs &a, int chunks, int chunk_heads, cudaStream_t stream)
+{
+    using S = Shape<kInt8, WT, NT>;
+    static bool ready[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!ready[dev]) {
+        e = cudaFuncSetAttribute(attend_decode_kernel<kInt8, WT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+        if (e != cudaSuccess) return e;
+        ready[dev] = true;
+    }
+    attend_decode_kernel<kInt8, WT, NT><<<std::min(2 * sm_count(), kDecodeMaxCtas), kWarps * 32, S::kSmem, stream>>>(a, chunks, chunk_heads);
+    return cudaGetLastError();
+}
+
+} // namespace
+
+// Query heads of a kv head are taken up to 16 at a time (two tiles of 8 columns; a single tile where at most 8 are left).
+void decode_chunks(int group, int &chunks, int &chunk_heads)
+{
+    chunks = (group + 15) / 16;
+    chunk_heads = (group + chunks - 1) / chunks;
+}
+
+size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim)
+{
+    int chunks, chunk_heads;
+    decode_chunks(heads / kv_heads, chunks, chunk_heads);
+    const size_t q = chunk_heads <= 8 ? 8 : 16, width = kv_row_width(head_dim) <= 64 ? 64 : 128;
+    return align_up(decode_counter_bytes() + (size_t)kDecodeMaxCtas * kMaxSplits * q * (width + 2) * 4, 256);
+}
+
+cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream)
+{
+    int chunks, chunk_heads;
+    decode_chunks(a.heads / a.cache.kv_heads, chunks, chunk_heads);
+    const bool narrow = a.cache.width <= 64, one = chunk_heads <= 8;
+    if (a.cache.k_scale) {
+        if (narrow) return one ? launch<true, 64, 1>(a, chunks, chunk_heads, stream) : launch<true, 64, 2>(a, chunks, chunk_heads, stream);
+        return one ? launch<true, 128, 1>(a, chunks, chunk_heads, stream) : launch<true, 128, 2>(a, chunks, chunk_heads, stream);
+    }
+    if (narrow) return one ? launch<false, 64, 1>(a, chunks, chunk_heads, stream) : launch<false, 64, 2>(a, chunks, chunk_heads, stream);
+    return one ? launch<false, 128, 1>(a, chunks, chunk_heads, stream) : launch<false, 128, 2>(a, chunks, chunk_heads, stream);
+}
+
+} // namespace bitlinear

@@ -85,18 +85,16 @@ __global__ void __launch_bounds__(128) attend_rows_kernel(const __grid_constant_
 
 } // namespace
 
-size_t attend_workspace_bytes(int heads, int kv_heads, int head_dim, bool prompt)
+size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim)
 {
     (void)heads;
     (void)kv_heads;
     (void)head_dim;
-    (void)prompt;
     return 256;
 }
 
-cudaError_t launch_attend(const AttendArgs &a, bool prompt, cudaStream_t stream)
+cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream)
 {
-    (void)prompt;
     const int64_t units = (int64_t)a.T * a.heads;
     const unsigned blocks = (unsigned)((units + 3) / 4);
     if (a.cache.k_scale)

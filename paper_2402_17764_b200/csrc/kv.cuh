@@ -102,7 +102,14 @@ struct AttendArgs {
     float scale; // of the scores, times log2(e): the kernels work with powers of two
     void *workspace;
 };
-size_t attend_workspace_bytes(int heads, int kv_heads, int head_dim, bool prompt);
-cudaError_t launch_attend(const AttendArgs &a, bool prompt, cudaStream_t stream);
+
+// Workspace of the decode kernel: a counter per CTA, then the partial results.  The grid has at most kDecodeMaxCtas CTAs.
+constexpr int kDecodeMaxCtas = 512;
+__host__ __device__ constexpr size_t decode_counter_bytes() { return kDecodeMaxCtas * sizeof(uint32_t); }
+size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim);
+cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream);
+
+size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim);
+cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream);
 
 } // namespace bitlinear

@@ -136,6 +136,11 @@ bool heads_ok(int heads, int kv_heads, int head_dim)
            head_dim <= kMaxHeadDim && head_dim % 4 == 0;
 }
 
+size_t workspace_for(int heads, int kv_heads, int head_dim, bool prompt)
+{
+    return prompt ? attend_prompt_workspace_bytes(heads, kv_heads, head_dim) : attend_decode_workspace_bytes(heads, kv_heads, head_dim);
+}
+
 bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q, int64_t q_stride, int64_t T,
                         int heads, float softmax_scale, void *out, int64_t out_stride, void *workspace, size_t workspace_bytes,
                         void *stream, bool prompt)
@@ -149,7 +154,7 @@ bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batc
     if ((st = check_rows(q, q_stride, heads, a.cache.head_dim)) != BITLINEAR_OK) return st;
     if ((st = check_rows(out, out_stride, heads, a.cache.head_dim)) != BITLINEAR_OK) return st;
     if (!aligned(workspace, 256)) return BITLINEAR_ERR_ALIGN;
-    if (workspace_bytes < attend_workspace_bytes(heads, a.cache.kv_heads, a.cache.head_dim, prompt)) return BITLINEAR_ERR_WORKSPACE;
+    if (workspace_bytes < workspace_for(heads, a.cache.kv_heads, a.cache.head_dim, prompt)) return BITLINEAR_ERR_WORKSPACE;
     a.scale = (float)((double)softmax_scale * 1.4426950408889634074); // log2 e
     if (!std::isfinite(a.scale)) return BITLINEAR_ERR_ARG;
     if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
@@ -161,7 +166,7 @@ bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batc
     a.T = (int32_t)T;
     a.heads = heads;
     a.workspace = workspace;
-    return launch_attend(a, prompt, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+    return (prompt ? launch_attend_prompt(a, (cudaStream_t)stream) : launch_attend_decode(a, (cudaStream_t)stream)) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }
 
 } // namespace
@@ -169,7 +174,7 @@ bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batc
 size_t bitlinear_attend_workspace_bytes(int heads, int kv_heads, int head_dim, int prompt)
 {
     if (!heads_ok(heads, kv_heads, head_dim) || (prompt != 0 && prompt != 1)) return 0;
-    return attend_workspace_bytes(heads, kv_heads, head_dim, prompt != 0);
+    return workspace_for(heads, kv_heads, head_dim, prompt != 0);
 }
 
 bitlinear_status bitlinear_attend_decode(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q,
