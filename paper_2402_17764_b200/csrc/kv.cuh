@@ -109,6 +109,9 @@ __host__ __device__ constexpr size_t decode_counter_bytes() { return kDecodeMaxC
 size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim);
 cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream);
 
+// Workspace of the prompt kernel: two words per tile of rows that several CTAs share, then their partial results.
+constexpr int kPromptMaxParts = 160;
+__host__ __device__ constexpr size_t prompt_counter_bytes() { return 256 * 2 * sizeof(uint32_t); }
 size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim);
 cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream);
 

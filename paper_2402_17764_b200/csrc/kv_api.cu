@@ -149,6 +149,7 @@ bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batc
     bitlinear_status st = take_views(cache, batch, a.cache, a.batch);
     if (st != BITLINEAR_OK) return st;
     if (T < 0 || T > (1 << 20) || !heads_ok(heads, a.cache.kv_heads, a.cache.head_dim)) return BITLINEAR_ERR_SHAPE;
+    if (prompt && T * (heads / a.cache.kv_heads) > (1 << 30)) return BITLINEAR_ERR_SHAPE;
     if (prompt != (batch->cu_tokens != nullptr)) return BITLINEAR_ERR_ARG;
     if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale) || !workspace || (T > 0 && (!q || !out || q == out))) return BITLINEAR_ERR_ARG;
     if ((st = check_rows(q, q_stride, heads, a.cache.head_dim)) != BITLINEAR_OK) return st;

@@ -77,7 +77,10 @@ def attend(setup, q, counts, scale=None, weight_rounding=0.0):
       every weight is then off by a factor within 1 +- d, d = 2 max_j |ds_j| + 2^-21 + weight_rounding (one rounding of the
         weight to fewer bits, for a kernel that does that), the sums of n terms and the joins by (n + 64) 2^-24 more;
       numerator and denominator together: 2 (d + (n + 64) 2^-24) A, to first order; 1 % on top covers the second;
-      the result is rounded to bf16: 2^-8 |out|, and half the smallest subnormal step.
+      the result is rounded to bf16: 2^-8 |out|, and half the smallest subnormal step;
+      weights below 2^-126 (the smallest normal number of fp32 and bf16) may count as zero, and so may a weight times an
+      int8 row's scale: the largest weight is at least 1 (the reference is never above the maximum), so what is lost is at
+      most L 2^-126 max |v| for weights and L 2^-126 127 for weights times scales, together at most L 2^-119 max(1, max |v|).
     """
     T, H, D = q.shape
     G = H // setup.kv_heads
@@ -102,7 +105,7 @@ def attend(setup, q, counts, scale=None, weight_rounding=0.0):
             A = torch.einsum("hgnl,hld->hgnd", w, v.abs())
             worst = size.masked_fill(hidden, 0.0).amax(-1, keepdim=True) * (D + 4) * 2.0 ** -24
             d = 2 * worst + 2.0 ** -21 + weight_rounding + (L + 64) * 2.0 ** -24
-            e = 1.01 * 2 * d * A + 2.0 ** -8 * y.abs() + 2.0 ** -134
+            e = 1.01 * 2 * d * A + 2.0 ** -8 * y.abs() + 2.0 ** -134 + L * 2.0 ** -119 * max(1.0, v.abs().nan_to_num(0.0, 0.0).max().item())
             out[at:at + n] = y.permute(2, 0, 1, 3).reshape(n, H, D)
             bound[at:at + n] = e.permute(2, 0, 1, 3).reshape(n, H, D)
         at += n
