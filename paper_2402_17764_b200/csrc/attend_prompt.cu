@@ -6,16 +6,19 @@
 // R % group of the group, so one tile of keys serves them all and a chunk of few tokens still fills a tile.  A CTA owns
 // 256 rows as two tiles of 128 (the MMA's M), and walks the keys they see in blocks of 128.
 //
-// Roles (12 warps):
+// Roles (16 warps):
 //   warps 0-3, 4-7 : the softmax of tile 0 and of tile 1, one row per thread: scores from tensor memory, maximum, 2^x, the
 //                    weights as bf16 back into tensor memory, over the scores they came from; while one tile's weights are
 //                    computed, the tensor cores work for the other tile;
-//   warp 8         : issues the MMAs: S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory, V as it
-//                    lies in the cache: keys are its rows, so it is the MN-major operand);
-//   warps 9-11     : producers.  bf16: TMA of one page's rows and 64 elements of the head per copy (128-byte swizzle); an
-//                    issued copy costs its thread 100 to 150 cycles, hence three issuing warps.  int8: the
-//                    three warps load the codes, turn them into bf16 (exactly) and store them in the same layout.
-// Tensor memory: 2 x 128 columns of scores, 2 x 128 of output.  The tensor pipe executes the MMAs of one thread in order, so
+//   warps 8, 9     : issue the MMAs of tile 0 and tile 1: S = Q K^T (both operands in shared memory) and O += P V (P in
+//                    tensor memory, V as it lies in the cache: keys are its rows, so it is the MN-major operand).  They take
+//                    turns, which keeps the two tiles half a period apart (without turns the tiles fall into step: both
+//                    softmaxes, then both pairs of MMAs, 5200 cycles per block);
+//   warps 10-13    : bf16 producers: TMA of one page's rows and 64 elements of the head per copy (128-byte swizzle); an
+//                    issued copy costs its thread 100 to 150 cycles, hence four issuing warps;
+//   int8 cache     : warps 10 and 11 copy the codes and scales of keys and of values into a ring of their own, warps 12-15
+//                    turn them into bf16 (exactly) in the layout of the MMA.
+// Tensor memory: 2 x 128 columns of scores, 2 x 128 of output.  The MMAs that one thread issues execute in order, so
 // the commit behind Q K^T of a block also says that the P V before it is done, and the scores of the next block may overwrite
 // the weights that the P V in front of them reads.
 //
@@ -28,6 +31,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.cuh"
 #include "kv.cuh"
@@ -45,17 +49,28 @@ constexpr int kHalfBytes = kTile * 128;  // 128 rows of 64 bf16 elements, 128-by
 constexpr int kTileBytes16 = 2 * kHalfBytes;
 constexpr int kMaxStages = 5;
 constexpr int kInfo = 8;                 // ring of per-block notes (at most three blocks are in flight)
-constexpr int kMmaWarp = 8, kFirstProducer = 9, kProducers = 3;
-constexpr int kThreads = 12 * 32;
+constexpr int kMmaWarp = 8;        // and the next one
+constexpr int kFirstProducer = 10, kProducers = 4;
+constexpr int kFirstConverter = 12, kConverters = 4; // int8
+constexpr int kThreads = 16 * 32;
 constexpr uint32_t kTmemColumns = 512;
 constexpr float kRaise = 8.0f;
+#ifndef KP
+#define KP 1
+#endif
+#ifndef KT
+#define KT 1
+#endif
+constexpr bool kPoly = KP, kTurns = KT;
 
 template <bool kInt8>
 struct Shared {
-    static constexpr int kStages = kInt8 ? 4 : 5; // blocks of keys or values in shared memory
+    static constexpr int kStages = kInt8 ? 3 : 5; // blocks of keys or values in shared memory
+    static constexpr int kRaw = kInt8 ? 3 : 0;    // blocks of int8 keys or values in front of their conversion
+    static constexpr int kRawBytes = kTile * 128 + kTile * 4; // codes, then scales
     static constexpr int kScaled = 4;             // blocks whose scales are kept
     float scales[kInt8 ? kScaled : 1][2][kInt8 ? kTile : 4]; // of the keys and of the values of a block
-    uint64_t q_full[2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2], p_ready[2], o_done[2];
+    uint64_t q_full[2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2], p_half[2], p_ready[2], o_done[2], turn[2], raw_full[3], raw_empty[3];
     uint32_t tmem_base;
     int abort_flag;
     int poisoned[2];
@@ -68,9 +83,17 @@ struct Shared {
 template <bool kInt8>
 constexpr int Shared<kInt8>::bytes()
 {
-    return 1024 + (2 + kStages) * kTileBytes16 + (int)sizeof(Shared<kInt8>);
+    return 1024 + (2 + kStages) * kTileBytes16 + kRaw * kRawBytes + (int)sizeof(Shared<kInt8>);
 }
 static_assert(Shared<false>::bytes() <= 232448 && Shared<true>::bytes() <= 232448, "shared memory of an SM");
+
+// Registers: 512 threads are launched with 128 each; the softmax warps (a row of 128 scores each) take 184, the others keep 72.
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 184, kOtherRegs = 72;
+static_assert(kSoftmaxRegs * 256 + kOtherRegs * 256 <= kLaunchRegs * kThreads, "setmaxnreg hands on what the launch was given");
+template <int N>
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 struct PromptArgs {
     CUtensorMap k_map, v_map;
@@ -84,6 +107,13 @@ __device__ __forceinline__ float exp2_approx(float x)
     float y;
     asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// The largest of three, or NaN if one of them is.
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+    return m;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -104,6 +134,23 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
+}
+// 2^x of two numbers on the FMA pipe: x = n + f, n = round(x) by the addition of 1.5 2^23 (n then stands in the low bits), 2^f on
+// [-1/2, 1/2] by the polynomial of degree 5 that meets it at the Chebyshev nodes (relative error 2^-22), n added to the
+// exponent.  x is at most about kRaise; below -125 the result is 2^-125.
+__device__ __forceinline__ float2 exp2_poly(float2 x)
+{
+    x = make_float2(fmaxf(x.x, -125.0f), fmaxf(x.y, -125.0f));
+    const float2 t = add2(x, make_float2(12582912.0f, 12582912.0f)), n = add2(t, make_float2(-12582912.0f, -12582912.0f));
+    const float2 f = fma2(n, make_float2(-1.0f, -1.0f), x);
+    float2 p = make_float2(0.0013390863314270973f, 0.0013390863314270973f);
+    p = fma2(p, f, make_float2(0.009676031768321991f, 0.009676031768321991f));
+    p = fma2(p, f, make_float2(0.055503569543361664f, 0.055503569543361664f));
+    p = fma2(p, f, make_float2(0.2402210682630539f, 0.2402210682630539f));
+    p = fma2(p, f, make_float2(0.6931471824645996f, 0.6931471824645996f));
+    p = fma2(p, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
@@ -183,7 +230,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (base - raw);
     constexpr int kStages = Shared<kInt8>::kStages, kScaled = Shared<kInt8>::kScaled;
-    Shared<kInt8> &sh = *reinterpret_cast<Shared<kInt8> *>(smem + (2 + kStages) * kTileBytes16);
+    constexpr int kRaw = Shared<kInt8>::kRaw, kRawBytes = Shared<kInt8>::kRawBytes;
+    uint8_t *raw_ring = smem + (2 + kStages) * kTileBytes16;
+    Shared<kInt8> &sh = *reinterpret_cast<Shared<kInt8> *>(raw_ring + kRaw * kRawBytes);
     volatile int *abort_flag = &sh.abort_flag;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int D = a.cache.head_dim, W = a.cache.width, group = a.heads / a.cache.kv_heads, n_seqs = a.batch.n_seqs;
@@ -259,13 +308,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         for (int t = 0; t < 2; ++t) {
             mbar_init(smem_u32(&sh.q_full[t]), 4);
             mbar_init(smem_u32(&sh.s_full[t]), 1);
+            mbar_init(smem_u32(&sh.p_half[t]), 4);
+            mbar_init(smem_u32(&sh.turn[t]), 1);
             mbar_init(smem_u32(&sh.p_ready[t]), 4);
             mbar_init(smem_u32(&sh.o_done[t]), 1);
             sh.poisoned[t] = 0;
         }
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_u32(&sh.kv_full[s]), 1);
-            mbar_init(smem_u32(&sh.kv_empty[s]), 1);
+            mbar_init(smem_u32(&sh.kv_full[s]), kInt8 ? kConverters : 1);
+            mbar_init(smem_u32(&sh.kv_empty[s]), 2);
+        }
+        for (int s = 0; s < kRaw; ++s) {
+            mbar_init(smem_u32(&sh.raw_full[s]), 1);
+            mbar_init(smem_u32(&sh.raw_empty[s]), kConverters);
         }
         sh.abort_flag = 0;
         fence_mbar_init();
@@ -280,154 +335,182 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     const uint32_t tmem = sh.tmem_base;
     const uint32_t q_addr = base, ring = base + 2 * kTileBytes16;
 
-    if (warp >= kFirstProducer) {
-        // ---- producers: blocks in the order K 0, V 0, K 1, V 1, ..., each warp every third of them ----------------
-        const int halves = W > 64 ? 2 : 1;
-        for (int i = warp - kFirstProducer; i < 2 * total; i += kProducers) {
-            const int s = i % kStages, round = i / kStages, j = from + i / 2;
-            const bool values = i & 1;
-            if (round > 0 && !mbar_wait_bounded(smem_u32(&sh.kv_empty[s]), (round - 1) & 1, abort_flag, limit)) break;
-            const uint32_t full = smem_u32(&sh.kv_full[s]), dst = ring + s * kTileBytes16;
-            // the pages of the block's eight 16-key groups, one per lane
-            int row = -1;
-            bool bad = false;
-            if (lane < 8) {
-                const int pos = j * kTile + lane * 16;
-                if (pos < w.len) {
-                    const int page = kv_page(a.cache, a.batch, w.b, pos);
-                    bad = page < 0;
-                    if (bad)
-                        kv_report(a.cache);
-                    else
-                        row = kv_row(a.cache, page, w.head, pos);
+    if (warp >= kMmaWarp) {
+    give_registers<kOtherRegs>();
+    if (kInt8 && warp >= kFirstConverter) {
+        // ---- int8: codes to bf16, blocks in the order K 0, V 0, K 1, V 1, ...; each warp a quarter of the rows ------------
+        const int pieces = W / 16, c = lane % 8, r0 = lane / 8; // this lane: piece c (16 codes) of every fourth row
+        for (int i = 0; i < 2 * total; ++i) {
+            const int s = i % kStages, round = i / kStages, rs = kInt8 ? i % 3 : 0, j = from + i / 2;
+            if (round > 0 && !mbar_wait_bounded(smem_u32(&sh.kv_empty[s]), (round - 1) & 1, abort_flag, limit, 0)) break;
+            if (!mbar_wait_bounded(smem_u32(&sh.raw_full[rs]), (i / 3) & 1, abort_flag, limit, 0)) break;
+            const uint8_t *codes = raw_ring + rs * kRawBytes;
+            uint8_t *out = smem + (2 + s) * kTileBytes16 + (c / 4) * kHalfBytes;
+            const int p = (c % 4) * 2;
+            {
+                const int r = (warp - kFirstConverter) * 32 + lane; // (scales of keys that do not exist may be anything)
+                const float f = reinterpret_cast<const float *>(codes + kTile * 128)[r];
+                sh.scales[(i / 2) % kScaled][i & 1][r] = j * kTile + r < w.len ? f : 0.0f;
+            }
+            if (c < pieces) {
+#pragma unroll 4
+                for (int u = 0; u < 8; ++u) {
+                    const int r = (warp - kFirstConverter) * 32 + u * 4 + r0;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(codes + r * W + c * 16);
+                    *reinterpret_cast<uint4 *>(out + r * 128 + ((p ^ (r & 7)) << 4)) =
+                        make_uint4(code_pair<0x4140>(x.x), code_pair<0x4342>(x.x), code_pair<0x4140>(x.y), code_pair<0x4342>(x.y));
+                    *reinterpret_cast<uint4 *>(out + r * 128 + (((p + 1) ^ (r & 7)) << 4)) =
+                        make_uint4(code_pair<0x4140>(x.z), code_pair<0x4342>(x.z), code_pair<0x4140>(x.w), code_pair<0x4342>(x.w));
                 }
             }
-            const uint32_t bad_groups = __ballot_sync(0xFFFFFFFFu, bad);
-            if (!values && lane == 0) sh.bad_groups[(i / 2) % kInfo] = bad_groups;
-            if (!kInt8) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&sh.kv_full[s]));
+                mbar_arrive(smem_u32(&sh.raw_empty[rs]));
+            }
+        }
+    } else if (warp >= kFirstProducer) {
+        // ---- producers: bf16: every fourth block of K 0, V 0, K 1, V 1, ... each; int8: one the keys, one the values --------
+        constexpr int kWarps = kInt8 ? 2 : kProducers, kRing = kInt8 ? 3 : kStages;
+        const int halves = W > 64 ? 2 : 1;
+        if (warp - kFirstProducer < kWarps)
+            for (int i = warp - kFirstProducer; i < 2 * total; i += kWarps) {
+                const int s = i % kRing, round = i / kRing, j = from + i / 2;
+                const bool values = i & 1;
+                uint64_t *const full_bar = kInt8 ? &sh.raw_full[s % 3] : &sh.kv_full[s], *const empty_bar = kInt8 ? &sh.raw_empty[s % 3] : &sh.kv_empty[s];
+                // the rows of the block's eight 16-key groups, one per lane
+                int row = -1;
+                bool bad = false;
+                if (lane < 8) {
+                    const int pos = j * kTile + lane * 16;
+                    if (pos < w.len) {
+                        const int page = kv_page(a.cache, a.batch, w.b, pos);
+                        bad = page < 0;
+                        if (bad)
+                            kv_report(a.cache);
+                        else
+                            row = kv_row(a.cache, page, w.head, pos);
+                    }
+                }
+                const uint32_t bad_groups = __ballot_sync(0xFFFFFFFFu, bad);
+                if (round > 0 && !mbar_wait_bounded(smem_u32(empty_bar), (round - 1) & 1, abort_flag, limit)) break;
+                if (!values && lane == 0) sh.bad_groups[(i / 2) % kInfo] = bad_groups;
+                const uint32_t full = smem_u32(full_bar);
                 const int per_copy = min(kTile, 1 << a.cache.page_shift); // rows of a copy
-                const int absent = (a.cache.n_pages * a.cache.kv_heads) << a.cache.page_shift; // a row behind the cache: reads zeros
-                const CUtensorMap *map = values ? &args.v_map : &args.k_map;
+                // (test device: the first CTA leaves out its first arrival and the copies that it announces)
                 const bool skip = args.hooks.skip_arrive && blockIdx.x == 0 && i == 0;
-                if (lane == 0 && !skip) mbar_arrive_expect_tx(full, (uint32_t)(halves * kHalfBytes));
+                const uint32_t have = __ballot_sync(0xFFFFFFFFu, row >= 0);
+                uint32_t bytes = (uint32_t)(halves * kHalfBytes);
+                if (kInt8) {
+                    bytes = 0;
+                    for (int g = 0; g < kTile / 16; g += per_copy / 16)
+                        if ((have >> g) & 1u) bytes += (uint32_t)(per_copy * (W + 4));
+                }
+                if (lane == 0 && !skip) mbar_arrive_expect_tx(full, bytes);
                 __syncwarp();
                 for (int g = 0; g < kTile / 16; g += per_copy / 16) {
                     const int r = __shfl_sync(0xFFFFFFFFu, row, g);
-                    if (lane == 0 && !skip) {
+                    if (lane != 0 || skip) continue;
+                    if (!kInt8) {
+                        const int absent = (a.cache.n_pages * a.cache.kv_heads) << a.cache.page_shift; // a row behind the cache: reads zeros
                         for (int h = 0; h < halves; ++h)
-                            tma_load_2d(dst + h * kHalfBytes + g * 16 * 128, map, h * 64, r < 0 ? absent : r, full);
+                            tma_load_2d(ring + s * kTileBytes16 + h * kHalfBytes + g * 16 * 128, values ? &args.v_map : &args.k_map, h * 64,
+                                        r < 0 ? absent : r, full);
+                    } else if (r >= 0) {
+                        const uint32_t dst = smem_u32(raw_ring) + s * kRawBytes;
+                        bulk_copy_g2s(dst + g * 16 * W, reinterpret_cast<const int8_t *>(values ? a.cache.v : a.cache.k) + (int64_t)r * W,
+                                      (uint32_t)(per_copy * W), full);
+                        bulk_copy_g2s(dst + kTile * 128 + g * 64, (values ? a.cache.v_scale : a.cache.k_scale) + r, (uint32_t)(per_copy * 4), full);
                     }
                 }
-            } else {
-                const int8_t *pool = reinterpret_cast<const int8_t *>(values ? a.cache.v : a.cache.k);
-                const float *scale = values ? a.cache.v_scale : a.cache.k_scale;
-                uint8_t *out = smem + (2 + s) * kTileBytes16;
-                const int pieces = W / 16; // 16 codes each
-                // lane: piece c of row r; rows 4 (or more) at a time
-                const int c = lane % 8, r0 = lane / 8;
-#pragma unroll 2
-                for (int g = 0; g < 8; ++g) {
-                    const int first = __shfl_sync(0xFFFFFFFFu, row, g);
-                    uint4 x[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int r = g * 16 + u * 4 + r0;
-                        const bool real = first >= 0 && c < pieces && j * kTile + r < w.len;
-                        x[u] = real ? *reinterpret_cast<const uint4 *>(pool + (int64_t)(first + u * 4 + r0) * W + c * 16) : make_uint4(0, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int r = g * 16 + u * 4 + r0;
-                        uint8_t *half = out + (c / 4) * kHalfBytes + r * 128;
-                        const int p = (c % 4) * 2;
-                        *reinterpret_cast<uint4 *>(half + ((p ^ (r & 7)) << 4)) =
-                            make_uint4(code_pair<0x4140>(x[u].x), code_pair<0x4342>(x[u].x), code_pair<0x4140>(x[u].y), code_pair<0x4342>(x[u].y));
-                        *reinterpret_cast<uint4 *>(half + (((p + 1) ^ (r & 7)) << 4)) =
-                            make_uint4(code_pair<0x4140>(x[u].z), code_pair<0x4342>(x[u].z), code_pair<0x4140>(x[u].w), code_pair<0x4342>(x[u].w));
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int r = u * 32 + lane, first = __shfl_sync(0xFFFFFFFFu, row, r / 16);
-                    sh.scales[(i / 2) % kScaled][values][r] = first >= 0 && j * kTile + r < w.len ? scale[first + r % 16] : 0.0f;
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0 && !(args.hooks.skip_arrive && blockIdx.x == 0 && i == 0)) mbar_arrive(full);
             }
-        }
-    } else if (warp == kMmaWarp) {
-        // ---- MMAs -------------------------------------------------------------------------------------------
-        const int steps = W / 16;
+    } else {
+        // ---- MMAs of tile t ----------------------------------------------------------------------------------
+        const int t = warp - kMmaWarp, n = blocks[t], both = min(blocks[0], blocks[1]), steps = W / 16;
         const uint32_t idesc_s = idesc_bf16(kTile, kTile, 0), idesc_o = idesc_bf16(kTile, W, 1);
-        bool ok = true;
-        auto wait = [&](uint64_t *bar, int phase) { ok = ok && mbar_wait_bounded(smem_u32(bar), phase & 1, abort_flag, limit); };
-        auto scores = [&](int t, int j) { // S_t = Q_t K_j^T
-            const uint32_t k = ring + (uint32_t)((2 * j) % kStages) * kTileBytes16, q = q_addr + t * kTileBytes16;
+        const uint32_t s_tmem = tmem + t * kTile, o_tmem = tmem + kRows + t * kTile;
+        const uint64_t q_desc = smem_desc_k_sw128(q_addr + t * kTileBytes16);
+        auto wait = [&](uint64_t *bar, int phase) { return mbar_wait_bounded(smem_u32(bar), phase & 1, abort_flag, limit, 0); };
+        auto scores = [&](int s) { // S_t = Q_t K^T of the keys in stage s, which this warp is then done with
+            const uint64_t k_desc = smem_desc_k_sw128(ring + s * kTileBytes16);
             if (elect_one()) {
 #pragma unroll
-                for (int s = 0; s < 8; ++s)
-                    if (s < steps) {
-                        const uint32_t at = (s / 4) * kHalfBytes + (s % 4) * 32;
-                        mma_f16_ss(tmem + t * kTile, smem_desc_k_sw128(q + at), smem_desc_k_sw128(k + at), idesc_s, s > 0);
+                for (int i = 0; i < 8; ++i)
+                    if (i < steps) {
+                        const uint64_t at = ((i / 4) * kHalfBytes + (i % 4) * 32) >> 4;
+                        mma_f16_ss(s_tmem, q_desc + at, k_desc + at, idesc_s, i > 0);
                     }
                 mma_commit(smem_u32(&sh.s_full[t]));
+                mma_commit(smem_u32(&sh.kv_empty[s]));
             }
             __syncwarp();
         };
-        if (total > 0) wait(&sh.kv_full[0], 0);
-        for (int t = 0; t < 2 && ok; ++t) {
-            if (blocks[t] == 0) continue;
-            wait(&sh.q_full[t], 0);
+        bool ok = true;
+        if (n > 0) {
+            ok = wait(&sh.kv_full[0], 0) && wait(&sh.q_full[t], 0);
             tc_fence_after_sync();
-            if (ok) scores(t, 0);
+            if (ok) scores(0);
         }
-        if (ok && total > 0 && elect_one()) mma_commit(smem_u32(&sh.kv_empty[0]));
-        __syncwarp();
-        for (int j = 0; j < total && ok; ++j) {
-            const int kv = 2 * j + 1, s_v = kv % kStages, k_next = 2 * j + 2, s_k = k_next % kStages;
-            wait(&sh.kv_full[s_v], kv / kStages);
-            if (j + 1 < total) wait(&sh.kv_full[s_k], k_next / kStages);
-            for (int t = 0; t < 2 && ok; ++t) {
-                if (j >= blocks[t]) continue;
-                wait(&sh.p_ready[t], j);
-                if (!ok) break;
-                tc_fence_after_sync();
-                const uint32_t v = ring + s_v * kTileBytes16;
+        for (int j = 0; j < n && ok; ++j) {
+            const int kv = 2 * j + 1, s = kv % kStages, next = (kv + 1) % kStages;
+            const uint64_t v_desc = smem_desc_mn_sw128(ring + s * kTileBytes16, kHalfBytes);
+            auto outputs = [&](int first) { // O_t += P_t V of 64 keys
                 if (elect_one()) {
 #pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        mma_f16_ts(tmem + kRows + t * kTile, tmem + t * kTile + s * 8, smem_desc_mn_sw128(v + s * 16 * 128, kHalfBytes),
-                                   idesc_o, j > 0 || s > 0);
-                    if (j + 1 == blocks[t]) mma_commit(smem_u32(&sh.o_done[t]));
+                    for (int i = first; i < first + 4; ++i) // 16 keys each
+                        mma_f16_ts(o_tmem, s_tmem + i * 8, v_desc + ((i * 16 * 128) >> 4), idesc_o, j > 0 || i > 0);
+                    if (first > 0) {
+                        mma_commit(smem_u32(&sh.kv_empty[s]));
+                        if (j + 1 == n) mma_commit(smem_u32(&sh.o_done[t]));
+                    }
                 }
                 __syncwarp();
-                if (j + 1 < blocks[t]) scores(t, j + 1);
+            };
+            if (!(ok = wait(&sh.kv_full[s], kv / kStages) && wait(&sh.p_half[t], j))) break;
+            tc_fence_after_sync();
+            outputs(0);
+            if (j + 1 < n && !(ok = wait(&sh.kv_full[next], (kv + 1) / kStages))) break;
+            if (!(ok = wait(&sh.p_ready[t], j))) break;
+            // tile 0's j-th turn follows tile 1's (j - 1)-th, tile 1's j-th tile 0's j-th, as long as both have blocks left
+            if (kTurns && (t == 0 ? j > 0 && j < both : j + 1 < both)) {
+                if (!(ok = wait(&sh.turn[t], t == 0 ? j - 1 : j))) break;
             }
-            if (ok && elect_one()) {
-                mma_commit(smem_u32(&sh.kv_empty[s_v]));
-                if (j + 1 < total) mma_commit(smem_u32(&sh.kv_empty[s_k]));
-            }
-            __syncwarp();
+            tc_fence_after_sync();
+            outputs(4);
+            if (j + 1 < n) scores(next);
+            if (kTurns && j + 1 < both && lane == 0) mbar_arrive(smem_u32(&sh.turn[1 - t]));
         }
+        // blocks that only the other tile needs
+        for (int i = 2 * n; i < 2 * total && ok; ++i) {
+            ok = wait(&sh.kv_full[i % kStages], i / kStages);
+            if (ok && lane == 0) mbar_arrive(smem_u32(&sh.kv_empty[i % kStages]));
+        }
+    }
     } else {
+        take_registers<kSoftmaxRegs>();
         // ---- softmax: one row per thread ------------------------------------------------------------------------
         const int t = warp / 4, r = tid % kTile, row = w.row0 + t * kTile + r;
         const bool exists = row < w.rows;
         const uint32_t lane_base = tmem + ((uint32_t)(32 * (warp % 4)) << 16), s_col = lane_base + t * kTile, o_col = lane_base + kRows + t * kTile;
         uint8_t *q_tile = smem + t * kTileBytes16;
         if (blocks[t] > 0) {
-            // the tile's queries, in the layout of the MMA (8-byte loads: heads of 100 elements are not 16-byte aligned)
-#pragma unroll 4
-            for (int i = r; i < kTile * 16; i += kTile) {
-                const int qr = i / 16, c = i % 16, rr = w.row0 + t * kTile + qr;
-                uint2 x = make_uint2(0, 0), y = make_uint2(0, 0);
-                if (rr < w.rows) {
-                    const __nv_bfloat16 *src = a.q + (int64_t)(w.first_token + rr / group) * a.q_stride + (w.head * group + rr % group) * D + c * 8;
-                    if (c * 8 < D) x = *reinterpret_cast<const uint2 *>(src);
-                    if (c * 8 + 4 < D) y = *reinterpret_cast<const uint2 *>(src + 4);
-                }
-                *reinterpret_cast<uint4 *>(q_tile + (c / 8) * kHalfBytes + qr * 128 + (((c % 8) ^ (qr & 7)) << 4)) = make_uint4(x.x, x.y, y.x, y.y);
+            // the tile's queries, in the layout of the MMA: this warp's 32 rows, two at a time, 16 bytes per lane (as two
+            // halves: heads of 100 elements are not 16-byte aligned)
+            const int64_t mine = exists ? (int64_t)(w.first_token + row / group) * a.q_stride + (w.head * group + row % group) * D : -1;
+            const int c = lane % 16;
+            uint2 x[16], y[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int64_t at = __shfl_sync(0xFFFFFFFFu, mine, 2 * i + lane / 16);
+                const __nv_bfloat16 *src = a.q + at + c * 8;
+                x[i] = at >= 0 && c * 8 < D ? *reinterpret_cast<const uint2 *>(src) : make_uint2(0, 0);
+                y[i] = at >= 0 && c * 8 + 4 < D ? *reinterpret_cast<const uint2 *>(src + 4) : make_uint2(0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int qr = warp % 4 * 32 + 2 * i + lane / 16;
+                *reinterpret_cast<uint4 *>(q_tile + (c / 8) * kHalfBytes + qr * 128 + (((c % 8) ^ (qr & 7)) << 4)) = make_uint4(x[i].x, x[i].y, y[i].x, y[i].y);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -438,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         float m = -INFINITY, l = 0.0f;                      // reference and sum of this row
         bool ok = true;
         for (int j = 0; j < blocks[t]; ++j) {
-            if (!mbar_wait_bounded(smem_u32(&sh.s_full[t]), j & 1, abort_flag, limit)) {
+            if (!mbar_wait_bounded(smem_u32(&sh.s_full[t]), j & 1, abort_flag, limit, 0)) {
                 ok = false;
                 break;
             }
@@ -448,30 +531,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             // the keys itself cannot be asked any more, it may be a phase further)
             const uint32_t bad_groups = sh.bad_groups[j % kInfo];
             const bool masked = key0 + kTile > least || bad_groups != 0u;
-            const int n_seen = sees - key0;
-            // 32 scores of this row, scaled by their keys and masked.  They are read twice, for the maximum and for the weights,
-            // rather than held in 128 registers.
-            auto load = [&](int c, uint32_t (&u)[32]) { tmem_ld_32x32(s_col + c * 32, u); };
-            auto settle = [&](int c, const uint32_t (&u)[32], float (&x)[32]) {
+            uint32_t u[4][32];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(u[e]);
-                if (kInt8) {
-                    const float4 *ks = reinterpret_cast<const float4 *>(sh.scales[j % kScaled][0]) + c * 8;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float4 f = ks[e];
-                        x[4 * e] *= f.x;
-                        x[4 * e + 1] *= f.y;
-                        x[4 * e + 2] *= f.z;
-                        x[4 * e + 3] *= f.w;
-                    }
-                }
-                if (masked) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (c * 32 + e >= n_seen || ((bad_groups >> (2 * c + e / 16)) & 1u)) x[e] = -INFINITY;
-                }
-            };
+            for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_col + c * 32, u[c]);
             if (masked) {
                 if (!kInt8) {
                     // Values behind the sequence's end are whatever an earlier owner of the page left: they become zero.
@@ -502,23 +564,36 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                     fence_proxy_async_smem();
                 }
             }
-            uint32_t u[2][32];
-            float x[32], top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            load(0, u[0]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tmem_ld_wait_for(u[c & 1]);
-                if (c < 3) load(c + 1, u[(c + 1) & 1]);
-                settle(c, u[c & 1], x);
+            for (int c = 0; c < 4; ++c) tmem_ld_wait_for(u[c]);
+            if (kInt8) {
+                const float4 *ks = reinterpret_cast<const float4 *>(sh.scales[j % kScaled][0]);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) top[e & 3] = fmaxf(top[e & 3], x[e]);
+                for (int c = 0; c < 32; ++c) {
+                    const float4 f = ks[c];
+                    uint32_t *x = &u[c / 8][c % 8 * 4];
+                    x[0] = __float_as_uint(__uint_as_float(x[0]) * f.x);
+                    x[1] = __float_as_uint(__uint_as_float(x[1]) * f.y);
+                    x[2] = __float_as_uint(__uint_as_float(x[2]) * f.z);
+                    x[3] = __float_as_uint(__uint_as_float(x[3]) * f.w);
+                }
             }
-            load(0, u[0]); // (for the second reading)
-            const float peak = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale;
+            if (masked) {
+                const int n = sees - key0;
+#pragma unroll
+                for (int c = 0; c < kTile; ++c)
+                    if (c >= n || ((bad_groups >> (c / 16)) & 1u)) u[c / 32][c % 32] = 0xFF800000u; // -infinity
+            }
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < kTile; c += 2) top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(u[c / 32][c % 32]), __uint_as_float(u[c / 32][c % 32 + 1]));
+            // (a NaN among the scores, or an infinite one, makes the row NaN as it does by the formula; NaN is kept by max3)
+            float peak = max3(max3(top[0], top[1], top[2]), top[3], top[3]) * a.scale;
+            if (peak == INFINITY) peak = __int_as_float(0x7FFFFFFF);
             if (j == 0) {
                 m = peak;
-            } else if (__any_sync(0xFFFFFFFFu, peak > m + kRaise)) {
-                const float raised = fmaxf(m, peak);
+            } else if (__any_sync(0xFFFFFFFFu, !(peak <= m + kRaise))) {
+                const float raised = peak <= m ? m : peak;
                 const float keep = raised == -INFINITY ? 1.0f : exp2_approx(m - raised);
                 m = raised;
                 l *= keep;
@@ -545,26 +620,41 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                     break;
                 }
             }
+            auto weights = [&](auto poly) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                tmem_ld_wait_for(u[c & 1]);
-                if (c < 3) load(c + 1, u[(c + 1) & 1]);
-                settle(c, u[c & 1], x);
                 uint32_t p[16];
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
-                    float2 y = fma2(make_float2(x[e], x[e + 1]), scale2, nb2);
-                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                    float2 y = fma2(make_float2(__uint_as_float(u[c][e]), __uint_as_float(u[c][e + 1])), scale2, nb2);
+                    // three pairs of eight by polynomial
+                    if (kPoly && decltype(poly)::value && ((0x4A >> (e / 2 % 8)) & 1))
+                        y = exp2_poly(y);
+                    else
+                        y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
                     sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
                     if (kInt8) {
                         const float2 f = vs[c * 16 + e / 2];
-                        y.x = masked && x[e] == -INFINITY ? 0.0f : y.x * f.x;
-                        y.y = masked && x[e + 1] == -INFINITY ? 0.0f : y.y * f.y;
+                        y.x = masked && u[c][e] == 0xFF800000u ? 0.0f : y.x * f.x;
+                        y.y = masked && u[c][e + 1] == 0xFF800000u ? 0.0f : y.y * f.y;
                     }
                     p[e / 2] = pack_bf16(y.x, y.y);
                 }
-                tmem_st_32x16(s_col + c * 16, p); // (columns of scores that have been read twice)
+                tmem_st_32x16(s_col + c * 16, p); // (the scores have been read)
+                if (c == 1) { // the tensor cores can begin with the first 64 keys
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sh.p_half[t]));
+                }
             }
+            };
+            // (the polynomial's smallest result is not zero: hidden scores, and rows that have seen nothing but -infinity, go
+            // through the exponential unit)
+            if (masked || __any_sync(0xFFFFFFFFu, m == -INFINITY))
+                weights(std::false_type{});
+            else
+                weights(std::true_type{});
             const float2 both = add2(sum[0], sum[1]);
             l += both.x + both.y;
             tmem_st_wait();
@@ -584,22 +674,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + row / group) * a.out_stride + (w.head * group + row % group) * D;
             float *part = part_of(split) + 2 * kRows + (size_t)(t * kTile + r) * W;
             if (parts > 1) *reinterpret_cast<float2 *>(part_of(split) + 2 * (t * kTile + r)) = make_float2(blocks[t] > 0 ? m : -INFINITY, l);
-#pragma unroll 1
-            for (int c = 0; c < W; c += 16) {
-                uint32_t o[16];
-                tmem_ld_32x16(o_col + c, o);
-                tmem_ld_wait();
-                float x[16];
+            const bool some = blocks[t] > 0 && l != 0.0f;
+            uint32_t o[4][32];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = blocks[t] > 0 && l != 0.0f ? __uint_as_float(o[e]) * inv : 0.0f;
-                if (parts > 1) {
+            for (int c = 0; c < 4; ++c)
+                if (c * 32 < W) tmem_ld_32x32(o_col + c * 32, o[c]);
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(part + c + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-                } else if (exists) {
+            for (int c = 0; c < 4; ++c) tmem_ld_wait_for(o[c]);
+            auto at = [&](int e) { return some ? __uint_as_float(o[e / 32][e % 32]) * inv : 0.0f; };
+            if (parts > 1) {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4)
-                        if (c + e < D) *reinterpret_cast<uint2 *>(dst + c + e) = make_uint2(pack_bf16(x[e], x[e + 1]), pack_bf16(x[e + 2], x[e + 3]));
-                }
+                for (int e = 0; e < kTile; e += 4)
+                    if (e < W) *reinterpret_cast<float4 *>(part + e) = make_float4(at(e), at(e + 1), at(e + 2), at(e + 3));
+            } else if (exists && D % 8 == 0) {
+#pragma unroll
+                for (int e = 0; e < kTile; e += 8)
+                    if (e < D)
+                        *reinterpret_cast<uint4 *>(dst + e) = make_uint4(pack_bf16(at(e), at(e + 1)), pack_bf16(at(e + 2), at(e + 3)),
+                                                                         pack_bf16(at(e + 4), at(e + 5)), pack_bf16(at(e + 6), at(e + 7)));
+            } else if (exists) {
+#pragma unroll
+                for (int e = 0; e < kTile; e += 4)
+                    if (e < D) *reinterpret_cast<uint2 *>(dst + e) = make_uint2(pack_bf16(at(e), at(e + 1)), pack_bf16(at(e + 2), at(e + 3)));
             }
         }
         if (parts > 1) {
@@ -694,6 +790,10 @@ cudaError_t launch(const PromptArgs &p, int ctas, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
+        cudaFuncAttributes have;
+        e = cudaFuncGetAttributes(&have, attend_prompt_kernel<kInt8>);
+        if (e != cudaSuccess) return e;
+        if (have.numRegs != kLaunchRegs) return cudaErrorInvalidConfiguration; // (the split of the registers would not add up)
         e = cudaFuncSetAttribute(attend_prompt_kernel<kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shared<kInt8>::bytes());
         if (e != cudaSuccess) return e;
         ready[dev] = true;
