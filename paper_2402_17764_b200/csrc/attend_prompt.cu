@@ -8,19 +8,19 @@
 //
 // Roles (16 warps):
 //   warps 0-3, 4-7 : the softmax of tile 0 and of tile 1, one row per thread: scores from tensor memory, maximum, 2^x, the
-//                    weights as bf16 back into tensor memory, over the scores they came from; while one tile's weights are
-//                    computed, the tensor cores work for the other tile;
+//                    weights as bf16 back into tensor memory, over the scores they came from;
 //   warps 8, 9     : issue the MMAs of tile 0 and tile 1: S = Q K^T (both operands in shared memory) and O += P V (P in
-//                    tensor memory, V as it lies in the cache: keys are its rows, so it is the MN-major operand).  They take
-//                    turns, which keeps the two tiles half a period apart (without turns the tiles fall into step: both
-//                    softmaxes, then both pairs of MMAs, 5200 cycles per block);
+//                    tensor memory, V as it lies in the cache: keys are its rows, so it is the MN-major operand);
 //   warps 10-13    : bf16 producers: TMA of one page's rows and 64 elements of the head per copy (128-byte swizzle); an
 //                    issued copy costs its thread 100 to 150 cycles, hence four issuing warps;
 //   int8 cache     : warps 10 and 11 copy the codes and scales of keys and of values into a ring of their own, warps 12-15
 //                    turn them into bf16 (exactly) in the layout of the MMA.
-// Tensor memory: 2 x 128 columns of scores, 2 x 128 of output.  The MMAs that one thread issues execute in order, so
-// the commit behind Q K^T of a block also says that the P V before it is done, and the scores of the next block may overwrite
-// the weights that the P V in front of them reads.
+// Tensor memory: 2 x 128 columns of scores, 2 x 128 of output.  The softmax works in steps of 64 keys, and a tile's two halves
+// of the score columns take the steps in turn: while step k is worked on, P V of step k - 1 and the scores of step k + 1 run in
+// the other half, so the softmax does not wait for the tensor cores between steps.  The MMAs that one thread issues execute in
+// order, so the scores of step k + 2 may overwrite the weights that the P V of step k in front of them reads.  (With steps
+// of 128 keys the scores of the next step could only start after P V of this one: softmax and MMAs of a tile took turns,
+// 3900 cycles per block of 128 keys.)
 //
 // Rescaling.  The output stands in tensor memory, and moving it for every new maximum would cost as much as the softmax.  The
 // reference m_i is therefore raised only when a score exceeds it by more than 8 (a factor 256, which fp32 sums and bf16 weights
@@ -44,6 +44,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kTile = 128;               // rows of a query tile, keys of a block
+constexpr int kStep = 64;                // keys of a softmax step
 constexpr int kRows = 2 * kTile;         // rows of a CTA
 constexpr int kHalfBytes = kTile * 128;  // 128 rows of 64 bf16 elements, 128-byte swizzle
 constexpr int kTileBytes16 = 2 * kHalfBytes;
@@ -55,14 +56,6 @@ constexpr int kFirstConverter = 12, kConverters = 4; // int8
 constexpr int kThreads = 16 * 32;
 constexpr uint32_t kTmemColumns = 512;
 constexpr float kRaise = 8.0f;
-#ifndef KP
-#define KP 1
-#endif
-#ifndef KT
-#define KT 1
-#endif
-constexpr bool kPoly = KP, kTurns = KT;
-
 template <bool kInt8>
 struct Shared {
     static constexpr int kStages = kInt8 ? 3 : 5; // blocks of keys or values in shared memory
@@ -70,7 +63,7 @@ struct Shared {
     static constexpr int kRawBytes = kTile * 128 + kTile * 4; // codes, then scales
     static constexpr int kScaled = 4;             // blocks whose scales are kept
     float scales[kInt8 ? kScaled : 1][2][kInt8 ? kTile : 4]; // of the keys and of the values of a block
-    uint64_t q_full[2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2], p_half[2], p_ready[2], o_done[2], turn[2], raw_full[3], raw_empty[3];
+    uint64_t q_full[2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2][2], p_ready[2][2], o_done[2], o_last[2], raw_full[3], raw_empty[3];
     uint32_t tmem_base;
     int abort_flag;
     int poisoned[2];
@@ -128,29 +121,19 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 __device__ __forceinline__ float2 add2(float2 a, float2 b)
 {
     float2 d;
     asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
-}
-// 2^x of two numbers on the FMA pipe: x = n + f, n = round(x) by the addition of 1.5 2^23 (n then stands in the low bits), 2^f on
-// [-1/2, 1/2] by the polynomial of degree 5 that meets it at the Chebyshev nodes (relative error 2^-22), n added to the
-// exponent.  x is at most about kRaise; below -125 the result is 2^-125.
-__device__ __forceinline__ float2 exp2_poly(float2 x)
-{
-    x = make_float2(fmaxf(x.x, -125.0f), fmaxf(x.y, -125.0f));
-    const float2 t = add2(x, make_float2(12582912.0f, 12582912.0f)), n = add2(t, make_float2(-12582912.0f, -12582912.0f));
-    const float2 f = fma2(n, make_float2(-1.0f, -1.0f), x);
-    float2 p = make_float2(0.0013390863314270973f, 0.0013390863314270973f);
-    p = fma2(p, f, make_float2(0.009676031768321991f, 0.009676031768321991f));
-    p = fma2(p, f, make_float2(0.055503569543361664f, 0.055503569543361664f));
-    p = fma2(p, f, make_float2(0.2402210682630539f, 0.2402210682630539f));
-    p = fma2(p, f, make_float2(0.6931471824645996f, 0.6931471824645996f));
-    p = fma2(p, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
@@ -238,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     const int D = a.cache.head_dim, W = a.cache.width, group = a.heads / a.cache.kv_heads, n_seqs = a.batch.n_seqs;
     const uint32_t limit = args.hooks.limit_us;
 
-    // ---- which rows: tiles are counted sequence by sequence, kv head by kv head, the last rows (which see most) first ----
+    // ---- which rows: tiles are counted sequence by sequence, the last rows (which see most) of all kv heads first ----
     const int split = blockIdx.x % args.splits;
     {
         const int64_t x = blockIdx.x / args.splits;
@@ -283,8 +266,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     w.rows = n_tokens * group;
     {
         const int tiles = (w.rows + kRows - 1) / kRows;
-        w.head = (int)(sh.found_local / tiles);
-        w.row0 = (tiles - 1 - (int)(sh.found_local % tiles)) * kRows;
+        w.head = (int)(sh.found_local % a.cache.kv_heads);
+        w.row0 = (tiles - 1 - (int)(sh.found_local / a.cache.kv_heads)) * kRows;
     }
     bool over;
     w.len = kv_length(a.batch, w.b, over);
@@ -297,21 +280,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     const int parts = max(1, min(args.splits, most / 4));
     if (split >= parts) return;
     const int from = (int)((int64_t)most * split / parts), to = (int)((int64_t)most * (split + 1) / parts);
-    int blocks[2];
+    int n_steps[2];
     for (int t = 0; t < 2; ++t) {
         const int first = w.row0 + t * kTile, last = min(first + kTile, w.rows) - 1;
-        blocks[t] = first < w.rows ? max(0, min((w.sees(last) + kTile - 1) / kTile, to) - from) : 0;
+        n_steps[t] = first < w.rows ? max(0, min((w.sees(last) + kStep - 1) / kStep, 2 * to) - 2 * from) : 0;
     }
-    const int total = max(blocks[0], blocks[1]);
+    const int total = (max(n_steps[0], n_steps[1]) + 1) / 2; // blocks
 
     if (tid == 0) {
         for (int t = 0; t < 2; ++t) {
             mbar_init(smem_u32(&sh.q_full[t]), 4);
-            mbar_init(smem_u32(&sh.s_full[t]), 1);
-            mbar_init(smem_u32(&sh.p_half[t]), 4);
-            mbar_init(smem_u32(&sh.turn[t]), 1);
-            mbar_init(smem_u32(&sh.p_ready[t]), 4);
+            for (int h = 0; h < 2; ++h) {
+                mbar_init(smem_u32(&sh.s_full[t][h]), 1);
+                mbar_init(smem_u32(&sh.p_ready[t][h]), 4);
+            }
             mbar_init(smem_u32(&sh.o_done[t]), 1);
+            mbar_init(smem_u32(&sh.o_last[t]), 1);
             sh.poisoned[t] = 0;
         }
         for (int s = 0; s < kStages; ++s) {
@@ -427,63 +411,58 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             }
     } else {
         // ---- MMAs of tile t ----------------------------------------------------------------------------------
-        const int t = warp - kMmaWarp, n = blocks[t], both = min(blocks[0], blocks[1]), steps = W / 16;
-        const uint32_t idesc_s = idesc_bf16(kTile, kTile, 0), idesc_o = idesc_bf16(kTile, W, 1);
+        const int t = warp - kMmaWarp, n = n_steps[t], k_steps = W / 16;
+        const uint32_t idesc_s = idesc_bf16(kTile, kStep, 0), idesc_o = idesc_bf16(kTile, W, 1);
         const uint32_t s_tmem = tmem + t * kTile, o_tmem = tmem + kRows + t * kTile;
         const uint64_t q_desc = smem_desc_k_sw128(q_addr + t * kTileBytes16);
-        auto wait = [&](uint64_t *bar, int phase) { return mbar_wait_bounded(smem_u32(bar), phase & 1, abort_flag, limit, 0); };
-        auto scores = [&](int s) { // S_t = Q_t K^T of the keys in stage s, which this warp is then done with
-            const uint64_t k_desc = smem_desc_k_sw128(ring + s * kTileBytes16);
+        auto wait = [&](uint64_t *bar, int phase) { return mbar_spin_bounded(smem_u32(bar), phase & 1, abort_flag, limit); };
+        auto full = [&](int i) { return wait(&sh.kv_full[i % kStages], i / kStages); }; // K of block j: i = 2 j, V: i = 2 j + 1
+        // S = Q K^T of step k, into half k % 2 of the tile's score columns
+        auto scores = [&](int k) {
+            const int stage = (k & ~1) % kStages;
+            const uint64_t k_desc = smem_desc_k_sw128(ring + stage * kTileBytes16 + (k & 1) * kStep * 128);
             if (elect_one()) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i < steps) {
+                    if (i < k_steps) {
                         const uint64_t at = ((i / 4) * kHalfBytes + (i % 4) * 32) >> 4;
-                        mma_f16_ss(s_tmem, q_desc + at, k_desc + at, idesc_s, i > 0);
+                        mma_f16_ss(s_tmem + (k & 1) * kStep, q_desc + at, k_desc + at, idesc_s, i > 0);
                     }
-                mma_commit(smem_u32(&sh.s_full[t]));
-                mma_commit(smem_u32(&sh.kv_empty[s]));
+                mma_commit(smem_u32(&sh.s_full[t][k & 1]));
+                if ((k & 1) || k + 1 == n) mma_commit(smem_u32(&sh.kv_empty[stage]));
             }
             __syncwarp();
         };
         bool ok = true;
         if (n > 0) {
-            ok = wait(&sh.kv_full[0], 0) && wait(&sh.q_full[t], 0);
+            ok = full(0) && wait(&sh.q_full[t], 0);
             tc_fence_after_sync();
             if (ok) scores(0);
+            if (ok && n > 1) scores(1);
         }
-        for (int j = 0; j < n && ok; ++j) {
-            const int kv = 2 * j + 1, s = kv % kStages, next = (kv + 1) % kStages;
-            const uint64_t v_desc = smem_desc_mn_sw128(ring + s * kTileBytes16, kHalfBytes);
-            auto outputs = [&](int first) { // O_t += P_t V of 64 keys
-                if (elect_one()) {
+        for (int k = 0; k < n && ok; ++k) {
+            const int v = k | 1, stage = v % kStages; // block k / 2: values are tile 2 (k / 2) + 1
+            if (!(ok = full(v) && wait(&sh.p_ready[t][k & 1], k >> 1))) break;
+            tc_fence_after_sync();
+            const uint64_t v_desc = smem_desc_mn_sw128(ring + stage * kTileBytes16 + (k & 1) * kStep * 128, kHalfBytes);
+            if (elect_one()) {
 #pragma unroll
-                    for (int i = first; i < first + 4; ++i) // 16 keys each
-                        mma_f16_ts(o_tmem, s_tmem + i * 8, v_desc + ((i * 16 * 128) >> 4), idesc_o, j > 0 || i > 0);
-                    if (first > 0) {
-                        mma_commit(smem_u32(&sh.kv_empty[s]));
-                        if (j + 1 == n) mma_commit(smem_u32(&sh.o_done[t]));
-                    }
-                }
-                __syncwarp();
-            };
-            if (!(ok = wait(&sh.kv_full[s], kv / kStages) && wait(&sh.p_half[t], j))) break;
-            tc_fence_after_sync();
-            outputs(0);
-            if (j + 1 < n && !(ok = wait(&sh.kv_full[next], (kv + 1) / kStages))) break;
-            if (!(ok = wait(&sh.p_ready[t], j))) break;
-            // tile 0's j-th turn follows tile 1's (j - 1)-th, tile 1's j-th tile 0's j-th, as long as both have blocks left
-            if (kTurns && (t == 0 ? j > 0 && j < both : j + 1 < both)) {
-                if (!(ok = wait(&sh.turn[t], t == 0 ? j - 1 : j))) break;
+                for (int i = 0; i < 4; ++i) // O += P V, 16 keys each
+                    mma_f16_ts(o_tmem, s_tmem + (k & 1) * kStep + i * 8, v_desc + ((i * 16 * 128) >> 4), idesc_o, k > 0 || i > 0);
+                mma_commit(smem_u32(&sh.o_done[t]));
+                if (k + 1 == n) mma_commit(smem_u32(&sh.o_last[t]));
+                if ((k & 1) || k + 1 == n) mma_commit(smem_u32(&sh.kv_empty[stage]));
             }
-            tc_fence_after_sync();
-            outputs(4);
-            if (j + 1 < n) scores(next);
-            if (kTurns && j + 1 < both && lane == 0) mbar_arrive(smem_u32(&sh.turn[1 - t]));
+            __syncwarp();
+            if (k + 2 < n) {
+                if (!(ok = full((k + 2) & ~1))) break;
+                tc_fence_after_sync();
+                scores(k + 2);
+            }
         }
         // blocks that only the other tile needs
-        for (int i = 2 * n; i < 2 * total && ok; ++i) {
-            ok = wait(&sh.kv_full[i % kStages], i / kStages);
+        for (int i = (n + 1) / 2 * 2; i < 2 * total && ok; ++i) {
+            ok = full(i);
             if (ok && lane == 0) mbar_arrive(smem_u32(&sh.kv_empty[i % kStages]));
         }
     }
@@ -494,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         const bool exists = row < w.rows;
         const uint32_t lane_base = tmem + ((uint32_t)(32 * (warp % 4)) << 16), s_col = lane_base + t * kTile, o_col = lane_base + kRows + t * kTile;
         uint8_t *q_tile = smem + t * kTileBytes16;
-        if (blocks[t] > 0) {
+        if (n_steps[t] > 0) {
             // the tile's queries, in the layout of the MMA: this warp's 32 rows, two at a time, 16 bytes per lane (as two
             // halves: heads of 100 elements are not 16-byte aligned)
             const int64_t mine = exists ? (int64_t)(w.first_token + row / group) * a.q_stride + (w.head * group + row % group) * D : -1;
@@ -520,84 +499,94 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         const int least = w.sees(w.row0 + t * kTile);       // of the tile's rows
         float m = -INFINITY, l = 0.0f;                      // reference and sum of this row
         bool ok = true;
-        for (int j = 0; j < blocks[t]; ++j) {
-            if (!mbar_wait_bounded(smem_u32(&sh.s_full[t]), j & 1, abort_flag, limit, 0)) {
+        for (int k = 0; k < n_steps[t]; ++k) {
+            if (!mbar_spin_bounded(smem_u32(&sh.s_full[t][k & 1]), (k >> 1) & 1, abort_flag, limit)) {
                 ok = false;
                 break;
             }
             tc_fence_after_sync();
-            const int key0 = (from + j) * kTile;
+            const int j = k >> 1, key0 = (from + j) * kTile + (k & 1) * kStep;
+            const uint32_t s_half = s_col + (k & 1) * kStep;
+            uint32_t u[2][32];
+            tmem_ld_32x32(s_half, u[0]);
+            tmem_ld_32x32(s_half + 32, u[1]);
             // (the producer's notes on a block of keys were written before its arrival, which Q K^T waited for; `kv_full` of
             // the keys itself cannot be asked any more, it may be a phase further)
-            const uint32_t bad_groups = sh.bad_groups[j % kInfo];
-            const bool masked = key0 + kTile > least || bad_groups != 0u;
-            uint32_t u[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_col + c * 32, u[c]);
-            if (masked) {
-                if (!kInt8) {
-                    // Values behind the sequence's end are whatever an earlier owner of the page left: they become zero.
-                    // Values inside that are not finite would reach rows that do not see them (0 x NaN): such a tile
-                    // is done again, row by row.
-                    const int kv = 2 * j + 1, st = kv % kStages;
-                    if (!mbar_wait_bounded(smem_u32(&sh.kv_full[st]), (kv / kStages) & 1, abort_flag, limit)) {
-                        ok = false;
-                        break;
-                    }
-                    uint8_t *v = smem + (2 + st) * kTileBytes16 + r * 128;
-                    const bool behind = key0 + r >= w.len;
+            const uint32_t bad_groups = sh.bad_groups[j % kInfo] >> (4 * (k & 1)) & 0xFu;
+            const bool masked = key0 + kStep > least || bad_groups != 0u;
+            const int kv = 2 * j + 1, v_stage = kv % kStages;
+            if ((masked || kInt8) && !mbar_spin_bounded(smem_u32(&sh.kv_full[v_stage]), (kv / kStages) & 1, abort_flag, limit)) {
+                ok = false; // (the values, or their scales, are looked at below)
+                break;
+            }
+            if (masked && !kInt8) {
+                // Values behind the sequence's end are whatever an earlier owner of the page left: they become zero.
+                // Values inside that are not finite would reach rows that do not see them (0 x NaN): such a tile is done
+                // again, row by row.  Two threads per key, 64 elements each.
+                const int key = (k & 1) * kStep + r % kStep;
+                uint8_t *v = smem + (2 + v_stage) * kTileBytes16 + (r / kStep) * kHalfBytes + key * 128;
+                if (r < kStep || W > 64) {
+                    const bool behind = (from + j) * kTile + key >= w.len;
                     bool odd = false;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (i >= 8 && W <= 64) break;
-                        uint4 *p = reinterpret_cast<uint4 *>(v + (i / 8) * kHalfBytes + (((i + r) & 7) << 4));
+                    for (int i = 0; i < 8; ++i) {
+                        uint4 *p = reinterpret_cast<uint4 *>(v + (((i + r) & 7) << 4));
                         if (behind) {
                             *p = make_uint4(0, 0, 0, 0);
                         } else {
                             const uint4 x = *p;
-                            const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+                            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) odd = odd || (u[e] & 0x7F800000u) == 0x7F800000u || (u[e] & 0x7F80u) == 0x7F80u;
+                            for (int e = 0; e < 4; ++e) odd = odd || (y[e] & 0x7F800000u) == 0x7F800000u || (y[e] & 0x7F80u) == 0x7F80u;
                         }
                     }
                     if (odd) sh.poisoned[t] = 1;
                     fence_proxy_async_smem();
                 }
             }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_wait_for(u[c]);
+            tmem_ld_wait_for(u[0]);
+            tmem_ld_wait_for(u[1]);
             if (kInt8) {
-                const float4 *ks = reinterpret_cast<const float4 *>(sh.scales[j % kScaled][0]);
+                const float4 *ks = reinterpret_cast<const float4 *>(sh.scales[j % kScaled][0] + (k & 1) * kStep);
 #pragma unroll
-                for (int c = 0; c < 32; ++c) {
+                for (int c = 0; c < kStep / 4; ++c) {
                     const float4 f = ks[c];
                     uint32_t *x = &u[c / 8][c % 8 * 4];
-                    x[0] = __float_as_uint(__uint_as_float(x[0]) * f.x);
-                    x[1] = __float_as_uint(__uint_as_float(x[1]) * f.y);
-                    x[2] = __float_as_uint(__uint_as_float(x[2]) * f.z);
-                    x[3] = __float_as_uint(__uint_as_float(x[3]) * f.w);
+                    const float2 y = mul2(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), make_float2(f.x, f.y));
+                    const float2 z = mul2(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), make_float2(f.z, f.w));
+                    x[0] = __float_as_uint(y.x);
+                    x[1] = __float_as_uint(y.y);
+                    x[2] = __float_as_uint(z.x);
+                    x[3] = __float_as_uint(z.y);
                 }
             }
             if (masked) {
                 const int n = sees - key0;
 #pragma unroll
-                for (int c = 0; c < kTile; ++c)
+                for (int c = 0; c < kStep; ++c)
                     if (c >= n || ((bad_groups >> (c / 16)) & 1u)) u[c / 32][c % 32] = 0xFF800000u; // -infinity
             }
             float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < kTile; c += 2) top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(u[c / 32][c % 32]), __uint_as_float(u[c / 32][c % 32 + 1]));
+            for (int c = 0; c < kStep; c += 2) top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(u[c / 32][c % 32]), __uint_as_float(u[c / 32][c % 32 + 1]));
             // (a NaN among the scores, or an infinite one, makes the row NaN as it does by the formula; NaN is kept by max3)
             float peak = max3(max3(top[0], top[1], top[2]), top[3], top[3]) * a.scale;
             if (peak == INFINITY) peak = __int_as_float(0x7FFFFFFF);
-            if (j == 0) {
+            if (k == 0) {
                 m = peak;
             } else if (__any_sync(0xFFFFFFFFu, !(peak <= m + kRaise))) {
                 const float raised = peak <= m ? m : peak;
                 const float keep = raised == -INFINITY ? 1.0f : exp2_approx(m - raised);
                 m = raised;
                 l *= keep;
-                // (the commit behind this block's scores covers the P V before it: the output is at rest)
+                // the P V in front of this step has to be at rest (the next one waits for this step's weights; the one before
+                // it is done, as the scores of this step were issued behind it, so the phase asked for is the current one or
+                // the one just completed)
+                if (!mbar_spin_bounded(smem_u32(&sh.o_done[t]), (k - 1) & 1, abort_flag, limit)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after_sync();
 #pragma unroll 1
                 for (int c = 0; c < W; c += 16) {
                     uint32_t o[16];
@@ -607,62 +596,49 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                     for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
                     tmem_st_32x16(o_col + c, o);
                 }
-                tmem_st_wait();
             }
             const float nb = m == -INFINITY ? 0.0f : -m;
             const float2 scale2 = make_float2(a.scale, a.scale), nb2 = make_float2(nb, nb);
             float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-            const float2 *vs = reinterpret_cast<const float2 *>(sh.scales[j % kScaled][1]);
-            if (kInt8) {
-                const int kv = 2 * j + 1;
-                if (!mbar_wait_bounded(smem_u32(&sh.kv_full[kv % kStages]), (kv / kStages) & 1, abort_flag, limit)) {
-                    ok = false;
-                    break;
-                }
-            }
-            auto weights = [&](auto poly) {
+            const float4 *vs = reinterpret_cast<const float4 *>(sh.scales[j % kScaled][1] + (k & 1) * kStep);
+            auto weights = [&](auto hidden) { // hidden: some of the scores are
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t p[16];
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t p[16];
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    float2 y = fma2(make_float2(__uint_as_float(u[c][e]), __uint_as_float(u[c][e + 1])), scale2, nb2);
-                    // three pairs of eight by polynomial
-                    if (kPoly && decltype(poly)::value && ((0x4A >> (e / 2 % 8)) & 1))
-                        y = exp2_poly(y);
-                    else
-                        y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
-                    sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], y);
-                    if (kInt8) {
-                        const float2 f = vs[c * 16 + e / 2];
-                        y.x = masked && u[c][e] == 0xFF800000u ? 0.0f : y.x * f.x;
-                        y.y = masked && u[c][e + 1] == 0xFF800000u ? 0.0f : y.y * f.y;
+                    for (int e = 0; e < 32; e += 4) {
+                        float4 f = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                        if (kInt8) f = vs[c * 8 + e / 4];
+                        const float2 fs[2] = {make_float2(f.x, f.y), make_float2(f.z, f.w)};
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t u0 = u[c][e + 2 * h], u1 = u[c][e + 2 * h + 1];
+                            float2 y = fma2(make_float2(__uint_as_float(u0), __uint_as_float(u1)), scale2, nb2);
+                            y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                            sum[h] = add2(sum[h], y);
+                            if (kInt8) {
+                                y = mul2(y, fs[h]);
+                                // (0 times the scale of a row that is not finite)
+                                if (decltype(hidden)::value) y = make_float2(u0 == 0xFF800000u ? 0.0f : y.x, u1 == 0xFF800000u ? 0.0f : y.y);
+                            }
+                            p[e / 2 + h] = pack_bf16(y.x, y.y);
+                        }
                     }
-                    p[e / 2] = pack_bf16(y.x, y.y);
+                    tmem_st_32x16(s_half + c * 16, p); // (the scores have been read)
                 }
-                tmem_st_32x16(s_col + c * 16, p); // (the scores have been read)
-                if (c == 1) { // the tensor cores can begin with the first 64 keys
-                    tmem_st_wait();
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&sh.p_half[t]));
-                }
-            }
             };
-            // (the polynomial's smallest result is not zero: hidden scores, and rows that have seen nothing but -infinity, go
-            // through the exponential unit)
-            if (masked || __any_sync(0xFFFFFFFFu, m == -INFINITY))
-                weights(std::false_type{});
-            else
+            if (kInt8 && masked)
                 weights(std::true_type{});
+            else
+                weights(std::false_type{});
             const float2 both = add2(sum[0], sum[1]);
             l += both.x + both.y;
             tmem_st_wait();
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[t]));
+            if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[t][k & 1]));
         }
-        if (blocks[t] > 0) ok = ok && mbar_wait_bounded(smem_u32(&sh.o_done[t]), 0, abort_flag, limit);
+        if (n_steps[t] > 0) ok = ok && mbar_spin_bounded(smem_u32(&sh.o_last[t]), 0, abort_flag, limit);
         tc_fence_after_sync();
 
         // ---- the result, or this CTA's part of it --------------------------------------------------------------
@@ -673,8 +649,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             const float inv = parts > 1 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
             __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + row / group) * a.out_stride + (w.head * group + row % group) * D;
             float *part = part_of(split) + 2 * kRows + (size_t)(t * kTile + r) * W;
-            if (parts > 1) *reinterpret_cast<float2 *>(part_of(split) + 2 * (t * kTile + r)) = make_float2(blocks[t] > 0 ? m : -INFINITY, l);
-            const bool some = blocks[t] > 0 && l != 0.0f;
+            if (parts > 1) *reinterpret_cast<float2 *>(part_of(split) + 2 * (t * kTile + r)) = make_float2(n_steps[t] > 0 ? m : -INFINITY, l);
+            const bool some = n_steps[t] > 0 && l != 0.0f;
             uint32_t o[4][32];
 #pragma unroll
             for (int c = 0; c < 4; ++c)

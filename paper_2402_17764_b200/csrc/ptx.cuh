@@ -113,6 +113,32 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
     }
 }
 
+// The same for waits on the critical path: tries follow each other without a pause (tens of cycles between the phase's end and
+// the return, against hundreds).
+__device__ __forceinline__ bool mbar_spin_bounded(uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t limit_us)
+{
+    uint64_t t0 = 0;
+    const uint64_t limit_ns = (uint64_t)limit_us * 1000ull;
+    for (uint32_t spin = 1;; ++spin) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+        if (done) return true;
+        if ((spin & 0xFFu) == 0u) {
+            if (*abort_flag) return false;
+            const uint64_t now = globaltimer_ns();
+            if (t0 == 0) {
+                t0 = now;
+            } else if (now - t0 > limit_ns) {
+                *abort_flag = 1;
+                return false;
+            }
+        }
+    }
+}
+
 // ---- flags in global memory ---------------------------------------------------------------------------
 
 __device__ __forceinline__ void st_release_gpu(uint32_t *p, uint32_t v)
