@@ -553,7 +553,7 @@ class KVCache:
             _refuse(where, "the tensors are contiguous and on one CUDA device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.kv_heads, self.page_size = k.shape[:3]
-        self.head_dim, self.bits, self.device = head_dim, bits, k.device
+        self.head_dim, self.bits, self.device, self.index = head_dim, bits, k.device, k.get_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self._desc = KVCacheDesc(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(self.status), self.n_pages, self.kv_heads,
                                  head_dim, self.page_size, bits)
@@ -584,7 +584,8 @@ class KVBatch:
         if (page_table.shape[1] > 1 and page_table.stride(1) != 1) or (n > 1 and kv_lens.stride(0) != 1) or \
                 (cu_tokens is not None and n > 0 and cu_tokens.stride(0) != 1):
             _refuse(where, "kv_lens, cu_tokens and the rows of page_table are contiguous")
-        self.page_table, self.kv_lens, self.cu_tokens, self.n_seqs, self.device = page_table, kv_lens, cu_tokens, n, kv_lens.device
+        self.page_table, self.kv_lens, self.cu_tokens, self.n_seqs = page_table, kv_lens, cu_tokens, n
+        self.device, self.index = kv_lens.device, kv_lens.get_device()
         pages = page_table.shape[1]
         stride = page_table.stride(0) if n > 1 else pages
         self._desc = KVBatchDesc(_ptr(page_table), _ptr(kv_lens), _ptr(cu_tokens), n, stride, pages)
@@ -603,14 +604,14 @@ def rope_table(n_pos: int, head_dim: int, base: float = 10000.0, device="cuda", 
     return table
 
 
-def _row_stride(t: torch.Tensor, heads: int, head_dim: int, rows: int, device, where: str) -> int:
+def _row_stride(t: torch.Tensor, heads: int, head_dim: int, rows: int, index: int, where: str) -> int:
     """Row stride of bf16 [rows, heads, head_dim] in elements; refuses what the kernels cannot address."""
-    if t.shape != (rows, heads, head_dim) or t.dtype != torch.bfloat16 or t.device != device:
-        _refuse(where, f"expected bf16 [{rows}, {heads}, {head_dim}] on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
-    s = t.stride()
-    if (head_dim > 1 and s[2] != 1) or (heads > 1 and s[1] != head_dim):
+    if t.shape != (rows, heads, head_dim) or t.dtype is not torch.bfloat16 or t.get_device() != index:
+        _refuse(where, f"expected bf16 [{rows}, {heads}, {head_dim}] on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
+    row, head, element = t.stride()
+    if (head_dim > 1 and element != 1) or (heads > 1 and head != head_dim):
         _refuse(where, "the heads of a row are contiguous")
-    return s[0] if rows > 1 else (heads * head_dim + 7) // 8 * 8
+    return row if rows > 1 else (heads * head_dim + 7) // 8 * 8
 
 
 def _empty_rows(rows: int, heads: int, head_dim: int, device) -> torch.Tensor:
@@ -620,9 +621,16 @@ def _empty_rows(rows: int, heads: int, head_dim: int, device) -> torch.Tensor:
     return t.as_strided((rows, heads, head_dim), (t.shape[1], head_dim, 1))
 
 
-def _same_device(cache: KVCache, batch: KVBatch, where: str):
-    if batch.device != cache.device:
+def _launch_device(cache: KVCache, batch: KVBatch, where: str) -> int:
+    """Index of the device that the cache and the batch are on."""
+    if batch.index != cache.index:
         _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
+    return cache.index
+
+
+def _stream_of(stream, index: int) -> int:
+    # (what torch.cuda.current_stream(index).cuda_stream gives, without the objects in between)
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
 
 
 def kv_append(cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor | None = None,
@@ -630,32 +638,32 @@ def kv_append(cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, 
     """bitlinear_kv_append: rotates k [T, kv_heads, head_dim] and stores it with v in the cache; rotates q [T, heads, head_dim]
     into q_out (allocated if not given, may be q itself) and returns it (None without q)."""
     where = "bitlinear_kv_append"
-    device = cache.device
-    _same_device(cache, batch, where)
-    if torch.cuda.current_device() != device.index:
-        with torch.cuda.device(device):
+    index = _launch_device(cache, batch, where)
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
             return kv_append(cache, batch, k, v, q, rope, interleaved, q_out, stream)
     T, D = k.shape[0], cache.head_dim
-    ks = _row_stride(k, cache.kv_heads, D, T, device, where)
-    vs = _row_stride(v, cache.kv_heads, D, T, device, where)
+    ks = _row_stride(k, cache.kv_heads, D, T, index, where)
+    vs = _row_stride(v, cache.kv_heads, D, T, index, where)
     heads = qs = os_ = positions = 0
     if q is not None:
         heads = q.shape[1] if q.dim() == 3 else 0
-        qs = _row_stride(q, heads, D, T, device, where)
+        qs = _row_stride(q, heads, D, T, index, where)
         if q_out is None:
-            q_out = _empty_rows(T, heads, D, device)
-        os_ = _row_stride(q_out, heads, D, T, device, where)
+            q_out = _empty_rows(T, heads, D, cache.device)
+        os_ = _row_stride(q_out, heads, D, T, index, where)
     elif q_out is not None:
         _refuse(where, "q_out without q")
     if rope is not None:
         positions = rope.shape[0]
-        if rope.shape != (positions, D // 2, 2) or rope.dtype != torch.float32 or not rope.is_contiguous() or rope.device != device:
-            _refuse(where, f"rope is a contiguous fp32 [positions, {D // 2}, 2] on {device}")
+        if rope.shape != (positions, D // 2, 2) or rope.dtype is not torch.float32 or not rope.is_contiguous() or rope.get_device() != index:
+            _refuse(where, f"rope is a contiguous fp32 [positions, {D // 2}, 2] on {cache.device}")
     st = (_lib or load_library()).bitlinear_kv_append(
         cache._address, batch._address, k.data_ptr(), ks, v.data_ptr(), vs, 0 if q is None else q.data_ptr(), qs, T, heads,
         0 if rope is None else rope.data_ptr(), positions, 1 if interleaved else 0, 0 if q_out is None else q_out.data_ptr(), os_,
-        _stream(stream))
-    _check(st, where)
+        _stream_of(stream, index))
+    if st != OK:
+        _check(st, where)
     return q_out
 
 
@@ -673,34 +681,35 @@ def alloc_attend_workspace(heads: int, kv_heads: int, head_dim: int, prompt: boo
 
 def _attend(prompt: bool, cache: KVCache, batch: KVBatch, q, scale, out, workspace, stream):
     where = "bitlinear_attend_prompt" if prompt else "bitlinear_attend_decode"
-    device = cache.device
-    _same_device(cache, batch, where)
-    if torch.cuda.current_device() != device.index:
-        with torch.cuda.device(device):
+    index = _launch_device(cache, batch, where)
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
             return _attend(prompt, cache, batch, q, scale, out, workspace, stream)
     if q.dim() != 3:
         _refuse(where, "q is [tokens, heads, head_dim]", ERR_SHAPE)
-    T, heads, D = q.shape[0], q.shape[1], cache.head_dim
+    T, heads, _ = q.shape
+    D = cache.head_dim
     if not prompt and T != batch.n_seqs:
         _refuse(where, f"{batch.n_seqs} sequences and {T} tokens", ERR_SHAPE)
-    qs = _row_stride(q, heads, D, T, device, where)
+    qs = _row_stride(q, heads, D, T, index, where)
     if out is None:
-        out = _empty_rows(T, heads, D, device)
-    os_ = _row_stride(out, heads, D, T, device, where)
+        out = _empty_rows(T, heads, D, cache.device)
+    os_ = _row_stride(out, heads, D, T, index, where)
     if workspace is None:
-        workspace = alloc_attend_workspace(heads, cache.kv_heads, D, prompt, device)
-    elif workspace.device != device or not workspace.is_contiguous():
-        _refuse(where, f"the workspace is contiguous and on {device}")
+        workspace = alloc_attend_workspace(heads, cache.kv_heads, D, prompt, cache.device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        _refuse(where, f"the workspace is contiguous and on {cache.device}")
     scale = D ** -0.5 if scale is None else float(scale)
     nbytes = workspace.numel() * workspace.element_size()
     L = _lib or load_library()
     if prompt:
         st = L.bitlinear_attend_prompt(cache._address, batch._address, q.data_ptr(), qs, T, heads, scale, out.data_ptr(), os_,
-                                       workspace.data_ptr(), nbytes, _stream(stream))
+                                       workspace.data_ptr(), nbytes, _stream_of(stream, index))
     else:
         st = L.bitlinear_attend_decode(cache._address, batch._address, q.data_ptr(), qs, heads, scale, out.data_ptr(), os_,
-                                       workspace.data_ptr(), nbytes, _stream(stream))
-    _check(st, where)
+                                       workspace.data_ptr(), nbytes, _stream_of(stream, index))
+    if st != OK:
+        _check(st, where)
     return out
 
 

@@ -98,7 +98,7 @@ struct PromptArgs {
 __device__ __forceinline__ float exp2_approx(float x)
 {
     float y;
-    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 // The largest of three, or NaN if one of them is.

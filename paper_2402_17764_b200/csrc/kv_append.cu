@@ -4,11 +4,18 @@
 // A pair (a, b) of a head becomes (a c - b s, b c + a s) with (c, s) of its position and its place i in the head.  Every
 // (token, head) is one group of lanes: 8 lanes with 16-byte pieces where the head is a multiple of 16 elements, a warp with
 // 4-byte pieces otherwise (the 100-wide heads of the 3B shape are only 8-byte aligned).  A lane holds both halves of
-// its pairs, so nothing but the 8-bit cache's row maximum crosses lanes.
+// its pairs, so nothing but the 8-bit cache's row maximum crosses lanes.  A CTA serves one token: its sequence, position, page
+// and angles are looked up once, and its groups walk the token's heads; with few tokens several CTAs share a token.
+//
+// 8 bits: code = round(127 x / beta) has to come out as in exact arithmetic, also for values half way between two codes.  All is
+// done in fp32 first; the few elements that fp32 cannot settle (candidates for the row's maximum, quotients near the
+// middle between two codes) are computed again in double from memory.
 //
 // What bounds it: memory (every byte read and written once) for prompts, the launch and one chain of dependent loads
 // (length, page number, row) for a decode step.
 #include <math.h>
+
+#include <algorithm>
 
 #include "internal.cuh"
 #include "kv.cuh"
@@ -64,73 +71,63 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&x)[V
     *reinterpret_cast<Piece<VEC> *>(p) = w;
 }
 
-// round(127 x / beta), half to even.  y32 is 127 x / beta up to 1e-4 (its few fp32 roundings at magnitude 127), which
-// settles all values except those near the middle between two codes; those are divided in double.
-__device__ __forceinline__ int code_of(float y32, double x, double beta)
-{
-    const float c = rintf(y32);
-    if (fabsf(fabsf(y32 - c) - 0.5f) > 4e-4f) return (int)c;
-    return (int)rint(x * 127.0 / beta);
-}
-
 // kRotate: 0 none, 1 pairs half a head apart, 2 adjacent pairs.
 template <int VEC, bool kInt8, int kRotate>
-__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ AppendArgs a)
+__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares)
 {
-    constexpr int kLanes = VEC == 8 ? 8 : 32;
+    constexpr int kLanes = VEC == 8 ? 8 : 32, kGroups = 256 / kLanes;
     const int D = a.cache.head_dim, half = D / 2, Hk = a.cache.kv_heads;
-    const int tasks = a.heads + 2 * Hk;
-    const int64_t group = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+    const int tasks = a.heads + 2 * Hk; // query heads, key heads, value heads
+    const int t = blockIdx.x / shares, share = blockIdx.x - t * shares;
     const int lane = threadIdx.x % kLanes;
-    const int64_t t64 = group / tasks;
-    const int task = (int)(group - t64 * tasks);
-    const int t = (int)t64;
-    bool active = t64 < a.T;
-    int b = -1, first = 0, count = 0, pos = -1;
-    if (active) b = kv_sequence_of(a.batch, t, first, count);
-    if (b >= 0) pos = a.batch.kv_lens[b] - count + (t - first);
-    active = active && b >= 0 && pos >= 0;
-    if (active && (pos >= a.batch.capacity || (kRotate != 0 && pos >= a.rope_positions))) {
+
+    int first, count;
+    const int b = kv_sequence_of(a.batch, t, first, count);
+    if (b < 0) return;
+    const int pos = a.batch.kv_lens[b] - count + (t - first);
+    if (pos < 0) return;
+    if (pos >= a.batch.capacity || (kRotate != 0 && pos >= a.rope_positions)) {
         kv_report(a.cache);
-        active = false;
+        return;
     }
-    const bool is_q = task < a.heads;
-    const bool is_k = !is_q && task < a.heads + Hk;
-    const int h = is_q ? task : (task - a.heads) % Hk;
-    int row = -1;
-    if (active && !is_q) {
-        const int page = kv_page(a.cache, a.batch, b, pos);
-        if (page < 0)
-            kv_report(a.cache);
-        else
-            row = kv_row(a.cache, page, h, pos);
-    }
+    const int page = kv_page(a.cache, a.batch, b, pos);
+    if (page < 0) kv_report(a.cache);
+
     const bool mine = lane * 2 * VEC < D;
     const int o0 = kRotate == 2 ? lane * 2 * VEC : lane * VEC;
     const int o1 = kRotate == 2 ? o0 + VEC : half + lane * VEC;
-    const __nv_bfloat16 *src = is_q ? a.q + t64 * a.q_stride : (is_k ? a.k + t64 * a.k_stride : a.v + t64 * a.v_stride);
-    const bool work = active && mine && (is_q || row >= 0);
-    float x0[VEC] = {}, x1[VEC] = {};
     float2 cs[VEC] = {};
-    const bool rotate = kRotate != 0 && !(task >= a.heads + Hk);
-    if (work) {
-        load_piece<VEC>(src + h * D + o0, x0);
-        load_piece<VEC>(src + h * D + o1, x1);
-        if (rotate) {
-            const float4 *p = reinterpret_cast<const float4 *>(a.rope + (int64_t)pos * half + lane * VEC);
+    if (kRotate != 0 && mine) {
+        const float4 *p = reinterpret_cast<const float4 *>(a.rope + (int64_t)pos * half + lane * VEC);
 #pragma unroll
-            for (int i = 0; i < VEC / 2; ++i) {
-                const float4 w = p[i];
-                cs[2 * i] = make_float2(w.x, w.y);
-                cs[2 * i + 1] = make_float2(w.z, w.w);
-            }
+        for (int i = 0; i < VEC / 2; ++i) {
+            const float4 w = p[i];
+            cs[2 * i] = make_float2(w.x, w.y);
+            cs[2 * i + 1] = make_float2(w.z, w.w);
         }
     }
-    // the j-th pair of this lane: (x0[j], x1[j]), or two neighbours
-    auto first_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j] : x1[2 * j - VEC]) : x0[j]; };
-    auto second_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j + 1] : x1[2 * j + 1 - VEC]) : x1[j]; };
-
-    if (!kInt8 || is_q) {
+    // every lane of a warp goes through the same rounds (the 8-bit row maximum is a shuffle)
+    for (int round = share * kGroups; round < tasks; round += shares * kGroups) {
+        const int task = round + threadIdx.x / kLanes;
+        const bool is_q = task < a.heads, is_k = !is_q && task < a.heads + Hk;
+        const int h = is_q ? task : (is_k ? task - a.heads : task - a.heads - Hk);
+        const bool work = task < tasks && mine && (is_q || page >= 0);
+        const __nv_bfloat16 *src =
+            (is_q ? a.q + (int64_t)t * a.q_stride : (is_k ? a.k + (int64_t)t * a.k_stride : a.v + (int64_t)t * a.v_stride)) + h * D;
+        float x0[VEC] = {}, x1[VEC] = {};
+        if (work) {
+            load_piece<VEC>(src + o0, x0);
+            load_piece<VEC>(src + o1, x1);
+        }
+        // the j-th pair of this lane: (x0[j], x1[j]), or two neighbours
+        auto first_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j] : x1[2 * j - VEC]) : x0[j]; };
+        auto second_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j + 1] : x1[2 * j + 1 - VEC]) : x1[j]; };
+        const bool rotate = kRotate != 0 && (is_q || is_k);
+        bool finite = true;
+        if (kInt8) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) finite = finite && fabsf(x0[i]) <= 3.4028235e38f && fabsf(x1[i]) <= 3.4028235e38f;
+        }
         if (rotate) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
@@ -139,72 +136,86 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ 
                 second_of(j) = r * cs[j].x + p * cs[j].y;
             }
         }
-        if (work) {
-            __nv_bfloat16 *dst = is_q ? a.q_out + t64 * a.q_out_stride + h * D
-                                      : reinterpret_cast<__nv_bfloat16 *>(is_k ? a.cache.k : a.cache.v) + (int64_t)row * a.cache.width;
-            store_piece<VEC>(dst + o0, x0);
-            store_piece<VEC>(dst + o1, x1);
+        const int64_t row = is_q || page < 0 ? 0 : kv_row(a.cache, page, h, pos);
+        if (!kInt8 || is_q) {
+            if (work) {
+                __nv_bfloat16 *dst = is_q ? a.q_out + (int64_t)t * a.q_out_stride + h * D
+                                          : reinterpret_cast<__nv_bfloat16 *>(is_k ? a.cache.k : a.cache.v) + row * a.cache.width;
+                store_piece<VEC>(dst + o0, x0);
+                store_piece<VEC>(dst + o1, x1);
+            }
+            if (VEC == 2 && !kInt8 && !is_q && task < tasks && page >= 0 && lane < a.cache.width - D) // (the row's padding)
+                reinterpret_cast<__nv_bfloat16 *>(is_k ? a.cache.k : a.cache.v)[row * a.cache.width + D + lane] = __float2bfloat16(0.0f);
         }
-        if (!kInt8 && row >= 0 && lane < a.cache.width - D)
-            reinterpret_cast<__nv_bfloat16 *>(is_k ? a.cache.k : a.cache.v)[(int64_t)row * a.cache.width + D + lane] = __float2bfloat16(0.0f);
-    }
-    if (kInt8) {
-        // every lane of the warp takes part in the shuffles, whatever its group does
-        double z0[VEC], z1[VEC], top = 0.0;
-        bool finite = true;
+        if (kInt8) {
+            // element i of x0, then of x1, exactly (up to 2^-53)
+            auto exact = [&](int i) -> double {
+                const int e = i < VEC ? o0 + i : o1 + i - VEC;
+                const double x = __bfloat162float(src[e]);
+                if (!rotate) return x;
+                const int pair = kRotate == 2 ? e >> 1 : (e < half ? e : e - half);
+                const bool second = kRotate == 2 ? (e & 1) != 0 : e >= half;
+                const float2 w = a.rope[(int64_t)pos * half + pair];
+                const double y = __bfloat162float(src[kRotate == 2 ? e ^ 1 : (second ? e - half : e + half)]);
+                return second ? x * (double)w.x + y * (double)w.y : x * (double)w.x - y * (double)w.y;
+            };
+            float top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            double p = first_of(j), r = second_of(j);
+            for (int i = 0; i < 2 * VEC; ++i) top = fmaxf(top, fabsf(i < VEC ? x0[i] : x1[i - VEC]));
+#pragma unroll
+            for (int d = 1; d < kLanes; d <<= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                finite = __shfl_xor_sync(0xFFFFFFFFu, (int)finite, d) && finite;
+            }
+            // The rotated fp32 values are within 2^-22 of the row's maximum of the exact ones (three roundings of a c and b s,
+            // |a c| + |b s| <= 2 max): only those within 2^-20 of the largest can be the exact maximum.  (Near the end of
+            // fp32's range, where a rotation may overflow, nothing is settled in fp32.)
+            const bool huge = !(top <= 1e38f);
+            constexpr uint32_t kAll = 2 * VEC == 32 ? ~0u : (1u << (2 * VEC)) - 1u;
+            double beta = top;
             if (rotate) {
-                const double c = cs[j].x, s = cs[j].y, u = p * c - r * s;
-                r = r * c + p * s;
-                p = u;
-            }
-            z0[j] = p;
-            z1[j] = r;
-            finite = finite && fabs(p) <= 1e300 && fabs(r) <= 1e300;
-            top = fmax(top, fmax(fabs(p), fabs(r)));
-        }
+                beta = 0.0;
+                uint32_t candidates = 0;
 #pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) {
-            top = fmax(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            finite = __shfl_xor_sync(0xFFFFFFFFu, (int)finite, d) && finite;
-        }
-        if (!is_q && row >= 0) {
-            const double beta = fmax(top, 1e-5);
-            const float inv = 127.0f / (float)beta;
-            int8_t c0[VEC], c1[VEC];
+                for (int i = 0; i < 2 * VEC; ++i) candidates |= (uint32_t)(fabsf(i < VEC ? x0[i] : x1[i - VEC]) >= top * 0.99999905f) << i;
+                if (huge) candidates = kAll;
+                if (!work || is_q || !finite) candidates = 0;
+                for (; candidates; candidates &= candidates - 1) beta = fmax(beta, fabs(exact(__ffs(candidates) - 1)));
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const int p = finite ? code_of((float)z0[j] * inv, z0[j], beta) : 0;
-                const int r = finite ? code_of((float)z1[j] * inv, z1[j], beta) : 0;
-                if (kRotate == 2) {
-                    if (j < VEC / 2) {
-                        c0[2 * j] = (int8_t)p;
-                        c0[2 * j + 1] = (int8_t)r;
-                    } else {
-                        c1[2 * j - VEC] = (int8_t)p;
-                        c1[2 * j + 1 - VEC] = (int8_t)r;
-                    }
-                } else {
-                    c0[j] = (int8_t)p;
-                    c1[j] = (int8_t)r;
-                }
+                for (int d = 1; d < kLanes; d <<= 1) beta = fmax(beta, __shfl_xor_sync(0xFFFFFFFFu, beta, d));
             }
-            int8_t *dst = reinterpret_cast<int8_t *>(is_k ? a.cache.k : a.cache.v) + (int64_t)row * a.cache.width;
+            if (is_q || task >= tasks || page < 0) continue;
+            beta = fmax(beta, 1e-5);
+            int8_t *dst = reinterpret_cast<int8_t *>(is_k ? a.cache.k : a.cache.v) + row * a.cache.width;
             if (mine) {
-                if (VEC == 8) {
+                const float inv = 127.0f / (float)beta;
+                int8_t c[2 * VEC];
+                uint32_t unsettled = 0;
+#pragma unroll
+                for (int i = 0; i < 2 * VEC; ++i) {
+                    // 127 x / beta up to 127 (2^-22 + 3 2^-24) < 6e-5
+                    const float y = (i < VEC ? x0[i] : x1[i - VEC]) * inv, r = rintf(y);
+                    unsettled |= (uint32_t)(fabsf(fabsf(y - r) - 0.5f) < 1e-4f) << i;
+                    c[i] = finite ? (int8_t)(int)r : (int8_t)0;
+                }
+                if (huge) unsettled = kAll;
+                if (!finite) unsettled = 0;
+                if constexpr (VEC == 8) {
                     uint2 w0, w1;
-                    memcpy(&w0, c0, 8);
-                    memcpy(&w1, c1, 8);
+                    memcpy(&w0, c, 8);
+                    memcpy(&w1, c + 8, 8);
                     *reinterpret_cast<uint2 *>(dst + o0) = w0;
                     *reinterpret_cast<uint2 *>(dst + o1) = w1;
                 } else {
-                    *reinterpret_cast<char2 *>(dst + o0) = make_char2(c0[0], c0[1]);
-                    *reinterpret_cast<char2 *>(dst + o1) = make_char2(c1[0], c1[1]);
+                    *reinterpret_cast<char2 *>(dst + o0) = make_char2(c[0], c[1]);
+                    *reinterpret_cast<char2 *>(dst + o1) = make_char2(c[2], c[3]);
+                }
+                for (; unsettled; unsettled &= unsettled - 1) {
+                    const int i = __ffs(unsettled) - 1;
+                    dst[i < VEC ? o0 + i : o1 + i - VEC] = (int8_t)(int)rint(exact(i) * 127.0 / beta);
                 }
             }
-            if (lane < a.cache.width - D) dst[D + lane] = 0;
+            if (VEC == 2 && lane < a.cache.width - D) dst[D + lane] = 0;
             if (lane == 0) (is_k ? a.cache.k_scale : a.cache.v_scale)[row] = finite ? (float)(beta / 127.0) : __int_as_float(0x7FFFFFFF);
         }
     }
@@ -213,15 +224,16 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ 
 template <int VEC, bool kInt8>
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t stream)
 {
-    const int64_t groups = (int64_t)a.T * (a.heads + 2 * a.cache.kv_heads);
-    const int per_block = 256 / (VEC == 8 ? 8 : 32);
-    const unsigned blocks = (unsigned)((groups + per_block - 1) / per_block);
+    // CTAs per token: one round of heads per CTA while that does not make more CTAs than the GPU holds at a time
+    const int groups = 256 / (VEC == 8 ? 8 : 32), rounds = (a.heads + 2 * a.cache.kv_heads + groups - 1) / groups;
+    const int shares = std::max(1, std::min(rounds, 8 * sm_count() / a.T));
+    const unsigned blocks = (unsigned)a.T * (unsigned)shares;
     if (!a.rope)
-        kv_append_kernel<VEC, kInt8, 0><<<blocks, 256, 0, stream>>>(a);
+        kv_append_kernel<VEC, kInt8, 0><<<blocks, 256, 0, stream>>>(a, shares);
     else if (!a.interleaved)
-        kv_append_kernel<VEC, kInt8, 1><<<blocks, 256, 0, stream>>>(a);
+        kv_append_kernel<VEC, kInt8, 1><<<blocks, 256, 0, stream>>>(a, shares);
     else
-        kv_append_kernel<VEC, kInt8, 2><<<blocks, 256, 0, stream>>>(a);
+        kv_append_kernel<VEC, kInt8, 2><<<blocks, 256, 0, stream>>>(a, shares);
     return cudaGetLastError();
 }
 

@@ -165,6 +165,28 @@ def test_codes_of_values_between_two_codes_and_of_rows_that_are_not_finite(head_
         assert torch.all(got[bad] == 0) and torch.all(scale[bad].isnan())
 
 
+def test_codes_of_rotated_rows_at_the_ends_of_the_range():
+    """Rotated pairs whose length is beyond fp32's (and bf16's) largest value, subnormal ones, and the floor of beta."""
+    T, D = 64, 64
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(T, 1, D, generator=g)
+    x[0:8] = torch.sign(x[0:8]) * 3.3e38
+    x[8:16] *= 2.0 ** 125
+    x[16:24] *= 1e-39
+    x[24:32] *= 1e-6
+    x = x.to(torch.bfloat16).cuda()
+    s = R.Setup([T], 1, D, 16, 8, seed=10)
+    rope = R.angles(T, D)
+    cache = s.cache()
+    B.kv_append(cache, B.KVBatch(s.table, s.kv_lens, torch.tensor([0, T], dtype=torch.int32, device="cuda")), x, x, rope=rope)
+    cache.check()
+    got = torch.cat([s.pools[0][p, 0] for p in s.table[0, :T // 16].tolist()])
+    scale = torch.cat([s.scales[0][p, 0] for p in s.table[0, :T // 16].tolist()])
+    z, _ = R.rotate(x, rope, torch.arange(T, device="cuda"), False)
+    c, want = R.codes(z)
+    assert torch.equal(got, c[:, 0]) and torch.equal(scale, want[:, 0])
+
+
 def test_rotary_table():
     for n, d, base in ((1, 4, 10000.0), (5000, 100, 10000.0), (70001, 128, 500000.0)):
         got = B.rope_table(n, d, base).double()
