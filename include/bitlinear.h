@@ -390,7 +390,8 @@ size_t bitlinear_attend_workspace_bytes(int heads, int kv_heads, int head_dim, i
  *   out_t,h = sum_j p_j v_j,  p = softmax_j(softmax_scale * q_t,h . k_j),  j = 0 .. position of t,  kv head h / (heads / kv_heads)
  *   q     in   bf16 [T, heads, head_dim] (rotated), row stride in elements;  T = n_seqs for decode
  *   out   out  bf16 [T, heads, head_dim], row stride in elements; must not overlap q
- *   heads      a multiple of kv_heads, heads <= 4096 (prompt: T * heads / kv_heads <= 2^30)
+ *   heads      a multiple of kv_heads, heads <= 4096.  decode: n_seqs * (table_pages * page_size / 64 + 2) * heads < 2^31;
+ *              prompt: T * heads / kv_heads <= 2^30
  *   softmax_scale  > 0 and finite; usually 1 / sqrt(head_dim)
  *   workspace  >= bitlinear_attend_workspace_bytes(...), 256-byte aligned, filled with zeros by the caller once before its
  *              first use; every call leaves it fit for the next.  Two calls that may run at the same time must not

@@ -7,9 +7,11 @@
 //
 // What bounds it: reading the cache once (HBM).  So all query heads of a kv head are handled together (8 or 16 columns of
 // a matrix instruction), and the work is cut by bytes, not by sequences: the blocks of all (sequence, kv head) pairs stand
-// in one row, and every CTA takes an equal, contiguous share of it, wherever that begins and ends.  A pair that several
-// CTAs share is joined by whichever of them finishes last, in the order of the shares, so the result does not depend on
-// which one it was.
+// in one row of units, and every CTA takes an equal, contiguous share of it, wherever that begins and ends.  A pair ends with one
+// unit that stands for what beginning and joining a pair costs, about the time of a block (without it CTAs whose share
+// is many short sequences finished 30 us after the others: 32 sequences of 1 to 4096 tokens, 32 heads, 82 us).  A pair that
+// several CTAs share is joined by whichever of them finishes last, in the order of the shares, so the result does not
+// depend on which one it was.
 //
 // Inside a CTA each of the four warps streams keys of its own through a ring of its own (cp.async, 8 KB per stage, no
 // barrier between warps before the end of a pair): the ring keeps loading the next pair's keys while this one's are
@@ -43,7 +45,8 @@ struct Shape {
     static constexpr int kStage = kStageBytes + kScaleBytes;
     static constexpr int kStages = 3;
     static constexpr int kQ = 8 * NT;
-    static constexpr int kSmem = kWarps * kStages * kStage + kWarps * kQ * 8;
+    static constexpr int kMl = kWarps * kQ; // (maximum, sum) of the warps, and later of the parts
+    static constexpr int kSmem = kWarps * kStages * kStage + kMl * 8;
     static_assert(kQ * WT * 4 <= kStageBytes, "a warp's output fits the stage that it has just used up");
     static constexpr int kPartFloats = kQ * (WT + 2); // a partial result in the workspace
 };
@@ -102,6 +105,14 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w)
     return *reinterpret_cast<const uint32_t *>(&d);
 }
 
+__device__ __forceinline__ void add_scaled(float4 &x, float f, const float4 &y)
+{
+    x.x += f * y.x;
+    x.y += f * y.y;
+    x.z += f * y.z;
+    x.w += f * y.w;
+}
+
 // Byte offset of 16-byte piece c of row r of a stage's keys or values: the eight rows that an ldmatrix reads at one
 // c lie in eight different bank groups.
 template <int kRowBytes>
@@ -111,98 +122,112 @@ __device__ __forceinline__ uint32_t piece(int r, int c)
     return (uint32_t)(r * kRowBytes + ((c ^ x) << 4));
 }
 
-// A place in the row of all blocks: block `blk` of pair `pair` (kv head and chunk of its query heads) of sequence b.
+// A block of keys: block `blk` of pair `pair` (kv head and chunk of its query heads) of sequence b, at `unit` in the row.
 struct Place {
-    int b, pair, blk, nblk, len;
+    int b, pair, blk, nblk, len, unit;
 };
+constexpr int kPairCost = 1; // units at the end of a pair
 
+// Equal shares of the row: the first `rest` shares have one unit more.
 struct Plan {
-    int64_t total;      // blocks of all pairs
-    int shares;         // CTAs that have work
-    __device__ __forceinline__ int64_t begin_of(int i) const { return total * i / shares; }
-    __device__ __forceinline__ int share_of(int64_t block) const { return (int)(((block + 1) * shares - 1) / total); }
+    int shares, each, rest;
+    __device__ __forceinline__ Plan(int total, int most)
+    {
+        shares = min(total, most);
+        each = shares > 0 ? total / shares : 0;
+        rest = shares > 0 ? total - each * shares : 0;
+    }
+    __device__ __forceinline__ int begin_of(int i) const { return i * each + min(i, rest); }
+    __device__ __forceinline__ int share_of(int unit) const
+    {
+        const int longer = rest * (each + 1);
+        return unit < longer ? unit / (each + 1) : rest + (unit - longer) / each;
+    }
 };
 
 template <bool kInt8, int WT, int NT>
 __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads)
 {
     using S = Shape<kInt8, WT, NT>;
-    constexpr int kKeys = S::kKeys, kBlock = kWarps * kKeys, kSteps = WT / 16, kRB = S::kRowBytes;
+    constexpr int kKeys = S::kKeys, kBlock = kWarps * kKeys, kSteps = WT / 16, kRB = S::kRowBytes, kThreads = kWarps * 32;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int64_t scan[kWarps + 1];
-    __shared__ int64_t found_rest;
-    __shared__ int found_b, is_last;
+    __shared__ int scan[kWarps], found_b, found_rest, is_last;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, tq = lane % 4;
     const int group = a.heads / a.cache.kv_heads, D = a.cache.head_dim, W = a.cache.width;
     const int pairs = a.cache.kv_heads * chunks, n_seqs = a.batch.n_seqs;
 
-    // ---- the row of all blocks: its length, and where this CTA's share begins --------------------------------
-    const int per_thread = (n_seqs + kWarps * 32 - 1) / (kWarps * 32);
+    // ---- the row: its length (the host made sure that it fits 31 bits), and where this CTA's share begins --------------
+    auto length = [&](int b) {
+        bool over;
+        return kv_length(a.batch, b, over);
+    };
+    auto blocks_of = [&](int len) { return (len + kBlock - 1) / kBlock; };
+    auto units_of = [&](int len) { return len > 0 ? (blocks_of(len) + kPairCost) * pairs : 0; };
+    const int per_thread = (n_seqs + kThreads - 1) / kThreads;
     const int b0 = min(n_seqs, tid * per_thread), b1 = min(n_seqs, b0 + per_thread);
-    int64_t mine = 0;
+    int mine = 0;
     for (int b = b0; b < b1; ++b) {
         bool over;
         const int n = kv_length(a.batch, b, over);
         if (over && blockIdx.x == 0) kv_report(a.cache);
-        mine += (int64_t)((n + kBlock - 1) / kBlock) * pairs;
+        mine += units_of(n);
     }
-    int64_t upto = mine;
+    int upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int64_t x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        const int x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
         if (lane >= d) upto += x;
     }
     if (lane == 31) scan[warp] = upto;
     __syncthreads();
-    Plan plan;
-    plan.total = 0;
+    int total = 0;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) upto += scan[w];
-        plan.total += scan[w];
+        total += scan[w];
     }
-    plan.shares = (int)(plan.total < (int64_t)gridDim.x ? plan.total : (int64_t)gridDim.x);
-
-    // empty slots of the batch get zeros
-    for (int b = blockIdx.x; b < n_seqs; b += gridDim.x) {
-        if (a.batch.kv_lens[b] > 0) continue;
-        uint32_t *row = reinterpret_cast<uint32_t *>(a.out + (int64_t)b * a.out_stride);
-        for (int i = tid; i < a.heads * D / 2; i += kWarps * 32) row[i] = 0u;
-    }
-    if ((int)blockIdx.x >= plan.shares) return;
-    const int64_t share_begin = plan.begin_of(blockIdx.x), share_end = plan.begin_of(blockIdx.x + 1);
-    if (share_begin >= upto - mine && share_begin < upto) {
-        int64_t rest = share_begin - (upto - mine);
-        int b = b0;
-        for (;; ++b) {
-            bool over;
-            const int64_t blocks = (int64_t)((kv_length(a.batch, b, over) + kBlock - 1) / kBlock) * pairs;
-            if (rest < blocks) break;
-            rest -= blocks;
+    const Plan plan(total, gridDim.x);
+    const bool works = (int)blockIdx.x < plan.shares;
+    const int share_begin = plan.begin_of(blockIdx.x), share_end = plan.begin_of(blockIdx.x + 1);
+    if (works && share_begin >= upto - mine && share_begin < upto) {
+        int rest = share_begin - (upto - mine), b = b0;
+        for (; b < b1 - 1; ++b) {
+            const int units = units_of(length(b));
+            if (rest < units) break;
+            rest -= units;
         }
         found_b = b;
         found_rest = rest;
     }
     __syncthreads();
 
-    auto length = [&](int b) {
-        bool over;
-        return kv_length(a.batch, b, over);
-    };
-    Place first;
-    first.b = found_b;
-    first.len = length(first.b);
-    first.nblk = (first.len + kBlock - 1) / kBlock;
-    first.pair = (int)(found_rest / first.nblk);
-    first.blk = (int)(found_rest - (int64_t)first.pair * first.nblk);
-    auto advance = [&](Place &p) { // only called while blocks are left behind p
-        if (++p.blk < p.nblk) return;
+    // a place that is inside the share, or `unit` >= share_end
+    auto settle = [&](Place &p) { // p.blk may be behind the pair's last block
+        if (p.blk < p.nblk) return;
+        p.unit += p.nblk + kPairCost - p.blk;
         p.blk = 0;
-        if (++p.pair < pairs) return;
+        if (p.unit >= share_end || ++p.pair < pairs) return;
         p.pair = 0;
         do p.len = length(++p.b);
         while (p.len == 0);
-        p.nblk = (p.len + kBlock - 1) / kBlock;
+        p.nblk = blocks_of(p.len);
     };
+    auto advance = [&](Place &p) {
+        ++p.blk;
+        ++p.unit;
+        settle(p);
+    };
+    Place first;
+    first.unit = share_end;
+    if (works) {
+        first.b = found_b;
+        first.len = length(first.b);
+        first.nblk = blocks_of(first.len);
+        first.pair = found_rest / (first.nblk + kPairCost);
+        first.blk = found_rest - first.pair * (first.nblk + kPairCost);
+        first.unit = share_begin;
+        settle(first);
+    }
 
     // ---- the ring --------------------------------------------------------------------------------------
     uint8_t *ring = smem + warp * S::kStages * S::kStage;
@@ -418,15 +443,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
     uint32_t *counters = reinterpret_cast<uint32_t *>(ws);
     float *parts = reinterpret_cast<float *>(ws + decode_counter_bytes());
     auto part_of = [&](int share, int which) { return parts + (int64_t)(share * kMaxSplits + which) * S::kPartFloats; };
-    auto store_out = [&](const Place &p, int q, int e, float x, float y) { // two neighbours of a query head's output
+    auto store_out = [&](const Place &p, int q, int e, const float4 &x, float inv) { // four neighbours of a query head's output
         const int head = p.pair / chunks, i = (p.pair % chunks) * chunk_heads + q;
-        if (q < chunk_heads && i < group && e < D)
-            *reinterpret_cast<uint32_t *>(a.out + (int64_t)p.b * a.out_stride + (int64_t)(head * group + i) * D + e) = pack_bf16(x, y);
+        if (i < group && e < D)
+            *reinterpret_cast<uint2 *>(a.out + (int64_t)p.b * a.out_stride + (int64_t)(head * group + i) * D + e) =
+                make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
     };
     // The warps lay their outputs down as [query][element] in the stage they have just used up (the next fetch into it
     // comes after this); element e of query q stands at e ^ 8 (q / 2 % 4), so that the lanes of a store hit 32 banks.
     auto laid = [](int q, int e) { return q * WT + (e ^ (((q >> 1) & 3) << 3)); };
-    auto end_pair = [&](const Place &p, int64_t block, int stage) { // p: the last block of the pair that this CTA has, at `block` in the row
+    auto end_pair = [&](const Place &p, int stage) { // p: the last block of the pair that this CTA has
         __syncwarp();
         float *own = reinterpret_cast<float *>(ring + stage * S::kStage);
 #pragma unroll
@@ -436,21 +462,24 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
                 const int q = t * 8 + 2 * tq + j;
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[t][j] += __shfl_xor_sync(0xFFFFFFFFu, l[t][j], d);
-                if (g == 0) join_ml[warp * S::kQ + q] = make_float2(m[t][j], l[t][j]);
+                if (q < chunk_heads) {
+                    if (g == 0) join_ml[warp * S::kQ + q] = make_float2(m[t][j], l[t][j]);
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    const int e = i * 16 + (kInt8 ? 2 * g : g);
-                    own[laid(q, e)] = o[t][i][j];
-                    own[laid(q, e + (kInt8 ? 1 : 8))] = o[t][i][2 + j];
+                    for (int i = 0; i < kSteps; ++i) {
+                        const int e = i * 16 + (kInt8 ? 2 * g : g);
+                        own[laid(q, e)] = o[t][i][j];
+                        own[laid(q, e + (kInt8 ? 1 : 8))] = o[t][i][2 + j];
+                    }
                 }
             }
         __syncthreads();
-        const int64_t pair_begin = block - p.blk, pair_end = pair_begin + p.nblk;
+        const int pair_begin = p.unit - p.blk, pair_end = pair_begin + p.nblk; // its blocks
         const bool whole = pair_begin >= share_begin && pair_end <= share_end;
-        const int which = pair_begin < share_begin ? 0 : 1;
-        float *part = whole ? nullptr : part_of(blockIdx.x, which);
-        for (int i = tid; i < S::kQ * WT / 2; i += kWarps * 32) {
-            const int q = i / (WT / 2), e = i % (WT / 2) * 2;
+        const int items = chunk_heads * (WT / 4); // four elements of a query each
+        // the four warps' results, in warp order
+        float *part = whole ? nullptr : part_of(blockIdx.x, pair_begin < share_begin ? 0 : 1);
+        for (int i = tid; i < items; i += kThreads) {
+            const int q = i / (WT / 4), e = i % (WT / 4) * 4;
             float2 ml[kWarps];
             float M = -INFINITY;
 #pragma unroll
@@ -459,20 +488,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
                 M = fmaxf(M, ml[w].x);
             }
             const float base = M == -INFINITY ? 0.0f : M;
-            float x = 0.0f, y = 0.0f, L = 0.0f;
+            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float L = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float f = exp2_approx(ml[w].x - base);
-                const float2 v = *reinterpret_cast<const float2 *>(smem + (w * S::kStages + stage) * S::kStage + 4 * laid(q, e));
-                x += f * v.x;
-                y += f * v.y;
+                add_scaled(x, f, *reinterpret_cast<const float4 *>(smem + (w * S::kStages + stage) * S::kStage + 4 * laid(q, e)));
                 L += f * ml[w].y;
             }
             if (whole) {
                 const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-                store_out(p, q, e, x * inv, y * inv);
+                store_out(p, q, e, x, inv);
             } else {
-                *reinterpret_cast<float2 *>(part + 2 * S::kQ + q * WT + e) = make_float2(x, y);
+                *reinterpret_cast<float4 *>(part + 2 * S::kQ + q * WT + e) = x;
                 if (e == 0) *reinterpret_cast<float2 *>(part + 2 * q) = make_float2(M, L);
             }
         }
@@ -489,28 +517,56 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
             __syncthreads();
             if (is_last) {
                 __threadfence();
-                for (int i = tid; i < S::kQ * WT / 4; i += kWarps * 32) {
-                    const int q = i / (WT / 4), e = i % (WT / 4) * 4;
-                    float M = -INFINITY;
-                    for (int c = from; c <= to; ++c) M = fmaxf(M, __ldcg(part_of(c, c == from ? 1 : 0) + 2 * q));
-                    const float base = M == -INFINITY ? 0.0f : M;
+                // the parts in the order of the shares; with few items each one is summed by several threads, every one
+                // over its own stretch of the parts, and their sums are added in order
+                int lanes = 1;
+                while (items * lanes * 2 <= kThreads) lanes *= 2;
+                const int n = to - from + 1, stretch = (n + lanes - 1) / lanes;
+                for (int i0 = 0; i0 < items; i0 += kThreads / lanes) {
+                    const int i = i0 + tid / lanes, q = i / (WT / 4), e = i % (WT / 4) * 4;
+                    const int c0 = from + min(n, tid % lanes * stretch), c1 = from + min(n, (tid % lanes + 1) * stretch);
                     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    float L = 0.0f;
-#pragma unroll 4
-                    for (int c = from; c <= to; ++c) {
-                        const float *src = part_of(c, c == from ? 1 : 0);
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(src + 2 * q));
-                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(src + 2 * S::kQ + q * WT + e));
-                        const float f = exp2_approx(ml.x - base);
-                        x.x += f * v.x;
-                        x.y += f * v.y;
-                        x.z += f * v.z;
-                        x.w += f * v.w;
-                        L += f * ml.y;
+                    float M = -INFINITY, L = 0.0f;
+                    if (i < items) {
+#pragma unroll 1
+                        for (int c = c0; c < c1; c += 8) { // eight parts' loads at a time
+                            float2 ml[8];
+                            float4 v[8];
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const int cc = min(c + u, c1 - 1);
+                                const float *src = part_of(cc, cc == from ? 1 : 0);
+                                ml[u] = __ldcg(reinterpret_cast<const float2 *>(src + 2 * q));
+                                v[u] = __ldcg(reinterpret_cast<const float4 *>(src + 2 * S::kQ + q * WT + e));
+                            }
+                            float top = M;
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) top = fmaxf(top, ml[u].x);
+                            const float base = top == -INFINITY ? 0.0f : top, keep = exp2_approx(M - base);
+                            x = make_float4(x.x * keep, x.y * keep, x.z * keep, x.w * keep);
+                            L *= keep;
+                            M = top;
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                const float f = c + u < c1 ? exp2_approx(ml[u].x - base) : 0.0f;
+                                if (c + u < c1) add_scaled(x, f, v[u]);
+                                L += c + u < c1 ? f * ml[u].y : 0.0f;
+                            }
+                        }
                     }
-                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-                    store_out(p, q, e, x.x * inv, x.y * inv);
-                    store_out(p, q, e + 2, x.z * inv, x.w * inv);
+                    // (lanes of one item are neighbours: at most 32 / its lanes items per warp)
+                    for (int d = 1; d < lanes; d <<= 1) {
+                        const float M2 = __shfl_xor_sync(0xFFFFFFFFu, M, d), L2 = __shfl_xor_sync(0xFFFFFFFFu, L, d);
+                        const float4 y = make_float4(__shfl_xor_sync(0xFFFFFFFFu, x.x, d), __shfl_xor_sync(0xFFFFFFFFu, x.y, d),
+                                                     __shfl_xor_sync(0xFFFFFFFFu, x.z, d), __shfl_xor_sync(0xFFFFFFFFu, x.w, d));
+                        const float top = fmaxf(M, M2), base = top == -INFINITY ? 0.0f : top;
+                        const float f = exp2_approx(M - base), f2 = exp2_approx(M2 - base);
+                        x = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+                        add_scaled(x, f2, y);
+                        L = L * f + L2 * f2;
+                        M = top;
+                    }
+                    if (i < items && tid % lanes == 0) store_out(p, q, e, x, L == 0.0f ? 0.0f : 1.0f / L);
                 }
             }
         }
@@ -521,45 +577,49 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
     // Three places walk along the share: the block whose page numbers are being looked up, the one being fetched (one
     // block behind it) and the one being consumed (kStages - 1 behind that).
     constexpr int kAhead = S::kStages - 1;
-    const int64_t blocks = share_end - share_begin;
-    Place now = first, get = first, look = first;
-    int pages_look = pages_of(look), pages_held[kAhead + 1];
-    int64_t fetched = 0;
+    Place now = first, look = first;
+    int pages_look = -1, pages_held[kAhead + 1];
+    if (look.unit < share_end) pages_look = pages_of(look);
     auto fetch_next = [&](int stage) { // returns the page numbers of the block it fetched
         int pages = -1;
-        if (fetched < blocks) {
+        if (look.unit < share_end) {
+            const Place get = look;
             pages = pages_look;
-            if (fetched + 1 < blocks) {
-                advance(look);
-                pages_look = pages_of(look);
-            }
+            advance(look);
+            if (look.unit < share_end) pages_look = pages_of(look);
             fetch(get, pages, stage);
-            get = look;
-            ++fetched;
         }
         cp_async_commit();
         return pages;
     };
+    if (now.unit < share_end) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) pages_held[i] = fetch_next(i);
-    begin_pair(now);
-    int stage = 0;
-    for (int64_t i = 0; i < blocks; ++i) {
-        cp_async_wait<kAhead - 1>();
-        __syncwarp();
-        pages_held[kAhead] = fetch_next(stage == 0 ? kAhead : stage - 1);
-        consume(now, pages_held[0], stage);
+        for (int i = 0; i < kAhead; ++i) pages_held[i] = fetch_next(i);
+        begin_pair(now);
+        int stage = 0;
+        for (;;) {
+            cp_async_wait<kAhead - 1>();
+            __syncwarp();
+            pages_held[kAhead] = fetch_next(stage == 0 ? kAhead : stage - 1);
+            consume(now, pages_held[0], stage);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) pages_held[j] = pages_held[j + 1];
-        const bool ends = now.blk + 1 == now.nblk;
-        if (ends || i + 1 == blocks) end_pair(now, share_begin + i, stage);
-        stage = stage == kAhead ? 0 : stage + 1;
-        if (i + 1 < blocks) {
+            for (int j = 0; j < kAhead; ++j) pages_held[j] = pages_held[j + 1];
+            const bool ends = now.blk + 1 == now.nblk;
+            if (ends || now.unit + 1 >= share_end) end_pair(now, stage);
+            stage = stage == kAhead ? 0 : stage + 1;
             advance(now);
+            if (now.unit >= share_end) break;
             if (ends) begin_pair(now);
         }
+        cp_async_wait<0>();
     }
-    cp_async_wait<0>();
+
+    // empty slots of the batch get zeros
+    for (int b = blockIdx.x; b < n_seqs; b += gridDim.x) {
+        if (length(b) > 0) continue;
+        uint32_t *row = reinterpret_cast<uint32_t *>(a.out + (int64_t)b * a.out_stride);
+        for (int i = tid; i < a.heads * D / 2; i += kThreads) row[i] = 0u;
+    }
 }
 
 template <bool kInt8, int WT, int NT>
@@ -595,6 +655,14 @@ size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim)
     decode_chunks(heads / kv_heads, chunks, chunk_heads);
     const size_t q = chunk_heads <= 8 ? 8 : 16, width = kv_row_width(head_dim) <= 64 ? 64 : 128;
     return align_up(decode_counter_bytes() + (size_t)kDecodeMaxCtas * kMaxSplits * q * (width + 2) * 4, 256);
+}
+
+bool attend_decode_fits(const AttendArgs &a)
+{
+    int chunks, chunk_heads;
+    decode_chunks(a.heads / a.cache.kv_heads, chunks, chunk_heads);
+    const int64_t units = (a.batch.capacity + 63) / 64 + kPairCost; // (blocks are 64 keys or more)
+    return units * a.cache.kv_heads * chunks <= 0x7FFFFFFF / std::max(a.batch.n_seqs, 1);
 }
 
 cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream)

@@ -107,6 +107,7 @@ struct AttendArgs {
 constexpr int kDecodeMaxCtas = 512;
 __host__ __device__ constexpr size_t decode_counter_bytes() { return kDecodeMaxCtas * sizeof(uint32_t); }
 size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim);
+bool attend_decode_fits(const AttendArgs &a); // the kernel counts its work in 31 bits
 cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream);
 
 // Workspace of the prompt kernel: two words per tile of rows that several CTAs share, then their partial results.

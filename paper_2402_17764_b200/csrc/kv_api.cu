@@ -156,6 +156,8 @@ bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batc
     if ((st = check_rows(out, out_stride, heads, a.cache.head_dim)) != BITLINEAR_OK) return st;
     if (!aligned(workspace, 256)) return BITLINEAR_ERR_ALIGN;
     if (workspace_bytes < workspace_for(heads, a.cache.kv_heads, a.cache.head_dim, prompt)) return BITLINEAR_ERR_WORKSPACE;
+    a.heads = heads;
+    if (!prompt && !attend_decode_fits(a)) return BITLINEAR_ERR_SHAPE;
     a.scale = (float)((double)softmax_scale * 1.4426950408889634074); // log2 e
     if (!std::isfinite(a.scale)) return BITLINEAR_ERR_ARG;
     if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
@@ -165,7 +167,6 @@ bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batc
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.T = (int32_t)T;
-    a.heads = heads;
     a.workspace = workspace;
     return (prompt ? launch_attend_prompt(a, (cudaStream_t)stream) : launch_attend_decode(a, (cudaStream_t)stream)) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }
