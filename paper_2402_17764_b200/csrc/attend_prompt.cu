@@ -135,6 +135,12 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
+// Copies kBytes to shared memory, or fills them with zeros (nothing is read then).
+template <int kBytes>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(real ? kBytes : 0) : "memory");
+}
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // Two signed bytes of w as two bf16 numbers, exactly (attend_decode.cu has the same step on its operands).
@@ -474,23 +480,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         const uint32_t lane_base = tmem + ((uint32_t)(32 * (warp % 4)) << 16), s_col = lane_base + t * kTile, o_col = lane_base + kRows + t * kTile;
         uint8_t *q_tile = smem + t * kTileBytes16;
         if (n_steps[t] > 0) {
-            // the tile's queries, in the layout of the MMA: this warp's 32 rows, two at a time, 16 bytes per lane (as two
-            // halves: heads of 100 elements are not 16-byte aligned)
+            // the tile's queries, in the layout of the MMA: this warp's 32 rows, two at a time, 16 bytes per lane (heads of 100
+            // elements are only 8-byte aligned: two halves)
             const int64_t mine = exists ? (int64_t)(w.first_token + row / group) * a.q_stride + (w.head * group + row % group) * D : -1;
-            const int c = lane % 16;
-            uint2 x[16], y[16];
+            const int c = lane % 16, left = D - c * 8; // elements of the head from this lane's piece on
+            const uint32_t dst = smem_u32(q_tile) + (c / 8) * kHalfBytes;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int64_t at = __shfl_sync(0xFFFFFFFFu, mine, 2 * i + lane / 16);
-                const __nv_bfloat16 *src = a.q + at + c * 8;
-                x[i] = at >= 0 && c * 8 < D ? *reinterpret_cast<const uint2 *>(src) : make_uint2(0, 0);
-                y[i] = at >= 0 && c * 8 + 4 < D ? *reinterpret_cast<const uint2 *>(src + 4) : make_uint2(0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
                 const int qr = warp % 4 * 32 + 2 * i + lane / 16;
-                *reinterpret_cast<uint4 *>(q_tile + (c / 8) * kHalfBytes + qr * 128 + (((c % 8) ^ (qr & 7)) << 4)) = make_uint4(x[i].x, x[i].y, y[i].x, y[i].y);
+                const uint32_t to = dst + qr * 128 + (((c % 8) ^ (qr & 7)) << 4);
+                const __nv_bfloat16 *src = a.q + (at < 0 || left <= 0 ? 0 : at + c * 8);
+                if (D % 8 == 0) {
+                    cp_async<16>(to, src, at >= 0 && left > 0);
+                } else {
+                    cp_async<8>(to, src, at >= 0 && left > 0);
+                    cp_async<8>(to + 8, left > 4 ? src + 4 : src, at >= 0 && left > 4);
+                }
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.q_full[t]));
@@ -662,16 +670,30 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
 #pragma unroll
                 for (int e = 0; e < kTile; e += 4)
                     if (e < W) *reinterpret_cast<float4 *>(part + e) = make_float4(at(e), at(e + 1), at(e + 2), at(e + 3));
-            } else if (exists && D % 8 == 0) {
+            } else {
+                // by way of the tile's queries, which are not needed any more, so that a warp stores whole rows
+                uint8_t *own = q_tile + (warp % 4) * 32 * 256;
 #pragma unroll
                 for (int e = 0; e < kTile; e += 8)
-                    if (e < D)
-                        *reinterpret_cast<uint4 *>(dst + e) = make_uint4(pack_bf16(at(e), at(e + 1)), pack_bf16(at(e + 2), at(e + 3)),
-                                                                         pack_bf16(at(e + 4), at(e + 5)), pack_bf16(at(e + 6), at(e + 7)));
-            } else if (exists) {
+                    *reinterpret_cast<uint4 *>(own + lane * 256 + (((e / 8) ^ (lane & 7)) << 4)) =
+                        make_uint4(pack_bf16(at(e), at(e + 1)), pack_bf16(at(e + 2), at(e + 3)), pack_bf16(at(e + 4), at(e + 5)),
+                                   pack_bf16(at(e + 6), at(e + 7)));
+                __syncwarp();
+                const int64_t mine = exists ? dst - a.out : -1;
+                const int c = lane % 16, left = D - c * 8;
 #pragma unroll
-                for (int e = 0; e < kTile; e += 4)
-                    if (e < D) *reinterpret_cast<uint2 *>(dst + e) = make_uint2(pack_bf16(at(e), at(e + 1)), pack_bf16(at(e + 2), at(e + 3)));
+                for (int i = 0; i < 16; ++i) {
+                    const int pr = 2 * i + lane / 16;
+                    const int64_t to = __shfl_sync(0xFFFFFFFFu, mine, pr);
+                    const uint4 y = *reinterpret_cast<const uint4 *>(own + pr * 256 + ((c ^ (pr & 7)) << 4));
+                    if (to < 0 || left <= 0) continue;
+                    if (D % 8 == 0) {
+                        *reinterpret_cast<uint4 *>(a.out + to + c * 8) = y;
+                    } else {
+                        *reinterpret_cast<uint2 *>(a.out + to + c * 8) = make_uint2(y.x, y.y);
+                        if (left > 4) *reinterpret_cast<uint2 *>(a.out + to + c * 8 + 4) = make_uint2(y.z, y.w);
+                    }
+                }
             }
         }
         if (parts > 1) {
