@@ -227,7 +227,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     const int D = a.cache.head_dim, W = a.cache.width, group = a.heads / a.cache.kv_heads, n_seqs = a.batch.n_seqs;
     const uint32_t limit = args.hooks.limit_us;
 
-    // ---- which rows: tiles are counted sequence by sequence, the last rows (which see most) of all kv heads first ----
+    // ---- which rows: tiles are counted sequence by sequence, the longest first, and within a sequence the last rows (which
+    // see most) of all kv heads first, so that the CTAs that start last have the least to do (four chunks of 86 to 512 tokens
+    // behind 3300 to 12000: 459 -> 383 us) ----
     const int split = blockIdx.x % args.splits;
     {
         const int64_t x = blockIdx.x / args.splits;
@@ -239,6 +241,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         const int b0 = min(n_seqs, tid * per_thread), b1 = min(n_seqs, b0 + per_thread);
         int64_t mine = 0;
         for (int b = b0; b < b1; ++b) mine += tiles_of(b);
+        int first_b = b0;
+        if (per_thread == 1) { // (longer lists of sequences are taken as they are)
+            int64_t *tiles_by_rank = reinterpret_cast<int64_t *>(smem);
+            int *lens = reinterpret_cast<int *>(tiles_by_rank + kThreads), *b_by_rank = lens + kThreads;
+            const int len = mine > 0 ? a.batch.kv_lens[b0] : 0;
+            lens[tid] = len;
+            __syncthreads();
+            int rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < n_seqs; ++j) rank += lens[j] > len || (lens[j] == len && j < tid);
+            if (tid < n_seqs) {
+                tiles_by_rank[rank] = mine;
+                b_by_rank[rank] = tid;
+            }
+            __syncthreads();
+            if (tid < n_seqs) {
+                mine = tiles_by_rank[tid];
+                first_b = b_by_rank[tid];
+            }
+            fence_proxy_async_smem(); // (the same bytes are copied to by the async proxy later)
+        }
         int64_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -251,11 +274,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         for (int w = 0; w < warp; ++w) upto += sh.scan[w];
         if (x >= upto - mine && x < upto) {
             int64_t rest = x - (upto - mine);
-            int b = b0;
-            for (; b < b1 - 1; ++b) {
+            int b = first_b;
+            for (int i = 1; i < per_thread; ++i) {
                 const int64_t n = tiles_of(b);
                 if (rest < n) break;
                 rest -= n;
+                ++b;
             }
             sh.found_b = b;
             sh.found_local = rest;
