@@ -18,8 +18,12 @@
 // finished.  Scores are K Q^T (keys are the 16 rows of the instruction, queries its 8 columns) and the output is
 // V^T P^T (16 elements of the head, 8 queries), so that a group of 1 to 8 query heads wastes at most the columns it does not have;
 // P^T changes from accumulator to operand by movmatrix.  The weights enter as two bf16 parts (value and remainder): the
-// tensor cores have time for it, and the result is as exact as fp32 weights would give.  int8 rows become bf16 exactly
-// (code_pair below); a key's scale multiplies its score, a value's scale its weight.
+// tensor cores have time for it, and the result is as exact as fp32 weights would give.
+//
+// int8 cache: a key's scale multiplies its score, a value's scale its weight.  Values become bf16 exactly (code_pair below, four
+// instructions per two elements, which is what bounds the kernel then).  Keys stay codes: the queries are written as integers of
+// 23 bits, relative to the power of two above their row's largest, in three signed bytes, and the scores are exact
+// integer products of codes and bytes (three MMAs of twice the depth instead of 16 conversions per MMA).
 #include <algorithm>
 
 #include "internal.cuh"
@@ -80,6 +84,12 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_s8(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float exp2_approx(float x)
@@ -278,7 +288,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
     };
 
     // ---- a pair's state ----------------------------------------------------------------------------------
-    uint32_t qf[NT][kSteps][2];
+    // (two tiles of queries as three bytes each would not fit the registers)
+    constexpr bool kDigits = kInt8 && NT == 1;
+    uint32_t qf[NT][kSteps][2];       // queries as the MMA's operand
+    uint32_t qd[kDigits ? 3 : 1][kSteps]; // or their bytes, highest first
+    float factor = 0.0f;              // kDigits: of the integer scores of query g
     float o[NT][kSteps][4], m[NT][2], l[NT][2];
     auto begin_pair = [&](const Place &p) {
         const int head = p.pair / chunks, chunk = p.pair % chunks;
@@ -298,6 +312,35 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
             m[t][0] = m[t][1] = -INFINITY;
             l[t][0] = l[t][1] = 0.0f;
         }
+        if (kDigits) {
+            // the largest magnitude of the row (as the bits of a non-negative bf16 number), over the four lanes that share it
+            uint32_t top = 0;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) top = max(top, max(qf[0][s][h] & 0x7FFFu, (qf[0][s][h] >> 16) & 0x7FFFu));
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            // 2^e with 2^21 <= largest 2^e < 2^22 (e is cut at 120: rows below 2^-99 keep fewer bits)
+            const int e = min(120, 21 + 127 - (int)max(top >> 7, 1u));
+            const float up = __int_as_float((127 + e) << 23);
+            factor = (top >> 7) == 0xFFu ? __int_as_float(0x7FFFFFFF) : a.scale * __int_as_float((127 - e) << 23); // (not finite: NaN)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                uint32_t d[3] = {0u, 0u, 0u};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t w = qf[0][s][i / 2];
+                    const int v = __float2int_rn(__uint_as_float(i % 2 ? w & 0xFFFF0000u : w << 16) * up);
+                    const int d2 = (int)(int8_t)v, v1 = (v - d2) >> 8, d1 = (int)(int8_t)v1, d0 = (v1 - d1) >> 8;
+                    d[0] |= ((uint32_t)d0 & 0xFFu) << (8 * i);
+                    d[1] |= ((uint32_t)d1 & 0xFFu) << (8 * i);
+                    d[2] |= ((uint32_t)d2 & 0xFFu) << (8 * i);
+                }
+#pragma unroll
+                for (int i = 0; i < (kDigits ? 3 : 1); ++i) qd[i][s] = d[i];
+            }
+        }
     };
 
     // one stage: the scores of its keys, the weights, and their share of the output
@@ -314,7 +357,19 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
 #pragma unroll
             for (int t = 0; t < NT; ++t) s[q][t][0] = s[q][t][1] = s[q][t][2] = s[q][t][3] = 0.0f;
             const int r = q * 16 + (lane & 15);
-            if (!kInt8) {
+            if (kDigits) {
+                int sum[3][4] = {};
+#pragma unroll
+                for (int i = 0; i < kSteps; i += 2) {
+                    uint32_t k[4];
+                    ldmatrix_x4(at + piece<kRB>(r, i + (lane >> 4)), k);
+#pragma unroll
+                    for (int d = 0; d < (kDigits ? 3 : 1); ++d) mma_s8(sum[d], k, qd[d][i], qd[d][i + 1]);
+                }
+                // (the upper two sums together are below 2^31: 128 products of 2^7 and 2^14 + 2^7)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[q][0][c] = (float)(sum[0][c] * 256 + sum[1][c]) * 256.0f + (float)sum[2][c];
+            } else if (!kInt8) {
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
                     uint32_t k[4];
@@ -338,6 +393,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
             }
         }
         // scale, mask, running maximum
+        // (the factor of query 2 tq + j stands in the lanes of its column's operand)
+        const float column_factor[2] = {kDigits ? __shfl_sync(0xFFFFFFFFu, factor, 8 * tq) : 0.0f, kDigits ? __shfl_sync(0xFFFFFFFFu, factor, 8 * tq + 4) : 0.0f};
         bool bad = false;
         if (lane < kGroups) bad = pages < 0;
         const uint32_t bad_groups = __ballot_sync(0xFFFFFFFFu, bad);
@@ -350,14 +407,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int r = q * 16 + h * 8 + g;
-                const float f = kInt8 ? a.scale * scales[r] : a.scale;
+                const float f = kDigits ? scales[r] : (kInt8 ? a.scale * scales[r] : a.scale);
                 const bool seen = all || (r < n && !((bad_groups >> q) & 1u));
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         float &x = s[q][t][2 * h + j];
-                        x = seen ? x * f : -INFINITY;
+                        x = seen ? (kDigits ? x * f * column_factor[j] : x * f) : -INFINITY;
                         top[t][j] = fmaxf(top[t][j], x);
                     }
             }

@@ -67,13 +67,15 @@ class Setup:
         return x.transpose(0, 1).reshape(self.kv_heads, -1, self.head_dim)[:, :n]
 
 
-def attend(setup, q, counts, scale=None, weight_rounding=0.0):
+def attend(setup, q, counts, scale=None, weight_rounding=0.0, query_rounding=0.0):
     """(out, bound): the attention of the new tokens (counts[b] rows of q [T, heads, D] belong to sequence b, at its last
     positions) and how far a result may be from it.
 
     The bound, per output element, with w_j the weights and A = sum_j w_j |v_j|:
       a score is a dot product of D fp32 terms, scaled: |ds| <= (D + 4) 2^-24 scale sum_i |q_i k_i| (+ an int8 row's scale,
         one more rounding, within the + 4);  exp2 and its argument reduction add 2^-21 relative;
+      a kernel that rounds the queries to fixed point, each element by at most query_rounding max_i |q_i|, adds
+        scale query_rounding max_i |q_i| sum_i |k_i|;
       every weight is then off by a factor within 1 +- d, d = 2 max_j |ds_j| + 2^-21 + weight_rounding (one rounding of the
         weight to fewer bits, for a kernel that does that), the sums of n terms and the joins by (n + 64) 2^-24 more;
       numerator and denominator together: 2 (d + (n + 64) 2^-24) A, to first order; 1 % on top covers the second;
@@ -104,6 +106,9 @@ def attend(setup, q, counts, scale=None, weight_rounding=0.0):
             y = torch.einsum("hgnl,hld->hgnd", w, v)
             A = torch.einsum("hgnl,hld->hgnd", w, v.abs())
             worst = size.masked_fill(hidden, 0.0).amax(-1, keepdim=True) * (D + 4) * 2.0 ** -24
+            if query_rounding:
+                fixed = scale * x.abs().amax(-1)[..., None] * k.abs().sum(-1)[:, None, None]
+                worst = worst + query_rounding * fixed.masked_fill(hidden, 0.0).amax(-1, keepdim=True)
             d = 2 * worst + 2.0 ** -21 + weight_rounding + (L + 64) * 2.0 ** -24
             e = 1.01 * 2 * d * A + 2.0 ** -8 * y.abs() + 2.0 ** -134 + L * 2.0 ** -119 * max(1.0, v.abs().nan_to_num(0.0, 0.0).max().item())
             out[at:at + n] = y.permute(2, 0, 1, 3).reshape(n, H, D)

@@ -10,6 +10,17 @@ pytestmark = pytest.mark.gpu
 
 WEIGHT_BF16 = 2.0 ** -8  # the prompt kernel rounds its weights to bf16
 WEIGHT_TWO_BF16 = 2.0 ** -16  # the decode kernel splits them into two bf16 parts
+# Over an int8 cache the decode kernel takes a query's elements to integers, the largest of which is 2^21 or more: each is off by at
+# most half, 2^-22 of the largest.
+QUERY_FIXED = 2.0 ** -22
+
+
+def decode_error(bits):
+    return dict(weight_rounding=WEIGHT_TWO_BF16, query_rounding=QUERY_FIXED if bits == 8 else 0.0)
+
+
+def error_of(prompt, bits):
+    return dict(weight_rounding=WEIGHT_BF16) if prompt else decode_error(bits)
 
 
 def rows(T, heads, head_dim, seed, extra=0, size=1.5):
@@ -54,7 +65,7 @@ def test_decode_against_64_bits(heads, kv_heads, head_dim, page, lens, bits):
     ws = B.alloc_attend_workspace(heads, kv_heads, head_dim, prompt=False)
     B.attend_decode(cache, B.KVBatch(s.table, s.kv_lens), q, out=out, workspace=ws)
     cache.check()
-    want, bound = R.attend(s, q, [1] * len(lens), weight_rounding=WEIGHT_TWO_BF16)
+    want, bound = R.attend(s, q, [1] * len(lens), **decode_error(s.bits))
     check(out, want, bound)
     if guard is not None:
         assert torch.equal(guard[:, heads * head_dim:], edge)
@@ -71,7 +82,7 @@ def test_decode_of_a_long_and_a_short_context_together(bits):
     s = R.Setup(lens, 2, 128, 64, bits, seed=3)
     q = rows(len(lens), 16, 128, 4)
     got = B.attend_decode(s.cache(), B.KVBatch(s.table, s.kv_lens), q)
-    want, bound = R.attend(s, q, [1] * len(lens), weight_rounding=WEIGHT_TWO_BF16)
+    want, bound = R.attend(s, q, [1] * len(lens), **decode_error(s.bits))
     check(got, want, bound)
 
 
@@ -82,7 +93,7 @@ def test_decode_of_a_large_batch():
     s = R.Setup(lens, 1, 16, 16, 16, seed=4)
     q = rows(len(lens), 2, 16, 5)
     got = B.attend_decode(s.cache(), B.KVBatch(s.table, s.kv_lens), q)
-    want, bound = R.attend(s, q, [1] * len(lens), weight_rounding=WEIGHT_TWO_BF16)
+    want, bound = R.attend(s, q, [1] * len(lens), **decode_error(s.bits))
     check(got, want, bound)
 
 
@@ -150,11 +161,10 @@ def test_sharp_and_flat_softmax(prompt, bits):
     cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device="cuda")
     batch = B.KVBatch(s.table, s.kv_lens, cu if prompt else None)
     attend = B.attend_prompt if prompt else B.attend_decode
-    rounding = WEIGHT_BF16 if prompt else WEIGHT_TWO_BF16
     for size, scale in ((30.0, None), (0.0, None), (1.5, 0.7), (1.5, 1e-6)):
         q = rows(sum(new), 16, 128, 3, size=size)
         got = attend(s.cache(), batch, q, scale=scale)
-        want, bound = R.attend(s, q, new, scale=scale, weight_rounding=rounding)
+        want, bound = R.attend(s, q, new, scale=scale, **error_of(prompt, bits))
         check(got, want, bound)
 
 
@@ -173,7 +183,7 @@ def test_rising_scores_move_the_running_maximum(prompt):
         q = (direction * 8.0).to(torch.bfloat16).expand(T, 2, 64).contiguous()
         cu = torch.tensor([0, T], dtype=torch.int32, device="cuda")
         got = (B.attend_prompt if prompt else B.attend_decode)(s.cache(), B.KVBatch(s.table, s.kv_lens, cu if prompt else None), q)
-        want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16 if prompt else WEIGHT_TWO_BF16)
+        want, bound = R.attend(s, q, new, **error_of(prompt, s.bits))
         check(got, want, bound)
 
 
@@ -186,7 +196,7 @@ def test_bad_pages_are_left_out_and_reported(prompt, bits):
         s = R.Setup(lens, 2, 64, 16, bits, seed=13, table_extra=0)
         q = rows(sum(new), 4, 64, 3)
         cu = torch.tensor([0, new[0], new[0] + new[1], sum(new)], dtype=torch.int32, device="cuda")
-        want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16 if prompt else WEIGHT_TWO_BF16)
+        want, bound = R.attend(s, q, new, **error_of(prompt, s.bits))
         if bad is None:  # a length beyond the table: the keys in it count, the rest does not exist
             s.kv_lens[1] = 16 * s.table.shape[1] + 1000
         else:
@@ -225,7 +235,7 @@ def test_a_page_shared_by_two_sequences(prompt):
     q = rows(sum(new), 4, 64, 3)
     cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device="cuda")
     got = (B.attend_prompt if prompt else B.attend_decode)(s.cache(), B.KVBatch(s.table, s.kv_lens, cu if prompt else None), q)
-    want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16 if prompt else WEIGHT_TWO_BF16)
+    want, bound = R.attend(s, q, new, **error_of(prompt, s.bits))
     check(got, want, bound)
 
 
@@ -255,7 +265,7 @@ def test_a_poisoned_row_reaches_only_the_tokens_that_see_it(where, poison):
     s.lens = [99, 99]
     got = B.attend_decode(s.cache(), B.KVBatch(s.table, s.kv_lens), q[:2])
     poisoned, s.pools = s.pools, clean
-    want, bound = R.attend(s, q[:2], [1, 1], weight_rounding=WEIGHT_TWO_BF16)
+    want, bound = R.attend(s, q[:2], [1, 1], **decode_error(s.bits))
     check(got[0], want[0], bound[0])
     if where == "value" or poison != poison:
         assert not torch.any(torch.isfinite(got[1, :, 5]))
@@ -289,7 +299,7 @@ def test_a_captured_graph_follows_lengths_pages_and_queries(prompt):
             for g, _, _ in graphs:
                 g.replay()
         for s, o in zip((one, two), out):
-            want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16 if prompt else WEIGHT_TWO_BF16)
+            want, bound = R.attend(s, q, new, **error_of(prompt, s.bits))
             check(o, want, bound)
 
 
@@ -310,7 +320,7 @@ def test_two_streams_with_workspaces_of_their_own(prompt):
             attend(cache, batch, q, out=out, workspace=ws, stream=stream)
     torch.cuda.synchronize()
     for s, _, _, q, _, _, out in cases:
-        want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16 if prompt else WEIGHT_TWO_BF16)
+        want, bound = R.attend(s, q, new, **error_of(prompt, s.bits))
         check(out, want, bound)
 
 
