@@ -60,6 +60,10 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, bool 
     const int n = real ? 16 : 0; // 0: the 16 bytes become zero and nothing is read
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -262,23 +266,40 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
         const int n = p.len - key0; // keys that exist
         if (n <= 0) return;
         const int head = p.pair / chunks;
-        constexpr int kRowsAtOnce = 32 / S::kChunks > 0 ? 32 / S::kChunks : 1;
+        constexpr int kElement = kInt8 ? 1 : 2, kRowsAtOnce = 32 / S::kChunks;
         const int c = lane % S::kChunks, r0 = lane / S::kChunks;
-        const bool real_c = c * 16 < W * (kInt8 ? 1 : 2);
+        // all rows exist and are as long in the cache as in the ring: nothing to check per copy
+        const bool plain = W == WT && n >= kKeys && !__any_sync(0xFFFFFFFFu, lane < kKeys / 16 && pages < 0);
+        const bool real_c = c * 16 < W * kElement;
 #pragma unroll
         for (int q = 0; q < kKeys / 16; ++q) {
             const int page = __shfl_sync(0xFFFFFFFFu, pages, q);
             const bool have = page >= 0;
             const int64_t row = have ? kv_row(a.cache, page, head, key0 + q * 16) : 0;
-            const int64_t offset = row * W * (kInt8 ? 1 : 2) + c * 16;
-            const uint8_t *k = reinterpret_cast<const uint8_t *>(a.cache.k) + offset, *v = reinterpret_cast<const uint8_t *>(a.cache.v) + offset;
+            const uint8_t *kp = reinterpret_cast<const uint8_t *>(a.cache.k), *vp = reinterpret_cast<const uint8_t *>(a.cache.v);
+            if (plain) {
+                const int64_t offset = row * kRB + lane * 16; // (the rows of a group follow each other)
+                kp += offset;
+                vp += offset;
 #pragma unroll
-            for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
-                const int r = q * 16 + i * kRowsAtOnce + r0;
-                const bool real = have && real_c && r < n;
-                const int64_t skip = real ? (int64_t)(r - q * 16) * W * (kInt8 ? 1 : 2) : -c * 16; // (an address that exists in any case)
-                cp_async_16(at + piece<kRB>(r, c), k + skip, real);
-                cp_async_16(at + kStageBytes / 2 + piece<kRB>(r, c), v + skip, real);
+                for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+                    const uint32_t dst = at + piece<kRB>(q * 16 + i * kRowsAtOnce + r0, c);
+                    cp_async_16(dst, kp + i * 512);
+                    cp_async_16(dst + kStageBytes / 2, vp + i * 512);
+                }
+            } else {
+                const int64_t offset = row * W * kElement;
+                kp += offset;
+                vp += offset;
+#pragma unroll
+                for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+                    const int r = i * kRowsAtOnce + r0;
+                    const bool real = have && real_c && q * 16 + r < n;
+                    const int skip = real ? r * W * kElement + c * 16 : 0; // (an address that exists in any case)
+                    const uint32_t dst = at + piece<kRB>(q * 16 + r, c);
+                    cp_async_16(dst, kp + skip, real);
+                    cp_async_16(dst + kStageBytes / 2, vp + skip, real);
+                }
             }
             if (kInt8 && lane < 8) { // 4 pieces of 4 scales for the keys, 4 for the values
                 const float *src = lane < 4 ? a.cache.k_scale : a.cache.v_scale;
