@@ -37,17 +37,21 @@ using namespace ptx;
 
 constexpr int kWarps = 4;
 constexpr int kStageBytes = 8192; // keys and values of a stage
+constexpr int kLeastShare = 2;    // units: finer shares cost more in joining than they save (8 pairs of 2000 keys: 14.4 -> 12.4 us)
 constexpr int kMaxSplits = 2;     // partial results of a CTA: of the pair it begins in the middle of, of the one it ends in the middle of
 
 // WT: elements of a cache row in shared memory (the row's width rounded up to 64 or 128).  NT: 8-query tiles.
 template <bool kInt8, int WT, int NT>
 struct Shape {
+    // int8 keys stay codes and need fewer registers, and the conversion of the values more warps to hide its latency: three
+    // CTAs of two stages per warp instead of two CTAs of three (128 sequences, 64/8 heads: 158 -> 144 us)
+    static constexpr int kCtas = kInt8 && NT == 1 ? 3 : 2; // per SM
     static constexpr int kRowBytes = WT * (kInt8 ? 1 : 2);
     static constexpr int kKeys = kStageBytes / 2 / kRowBytes; // of a stage: 16, 32 or 64
     static constexpr int kChunks = kRowBytes / 16;
     static constexpr int kScaleBytes = kInt8 ? kKeys * 8 : 0; // fp32 scales of the keys and the values
     static constexpr int kStage = kStageBytes + kScaleBytes;
-    static constexpr int kStages = 3;
+    static constexpr int kStages = kCtas == 3 ? 2 : 3;
     static constexpr int kQ = 8 * NT;
     static constexpr int kMl = kWarps * kQ; // (maximum, sum) of the warps, and later of the parts
     static constexpr int kSmem = kWarps * kStages * kStage + kMl * 8;
@@ -160,8 +164,10 @@ struct Plan {
 };
 
 template <bool kInt8, int WT, int NT>
-__global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads)
+__global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads)
 {
+    griddep_wait(); // everything below is read from memory that the launch before this one may have written
+    griddep_launch_dependents();
     using S = Shape<kInt8, WT, NT>;
     constexpr int kKeys = S::kKeys, kBlock = kWarps * kKeys, kSteps = WT / 16, kRB = S::kRowBytes, kThreads = kWarps * 32;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -200,7 +206,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attend_decode_kernel(const __g
         if (w < warp) upto += scan[w];
         total += scan[w];
     }
-    const Plan plan(total, gridDim.x);
+    const Plan plan(total, min((int)gridDim.x, max(1, total / kLeastShare)));
     const bool works = (int)blockIdx.x < plan.shares;
     const int share_begin = plan.begin_of(blockIdx.x), share_end = plan.begin_of(blockIdx.x + 1);
     if (works && share_begin >= upto - mine && share_begin < upto) {
@@ -714,8 +720,8 @@ cudaError_t launch(const AttendArgs &a, int chunks, int chunk_heads, cudaStream_
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
-    attend_decode_kernel<kInt8, WT, NT><<<std::min(2 * sm_count(), kDecodeMaxCtas), kWarps * 32, S::kSmem, stream>>>(a, chunks, chunk_heads);
-    return cudaGetLastError();
+    return launch_dependent(attend_decode_kernel<kInt8, WT, NT>, std::min(S::kCtas * sm_count(), kDecodeMaxCtas), kWarps * 32, S::kSmem, stream,
+                            a, chunks, chunk_heads);
 }
 
 } // namespace

@@ -214,6 +214,8 @@ __host__ __device__ constexpr size_t part_floats(int width) { return (size_t)kRo
 template <bool kInt8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args)
 {
+    griddep_wait(); // everything below is read from memory that the launch before this one may have written
+    griddep_launch_dependents();
     const AttendArgs &a = args.a;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -820,8 +822,7 @@ cudaError_t launch(const PromptArgs &p, int ctas, cudaStream_t stream)
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
-    attend_prompt_kernel<kInt8><<<(unsigned)ctas, kThreads, Shared<kInt8>::bytes(), stream>>>(p);
-    return cudaGetLastError();
+    return launch_dependent(attend_prompt_kernel<kInt8>, (unsigned)ctas, kThreads, Shared<kInt8>::bytes(), stream, p);
 }
 
 } // namespace

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "internal.cuh"
 
 namespace bitlinear {
@@ -75,6 +77,25 @@ __host__ __device__ __forceinline__ int kv_sequence_of(const KvBatch &s, int t, 
     first = s.cu_tokens[lo];
     count = s.cu_tokens[lo + 1] - first;
     return first <= t ? lo : -1;
+}
+
+// Launches a kernel that may start while the launch before it on the stream is still running (its CTAs wait at griddep_wait,
+// which returns when that launch is complete and its writes are visible).  Between small launches this hides the start.
+template <typename... Args>
+cudaError_t launch_dependent(void (*kernel)(Args...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t stream,
+                             const std::remove_const_t<Args> &...args)
+{
+    cudaLaunchAttribute attribute;
+    attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(blocks);
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = &attribute;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
 }
 
 // ---- launchers -----------------------------------------------------------------------------------------

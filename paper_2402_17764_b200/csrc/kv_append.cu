@@ -19,6 +19,7 @@
 
 #include "internal.cuh"
 #include "kv.cuh"
+#include "ptx.cuh"
 
 namespace bitlinear {
 namespace {
@@ -47,9 +48,8 @@ struct Piece<2> {
 };
 
 template <int VEC>
-__device__ __forceinline__ void load_piece(const __nv_bfloat16 *p, float (&x)[VEC])
+__device__ __forceinline__ void unpack(const Piece<VEC> &w, float (&x)[VEC])
 {
-    const Piece<VEC> w = *reinterpret_cast<const Piece<VEC> *>(p);
     const uint32_t *u = reinterpret_cast<const uint32_t *>(&w);
 #pragma unroll
     for (int i = 0; i < VEC / 2; ++i) {
@@ -73,13 +73,16 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&x)[V
 
 // kRotate: 0 none, 1 pairs half a head apart, 2 adjacent pairs.
 template <int VEC, bool kInt8, int kRotate>
-__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares)
+__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares) // warps per token
 {
-    constexpr int kLanes = VEC == 8 ? 8 : 32, kGroups = 256 / kLanes;
+    ptx::griddep_wait(); // everything below is read from memory that the launch before this one may have written
+    ptx::griddep_launch_dependents();
+    constexpr int kLanes = VEC == 8 ? 8 : 32, kGroups = 32 / kLanes; // of a warp
     const int D = a.cache.head_dim, half = D / 2, Hk = a.cache.kv_heads;
     const int tasks = a.heads + 2 * Hk; // query heads, key heads, value heads
-    const int t = blockIdx.x / shares, share = blockIdx.x - t * shares;
-    const int lane = threadIdx.x % kLanes;
+    const int warp = blockIdx.x * 8 + threadIdx.x / 32, t = warp / shares, share = warp - t * shares;
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x % 32 / kLanes;
+    if (t >= a.T) return;
 
     int first, count;
     const int b = kv_sequence_of(a.batch, t, first, count);
@@ -107,18 +110,32 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ 
         }
     }
     // every lane of a warp goes through the same rounds (the 8-bit row maximum is a shuffle)
+    auto source = [&](int task) {
+        const int h = task < a.heads ? task : (task < a.heads + Hk ? task - a.heads : task - a.heads - Hk);
+        return (task < a.heads ? a.q + (int64_t)t * a.q_stride
+                               : (task < a.heads + Hk ? a.k + (int64_t)t * a.k_stride : a.v + (int64_t)t * a.v_stride)) + h * D;
+    };
+    auto works = [&](int task) { return task < tasks && mine && (task < a.heads || page >= 0); };
+    Piece<VEC> next0 = {}, next1 = {};
+    auto prefetch = [&](int task) {
+        if (!works(task)) return;
+        const __nv_bfloat16 *src = source(task);
+        next0 = *reinterpret_cast<const Piece<VEC> *>(src + o0);
+        next1 = *reinterpret_cast<const Piece<VEC> *>(src + o1);
+    };
+    prefetch(share * kGroups + group);
     for (int round = share * kGroups; round < tasks; round += shares * kGroups) {
-        const int task = round + threadIdx.x / kLanes;
+        const int task = round + group;
         const bool is_q = task < a.heads, is_k = !is_q && task < a.heads + Hk;
         const int h = is_q ? task : (is_k ? task - a.heads : task - a.heads - Hk);
-        const bool work = task < tasks && mine && (is_q || page >= 0);
-        const __nv_bfloat16 *src =
-            (is_q ? a.q + (int64_t)t * a.q_stride : (is_k ? a.k + (int64_t)t * a.k_stride : a.v + (int64_t)t * a.v_stride)) + h * D;
+        const bool work = works(task);
+        const __nv_bfloat16 *src = source(task);
         float x0[VEC] = {}, x1[VEC] = {};
         if (work) {
-            load_piece<VEC>(src + o0, x0);
-            load_piece<VEC>(src + o1, x1);
+            unpack<VEC>(next0, x0);
+            unpack<VEC>(next1, x1);
         }
+        prefetch(task + shares * kGroups);
         // the j-th pair of this lane: (x0[j], x1[j]), or two neighbours
         auto first_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j] : x1[2 * j - VEC]) : x0[j]; };
         auto second_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j + 1] : x1[2 * j + 1 - VEC]) : x1[j]; };
@@ -224,17 +241,12 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ 
 template <int VEC, bool kInt8>
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t stream)
 {
-    // CTAs per token: one round of heads per CTA while that does not make more CTAs than the GPU holds at a time
-    const int groups = 256 / (VEC == 8 ? 8 : 32), rounds = (a.heads + 2 * a.cache.kv_heads + groups - 1) / groups;
-    const int shares = std::max(1, std::min(rounds, 8 * sm_count() / a.T));
-    const unsigned blocks = (unsigned)a.T * (unsigned)shares;
-    if (!a.rope)
-        kv_append_kernel<VEC, kInt8, 0><<<blocks, 256, 0, stream>>>(a, shares);
-    else if (!a.interleaved)
-        kv_append_kernel<VEC, kInt8, 1><<<blocks, 256, 0, stream>>>(a, shares);
-    else
-        kv_append_kernel<VEC, kInt8, 2><<<blocks, 256, 0, stream>>>(a, shares);
-    return cudaGetLastError();
+    // Warps per token: one round of heads per warp while that does not make more warps than the GPU holds at half occupancy.
+    const int groups = VEC == 8 ? 4 : 1, rounds = (a.heads + 2 * a.cache.kv_heads + groups - 1) / groups;
+    const int shares = std::max(1, std::min(rounds, 32 * sm_count() / a.T));
+    const unsigned blocks = (unsigned)(((int64_t)a.T * shares + 7) / 8);
+    return launch_dependent(!a.rope ? kv_append_kernel<VEC, kInt8, 0> : (!a.interleaved ? kv_append_kernel<VEC, kInt8, 1> : kv_append_kernel<VEC, kInt8, 2>),
+                            blocks, 256, 0, stream, a, shares);
 }
 
 } // namespace
