@@ -73,7 +73,7 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&x)[V
 
 // kRotate: 0 none, 1 pairs half a head apart, 2 adjacent pairs.
 template <int VEC, bool kInt8, int kRotate>
-__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares) // warps per token
+__global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares) // warps per token
 {
     ptx::griddep_wait(); // everything below is read from memory that the launch before this one may have written
     ptx::griddep_launch_dependents();
@@ -241,9 +241,9 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ 
 template <int VEC, bool kInt8>
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t stream)
 {
-    // Warps per token: one round of heads per warp while that does not make more warps than the GPU holds at half occupancy.
+    // Warps per token: one round of heads per warp while that does not make more warps than the GPU holds.
     const int groups = VEC == 8 ? 4 : 1, rounds = (a.heads + 2 * a.cache.kv_heads + groups - 1) / groups;
-    const int shares = std::max(1, std::min(rounds, 32 * sm_count() / a.T));
+    const int shares = std::max(1, std::min(rounds, 64 * sm_count() / a.T));
     const unsigned blocks = (unsigned)(((int64_t)a.T * shares + 7) / 8);
     return launch_dependent(!a.rope ? kv_append_kernel<VEC, kInt8, 0> : (!a.interleaved ? kv_append_kernel<VEC, kInt8, 1> : kv_append_kernel<VEC, kInt8, 2>),
                             blocks, 256, 0, stream, a, shares);
