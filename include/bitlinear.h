@@ -325,7 +325,8 @@ void bitlinear_sequence_destroy(bitlinear_sequence *seq);
  *   n_pages * kv_heads * page_size < 2^31
  * `status` (device, one int32, set to 0 by the owner) receives BITLINEAR_ERR_PAGE when a call met a page number outside
  * 0 .. n_pages - 1, a length beyond table_pages * page_size, or a position beyond the rotary table: nothing is read or
- * written there (what that does to the results is said at each call), and the word keeps the code until the owner clears it.
+ * written there (what that does to the results is said at each call).  BITLINEAR_ERR_TIMEOUT: a bounded wait of
+ * bitlinear_attend_prompt expired, its results are unspecified.  The word keeps the code until the owner clears it.
  */
 typedef struct {
     void *k, *v;             /* device, bitlinear_kv_cache_bytes(...) bytes each, 16-byte aligned */
@@ -396,9 +397,11 @@ size_t bitlinear_attend_workspace_bytes(int heads, int kv_heads, int head_dim, i
  *   workspace  >= bitlinear_attend_workspace_bytes(...), 256-byte aligned, filled with zeros by the caller once before its
  *              first use; every call leaves it fit for the next.  Two calls that may run at the same time must not
  *              share a workspace.
- * Sums, maxima and the softmax's denominators are fp32; weights are rounded to bf16 before they meet the values in the
- * prompt kernel.  A token that sees nothing (an empty slot) gets zeros.  Keys on a bad page, or behind the page table, take
- * no part and the status is set.  Calls with the same arguments on the same contents give the same bits.
+ * Sums, maxima and the softmax's denominators are fp32.  Roundings to fewer bits: the prompt kernel rounds the weights to
+ * bf16 before they meet the values; the decode kernel splits them into two bf16 parts (16 bits) and, over an 8-bit cache, takes
+ * the queries to integers of 22 bits relative to the row's largest element; the results are rounded to bf16.  A token that
+ * sees nothing (an empty slot) gets zeros.  Keys on a bad page, or behind the page table, take no part and the status is
+ * set.  Calls with the same arguments on the same contents give the same bits.
  */
 bitlinear_status bitlinear_attend_decode(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q,
                                          int64_t q_stride, int heads, float softmax_scale, void *out, int64_t out_stride,
@@ -441,10 +444,10 @@ bitlinear_status bitlinear_validate_packed(const void *packed, int64_t N, int64_
 bitlinear_status bitlinear_probe_int8_peak(int iters, int32_t *status, int64_t *int_ops, void *stream);
 
 /*
- * Test hook for the bounded waits (no counterpart in the paper).  Every device-side wait of the matmul kernels gives
- * up after a limit (2 s), sets the workspace's status word to BITLINEAR_ERR_TIMEOUT and lets the kernel return.  This
- * call arms the NEXT matmul launch of the process (one launch only; the quantiser launch in front of it does not
- * count): its waits give up after limit_us microseconds (0: the default), and, if skip_arrive is non-zero, one
+ * Test hook for the bounded waits (no counterpart in the paper).  Every device-side wait of the matmul kernels and of the
+ * prompt attention gives up after a limit (2 s), sets the workspace's (attention: the cache's) status word to
+ * BITLINEAR_ERR_TIMEOUT and lets the kernel return.  This call arms the NEXT launch of one of them in the process (one
+ * launch only; the quantiser launch in front of a matmul does not count): its waits give up after limit_us microseconds (0: the default), and, if skip_arrive is non-zero, one
  * producer thread of its first CTA leaves out one barrier arrival (and the copy it announces), so that a wait really
  * runs out.  The launch then
  * ends with BITLINEAR_ERR_TIMEOUT in the status word and unspecified outputs; the workspace is usable again at once.

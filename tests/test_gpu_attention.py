@@ -241,15 +241,17 @@ def test_a_page_shared_by_two_sequences(prompt):
 
 @pytest.mark.parametrize("poison", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("where", ["key", "value"])
-def test_a_poisoned_row_reaches_only_the_tokens_that_see_it(where, poison):
-    """Position 99 of a prompt whose new tokens are positions 50 .. 199: tokens 0 .. 48 lie in front of it."""
-    s = R.Setup([200, 200], 1, 64, 16, 16, seed=15)
-    new = [150, 150]
+@pytest.mark.parametrize("past", [50, 2850])
+def test_a_poisoned_row_reaches_only_the_tokens_that_see_it(where, poison, past):
+    """The 50th of 150 new tokens is poisoned: the 49 in front of it do not see it.  With the longer past several CTAs share
+    the keys of a tile of rows."""
+    lens, new, at = [past + 150, past + 150], [150, 150], past + 49
+    s = R.Setup(lens, 1, 64, 16, 16, seed=15)
     clean = [p.clone() for p in s.pools]
     q = rows(300, 2, 64, 3)
     cu = torch.tensor([0, 150, 300], dtype=torch.int32, device="cuda")
     want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16)
-    s.pools[0 if where == "key" else 1][s.table[0, 6].item(), 0, 3, 5] = poison
+    s.pools[0 if where == "key" else 1][s.table[0, at // 16].item(), 0, at % 16, 5] = poison
     got = B.attend_prompt(s.cache(), B.KVBatch(s.table, s.kv_lens, cu), q)
     free = list(range(49)) + list(range(150, 300))
     check(got[free], want[free], bound[free])
@@ -260,15 +262,151 @@ def test_a_poisoned_row_reaches_only_the_tokens_that_see_it(where, poison):
     elif poison != poison:
         assert torch.all(got[49:150].isnan())
     # single tokens: in front of the poisoned position and behind it
-    s.kv_lens.copy_(torch.tensor([99, 100], dtype=torch.int32))
+    s.kv_lens.copy_(torch.tensor([at, at + 1], dtype=torch.int32))
     s.table[1] = s.table[0]
-    s.lens = [99, 99]
+    s.lens = [at, at]
     got = B.attend_decode(s.cache(), B.KVBatch(s.table, s.kv_lens), q[:2])
-    poisoned, s.pools = s.pools, clean
+    s.pools = clean
     want, bound = R.attend(s, q[:2], [1, 1], **decode_error(s.bits))
     check(got[0], want[0], bound[0])
     if where == "value" or poison != poison:
         assert not torch.any(torch.isfinite(got[1, :, 5]))
+
+
+@pytest.mark.parametrize("where", ["key", "value"])
+@pytest.mark.parametrize("past", [50, 2850])
+def test_an_int8_row_that_is_not_finite_reaches_only_the_tokens_that_see_it(where, past):
+    """Such a row has codes 0 and a scale of NaN."""
+    lens, new, at = [past + 150, past + 150], [150, 150], past + 49
+    s = R.Setup(lens, 1, 64, 16, 8, seed=18)
+    q = rows(300, 2, 64, 3)
+    cu = torch.tensor([0, 150, 300], dtype=torch.int32, device="cuda")
+    want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16)
+    which, page = 0 if where == "key" else 1, s.table[0, at // 16].item()
+    s.pools[which][page, 0, at % 16] = 0
+    s.scales[which][page, 0, at % 16] = float("nan")
+    got = B.attend_prompt(s.cache(), B.KVBatch(s.table, s.kv_lens, cu), q)
+    free = list(range(49)) + list(range(150, 300))
+    check(got[free], want[free], bound[free])
+    assert torch.all(got[49:150].isnan())
+    s.kv_lens.copy_(torch.tensor([at, at + 1], dtype=torch.int32))
+    s.table[1] = s.table[0]
+    got = B.attend_decode(s.cache(), B.KVBatch(s.table, s.kv_lens), q[:2])
+    s.lens = [at, at]
+    want, bound = R.attend(s, q[:1], [1, 0], **decode_error(s.bits))
+    check(got[:1], want, bound)
+    assert torch.all(got[1].isnan())
+
+
+@pytest.mark.parametrize("prompt", [False, True])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_queries_of_any_size(prompt, bits):
+    """Rows of zeros, of subnormal, tiny and huge elements, and of elements 30 binary orders apart; a NaN and an infinity stay in
+    their own row and head."""
+    lens, new = [100] * 8, [1] * 8
+    s = R.Setup(lens, 2, 64, 16, bits, seed=19)
+    q = rows(8, 4, 64, 5)
+    q[0] = 0.0
+    q[1] *= 1e-39
+    q[2] *= 1e-30
+    q[3] *= 1e4
+    q[4, :, ::2] *= 2.0 ** -30
+    cu = torch.arange(9, dtype=torch.int32, device="cuda")
+    attend = B.attend_prompt if prompt else B.attend_decode
+    batch = B.KVBatch(s.table, s.kv_lens, cu if prompt else None)
+    got = attend(s.cache(), batch, q)
+    want, bound = R.attend(s, q, new, **error_of(prompt, bits))
+    check(got, want, bound)
+    sick = q.clone()
+    sick[5, 1, 7] = float("nan")
+    sick[6, 2, 9] = float("inf")
+    got = attend(s.cache(), batch, sick)
+    well = torch.ones(8, 4, dtype=torch.bool, device="cuda")
+    well[5, 1] = well[6, 2] = False
+    check(got[well], want[well], bound[well])
+    assert torch.all(got[5, 1].isnan()) and not torch.any(torch.isfinite(got[6, 2]))
+
+
+def test_prompts_of_more_sequences_than_are_put_in_order():
+    g = torch.Generator().manual_seed(2)
+    new = torch.randint(0, 6, (700,), generator=g).tolist()
+    lens = [n + p for n, p in zip(new, torch.randint(0, 60, (700,), generator=g).tolist())]
+    s = R.Setup(lens, 1, 16, 16, 16, seed=20)
+    q = rows(sum(new), 2, 16, 5)
+    cu = torch.tensor([sum(new[:i]) for i in range(701)], dtype=torch.int32, device="cuda")
+    got = B.attend_prompt(s.cache(), B.KVBatch(s.table, s.kv_lens, cu), q)
+    want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16)
+    check(got, want, bound)
+
+
+def test_one_workspace_serves_both_kernels_in_turn():
+    s = R.Setup([3000, 200], 2, 128, 16, 16, seed=23)
+    ws = torch.zeros(max(B.attend_workspace_bytes(8, 2, 128, p) for p in (False, True)), dtype=torch.uint8, device="cuda")
+    cu = torch.tensor([0, 20, 30], dtype=torch.int32, device="cuda")
+    q, single = rows(30, 8, 128, 1), rows(2, 8, 128, 2)
+    for _ in range(3):
+        got = B.attend_prompt(s.cache(), B.KVBatch(s.table, s.kv_lens, cu), q, workspace=ws)
+        want, bound = R.attend(s, q, [20, 10], weight_rounding=WEIGHT_BF16)
+        check(got, want, bound)
+        got = B.attend_decode(s.cache(), B.KVBatch(s.table, s.kv_lens), single, workspace=ws)
+        want, bound = R.attend(s, single, [1, 1], **decode_error(16))
+        check(got, want, bound)
+
+
+def test_a_cache_beyond_32_bit_offsets():
+    """Pages at the end of a pool of more than 2^32 bytes: appended to, and read by both kernels."""
+    pages, page_size, kv_heads, D = 33000, 64, 8, 128
+    shape = (pages, kv_heads, page_size, D)
+    if torch.cuda.mem_get_info()[0] < 14 << 30:
+        pytest.skip("not enough free memory")
+    k, v = (torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert k.numel() * 2 > 1 << 32
+    s = R.Setup([130], kv_heads, D, page_size, 16, seed=24, spare=0, table_extra=0)
+    small = s.pools
+    s.table = torch.tensor([[pages - 1, 32800, pages - 2]], dtype=torch.int32, device="cuda")
+    s.pools = [k, v]
+    n = 130
+    new_k, new_v = rows(n, kv_heads, D, 1, size=1.0), rows(n, kv_heads, D, 2, size=1.0)
+    cache, cu = s.cache(), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    B.kv_append(cache, B.KVBatch(s.table, s.kv_lens, cu), new_k, new_v)
+    assert torch.equal(k[pages - 1, :, 0], new_k[0]) and torch.equal(v[32800, :, 63], new_v[127])
+    q = rows(n, 16, D, 3)
+    got = B.attend_prompt(cache, B.KVBatch(s.table, s.kv_lens, cu), q)
+    want, bound = R.attend(s, q, [n], weight_rounding=WEIGHT_BF16)
+    check(got, want, bound)
+    got = B.attend_decode(cache, B.KVBatch(s.table, s.kv_lens), q[:1])
+    want, bound = R.attend(s, q[:1], [1], **decode_error(16))
+    check(got, want, bound)
+    cache.check()
+    del k, v, small
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_an_expired_wait_of_the_prompt_kernel_ends_it_with_a_status(bits):
+    """One CTA, whose first copy and its announcement are left out, with a limit of 2 ms: the call returns, the cache's
+    status says so, and the next call on the same workspace is right."""
+    s = R.Setup([200], 1, 64, 16, bits, seed=25)
+    q = rows(60, 2, 64, 1)
+    cu = torch.tensor([0, 60], dtype=torch.int32, device="cuda")
+    cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens, cu)
+    ws, out = B.alloc_attend_workspace(2, 1, 64, prompt=True), torch.empty(60, 2, 64, dtype=torch.bfloat16, device="cuda")
+    want, bound = R.attend(s, q, [60], weight_rounding=WEIGHT_BF16)
+    B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+    check(out, want, bound)
+    B.test_expire_next_wait(2000, True)
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+    end.record()
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_TIMEOUT
+    assert 1.5 < start.elapsed_time(end) < 500.0
+    for _ in range(2):
+        out.fill_(0.5)
+        B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+        cache.check()
+        check(out, want, bound)
 
 
 @pytest.mark.parametrize("prompt", [False, True])
