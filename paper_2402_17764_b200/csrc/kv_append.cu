@@ -71,6 +71,12 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&x)[V
     *reinterpret_cast<Piece<VEC> *>(p) = w;
 }
 
+// Heads that a group of lanes takes at a time.  With 4-byte pieces four heads' loads have to be in flight to hide the
+// memory's latency (4096 tokens, 32/32 heads of 100: one at a time 74 us, two or four 57, eight 66); with 16-byte pieces the
+// registers are worth more as warps (64/8 heads of 128: one 32 us, two 38).  An 8-bit row works on more values: one.
+template <int VEC, bool kInt8>
+constexpr int kHeadsAtATime = VEC == 2 && !kInt8 ? 4 : 1;
+
 // kRotate: 0 none, 1 pairs half a head apart, 2 adjacent pairs.
 template <int VEC, bool kInt8, int kRotate>
 __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares) // warps per token
@@ -78,6 +84,7 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
     ptx::griddep_wait(); // everything below is read from memory that the launch before this one may have written
     ptx::griddep_launch_dependents();
     constexpr int kLanes = VEC == 8 ? 8 : 32, kGroups = 32 / kLanes; // of a warp
+    constexpr int kBatch = kHeadsAtATime<VEC, kInt8>;
     const int D = a.cache.head_dim, half = D / 2, Hk = a.cache.kv_heads;
     const int tasks = a.heads + 2 * Hk; // query heads, key heads, value heads
     const int warp = blockIdx.x * 8 + threadIdx.x / 32, t = warp / shares, share = warp - t * shares;
@@ -116,26 +123,27 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
                                : (task < a.heads + Hk ? a.k + (int64_t)t * a.k_stride : a.v + (int64_t)t * a.v_stride)) + h * D;
     };
     auto works = [&](int task) { return task < tasks && mine && (task < a.heads || page >= 0); };
-    Piece<VEC> next0 = {}, next1 = {};
-    auto prefetch = [&](int task) {
-        if (!works(task)) return;
-        const __nv_bfloat16 *src = source(task);
-        next0 = *reinterpret_cast<const Piece<VEC> *>(src + o0);
-        next1 = *reinterpret_cast<const Piece<VEC> *>(src + o1);
+    Piece<VEC> next0[kBatch] = {}, next1[kBatch] = {};
+    auto prefetch = [&](int first_task) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int task = first_task + u * kGroups;
+            if (!works(task)) continue;
+            const __nv_bfloat16 *src = source(task);
+            next0[u] = *reinterpret_cast<const Piece<VEC> *>(src + o0);
+            next1[u] = *reinterpret_cast<const Piece<VEC> *>(src + o1);
+        }
     };
-    prefetch(share * kGroups + group);
-    for (int round = share * kGroups; round < tasks; round += shares * kGroups) {
-        const int task = round + group;
+    auto serve = [&](const int task, const Piece<VEC> &now0, const Piece<VEC> &now1) {
         const bool is_q = task < a.heads, is_k = !is_q && task < a.heads + Hk;
         const int h = is_q ? task : (is_k ? task - a.heads : task - a.heads - Hk);
         const bool work = works(task);
         const __nv_bfloat16 *src = source(task);
         float x0[VEC] = {}, x1[VEC] = {};
         if (work) {
-            unpack<VEC>(next0, x0);
-            unpack<VEC>(next1, x1);
+            unpack<VEC>(now0, x0);
+            unpack<VEC>(now1, x1);
         }
-        prefetch(task + shares * kGroups);
         // the j-th pair of this lane: (x0[j], x1[j]), or two neighbours
         auto first_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j] : x1[2 * j - VEC]) : x0[j]; };
         auto second_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j + 1] : x1[2 * j + 1 - VEC]) : x1[j]; };
@@ -201,7 +209,7 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
 #pragma unroll
                 for (int d = 1; d < kLanes; d <<= 1) beta = fmax(beta, __shfl_xor_sync(0xFFFFFFFFu, beta, d));
             }
-            if (is_q || task >= tasks || page < 0) continue;
+            if (is_q || task >= tasks || page < 0) return;
             beta = fmax(beta, 1e-5);
             int8_t *dst = reinterpret_cast<int8_t *>(is_k ? a.cache.k : a.cache.v) + row * a.cache.width;
             if (mine) {
@@ -235,6 +243,20 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
             if (VEC == 2 && lane < a.cache.width - D) dst[D + lane] = 0;
             if (lane == 0) (is_k ? a.cache.k_scale : a.cache.v_scale)[row] = finite ? (float)(beta / 127.0) : __int_as_float(0x7FFFFFFF);
         }
+    };
+
+    const int step = shares * kGroups * kBatch;
+    prefetch(share * kGroups * kBatch + group);
+    for (int round = share * kGroups * kBatch; round < tasks; round += step) {
+        Piece<VEC> now0[kBatch], now1[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            now0[u] = next0[u];
+            now1[u] = next1[u];
+        }
+        prefetch(round + step + group);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) serve(round + u * kGroups + group, now0[u], now1[u]);
     }
 }
 
@@ -242,7 +264,7 @@ template <int VEC, bool kInt8>
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t stream)
 {
     // Warps per token: one round of heads per warp while that does not make more warps than the GPU holds.
-    const int groups = VEC == 8 ? 4 : 1, rounds = (a.heads + 2 * a.cache.kv_heads + groups - 1) / groups;
+    const int groups = (VEC == 8 ? 4 : 1) * kHeadsAtATime<VEC, kInt8>, rounds = (a.heads + 2 * a.cache.kv_heads + groups - 1) / groups;
     const int shares = std::max(1, std::min(rounds, 64 * sm_count() / a.T));
     const unsigned blocks = (unsigned)(((int64_t)a.T * shares + 7) / 8);
     return launch_dependent(!a.rope ? kv_append_kernel<VEC, kInt8, 0> : (!a.interleaved ? kv_append_kernel<VEC, kInt8, 1> : kv_append_kernel<VEC, kInt8, 2>),
