@@ -594,12 +594,15 @@ class KVBatch:
 
 def rope_table(n_pos: int, head_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
     """bitlinear_rope_table: -> fp32 [n_pos, head_dim / 2, 2], (cos, sin) of every position and pair."""
+    if stream is not None:
+        with _allocating_on(stream, device):
+            return rope_table(n_pos, head_dim, base, device)
     table = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=device)
     if torch.cuda.current_device() != table.device.index:
         with torch.cuda.device(table.device):
-            st = load_library().bitlinear_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(stream))
+            st = load_library().bitlinear_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(None))
     else:
-        st = load_library().bitlinear_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(stream))
+        st = load_library().bitlinear_rope_table(_ptr(table), n_pos, head_dim, float(base), _stream(None))
     _check(st, "bitlinear_rope_table")
     return table
 
@@ -619,6 +622,12 @@ def _empty_rows(rows: int, heads: int, head_dim: int, device) -> torch.Tensor:
     n = heads * head_dim
     t = torch.empty((rows, (n + 7) // 8 * 8), dtype=torch.bfloat16, device=device)
     return t.as_strided((rows, heads, head_dim), (t.shape[1], head_dim, 1))
+
+
+def _allocating_on(stream, device):
+    """Context in which `stream` is the current one: what a call allocates (and fills) for itself has to belong to the stream
+    that uses it, or it is not filled in time and may be handed out again too early."""
+    return torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device))
 
 
 def _launch_device(cache: KVCache, batch: KVBatch, where: str) -> int:
@@ -642,6 +651,9 @@ def kv_append(cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, 
     if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return kv_append(cache, batch, k, v, q, rope, interleaved, q_out, stream)
+    if stream is not None and q is not None and q_out is None:
+        with _allocating_on(stream, cache.device):
+            return kv_append(cache, batch, k, v, q, rope, interleaved)
     T, D = k.shape[0], cache.head_dim
     ks = _row_stride(k, cache.kv_heads, D, T, index, where)
     vs = _row_stride(v, cache.kv_heads, D, T, index, where)
@@ -685,6 +697,9 @@ def _attend(prompt: bool, cache: KVCache, batch: KVBatch, q, scale, out, workspa
     if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return _attend(prompt, cache, batch, q, scale, out, workspace, stream)
+    if stream is not None and (out is None or workspace is None):
+        with _allocating_on(stream, cache.device):
+            return _attend(prompt, cache, batch, q, scale, out, workspace, None)
     if q.dim() != 3:
         _refuse(where, "q is [tokens, heads, head_dim]", ERR_SHAPE)
     T, heads, _ = q.shape

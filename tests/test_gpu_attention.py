@@ -462,6 +462,32 @@ def test_two_streams_with_workspaces_of_their_own(prompt):
         check(out, want, bound)
 
 
+@pytest.mark.parametrize("prompt", [False, True])
+def test_what_a_call_allocates_belongs_to_its_stream(prompt):
+    # the current stream is busy, and its free memory holds ones: a workspace that it filled would not be zero in time
+    new = [1, 1] if not prompt else [100, 33]
+    attend = B.attend_prompt if prompt else B.attend_decode
+    cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device="cuda")
+    s = R.Setup([4000, 600], 2, 128, 16, 16, seed=31)
+    cache, batch, q = s.cache(), B.KVBatch(s.table, s.kv_lens, cu if prompt else None), rows(sum(new), 8, 128, 31)
+    stale = torch.full((B.attend_workspace_bytes(8, 2, 128, prompt),), 255, dtype=torch.uint8, device="cuda")
+    side, by_number = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    del stale
+    torch.cuda._sleep(100_000_000)
+    outs = []
+    for stream in (side, by_number.cuda_stream):
+        q_rotated = B.kv_append(s.cache(), B.KVBatch(s.table[:0], s.kv_lens[:0]), q[:0, :2], q[:0, :2], q=q[:0], stream=stream)
+        assert q_rotated.shape == (0, 8, 128)
+        table = B.rope_table(64, 128, stream=stream)
+        outs.append((attend(cache, batch, q, stream=stream), table))
+    torch.cuda.synchronize()
+    want, bound = R.attend(s, q, new, **error_of(prompt, s.bits))
+    for out, table in outs:
+        check(out, want, bound)
+        assert torch.equal(table, B.rope_table(64, 128))
+
+
 def test_nothing_to_attend():
     s = R.Setup([4], 2, 64, 16, 16)
     none = torch.empty(0, 4, 64, dtype=torch.bfloat16, device="cuda")
