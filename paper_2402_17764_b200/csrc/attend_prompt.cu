@@ -188,21 +188,39 @@ __device__ void attend_row(const AttendArgs &a, const Work &w, int r, int lane)
     float m = -INFINITY, l = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const int end = w.sees(r);
-    for (int j = 0; j < end; ++j) {
+    constexpr int kAtATime = 4; // keys (a page holds 16 or more)
+    for (int j = 0; j < end; j += kAtATime) {
         const int page = kv_page(a.cache, a.batch, w.b, j);
         if (page < 0) continue;
         const int64_t row = (int64_t)kv_row(a.cache, page, w.head, j) * a.cache.width;
-        const float4 k = load(reinterpret_cast<const __nv_bfloat16 *>(a.cache.k) + row);
-        const float4 v = load(reinterpret_cast<const __nv_bfloat16 *>(a.cache.v) + row);
-        float s = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
+        const __nv_bfloat16 *kp = reinterpret_cast<const __nv_bfloat16 *>(a.cache.k) + row, *vp = reinterpret_cast<const __nv_bfloat16 *>(a.cache.v) + row;
+        float4 k[kAtATime], v[kAtATime];
+        float s[kAtATime];
 #pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-        s *= a.scale;
-        const float mn = fmaxf(m, s);
-        const float base = mn == -INFINITY ? 0.0f : mn;
-        const float keep = exp2_approx(m - base), p = exp2_approx(s - base);
-        l = l * keep + p;
-        o = make_float4(o.x * keep + p * v.x, o.y * keep + p * v.y, o.z * keep + p * v.z, o.w * keep + p * v.w);
+        for (int i = 0; i < kAtATime; ++i) {
+            const int at = j + i < end ? i * a.cache.width : 0;
+            k[i] = load(kp + at);
+            v[i] = load(vp + at);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtATime; ++i) {
+            s[i] = q.x * k[i].x + q.y * k[i].y + q.z * k[i].z + q.w * k[i].w;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], d);
+            s[i] = j + i < end ? s[i] * a.scale : -INFINITY;
+        }
+        float mn = m;
+#pragma unroll
+        for (int i = 0; i < kAtATime; ++i) mn = fmaxf(mn, s[i]);
+        const float base = mn == -INFINITY ? 0.0f : mn, keep = exp2_approx(m - base);
+        l *= keep;
+        o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+#pragma unroll
+        for (int i = 0; i < kAtATime; ++i) {
+            const float p = exp2_approx(s[i] - base);
+            l += p;
+            if (j + i < end) o = make_float4(o.x + p * v[i].x, o.y + p * v[i].y, o.z + p * v[i].z, o.w + p * v[i].w);
+        }
         m = mn;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -218,7 +236,7 @@ template <bool kInt8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args)
 {
     griddep_wait(); // everything below is read from memory that the launch before this one may have written
-    griddep_launch_dependents();
+    if (kInt8) griddep_launch_dependents();
     const AttendArgs &a = args.a;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -774,6 +792,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         }
         if (!kInt8) {
             named_barrier(1, kRows);
+            // The next launch may start, unless rows have to be done again: that takes long when they see many keys, and the
+            // waits of a matmul that were resident meanwhile would run out.
+            if (tid == 0 && !((parts == 1 || sh.is_last) && (sh.poisoned[0] || sh.poisoned[1]))) griddep_launch_dependents();
             if (parts == 1 || sh.is_last) {
                 if (sh.poisoned[t])
                     for (int i = warp % 4; i < kTile; i += 4)
