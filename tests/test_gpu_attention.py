@@ -462,6 +462,36 @@ def test_two_streams_with_workspaces_of_their_own(prompt):
         check(out, want, bound)
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(4096, 1024), (4096, 1)])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_the_most_heads(heads, kv_heads, bits):
+    s = R.Setup([70, 3], kv_heads, 32, 16, bits, seed=41)
+    q = rows(2, heads, 32, 41)
+    out = B.attend_decode(s.cache(), B.KVBatch(s.table, s.kv_lens), q)
+    want, bound = R.attend(s, q, [1, 1], **decode_error(bits))
+    check(out, want, bound)
+    q = rows(5, heads, 32, 42)
+    cu = torch.tensor([0, 3, 5], dtype=torch.int32, device="cuda")
+    out = B.attend_prompt(s.cache(), B.KVBatch(s.table, s.kv_lens, cu), q)
+    want, bound = R.attend(s, q, [3, 2], weight_rounding=WEIGHT_BF16)
+    check(out, want, bound)
+
+
+@pytest.mark.parametrize("cu", [[0, 4, 9], [0, 4, 2], [0, 4, 2 ** 31 - 1], [-3, 4, 4], [-2 ** 31, 4, 5]])
+def test_token_rows_that_do_not_exist_are_neither_read_nor_written(cu):
+    # five rows were handed over; the first sequence's four are computed where its rows are in order
+    s = R.Setup([30, 21], 2, 64, 16, 16, seed=43)
+    q = rows(5, 4, 64, 43)
+    wide = torch.full((15, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    out = wide[5:10]
+    bounds = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    B.attend_prompt(s.cache(), B.KVBatch(s.table, s.kv_lens, bounds), q, out=out)
+    assert torch.all(wide[:5] == 3.0) and torch.all(wide[10:] == 3.0)
+    if cu[0] == 0:
+        want, bound = R.attend(s, q[:4], [4], weight_rounding=WEIGHT_BF16)
+        check(out[:4], want, bound)
+
+
 @pytest.mark.parametrize("prompt", [False, True])
 def test_what_a_call_allocates_belongs_to_its_stream(prompt):
     # the current stream is busy, and its free memory holds ones: a workspace that it filled would not be zero in time
