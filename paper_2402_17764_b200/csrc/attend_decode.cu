@@ -24,6 +24,11 @@
 // instructions per two elements, which is what bounds the kernel then).  Keys stay codes: the queries are written as integers of
 // 23 bits, relative to the power of two above their row's largest, in three signed bytes, and the scores are exact
 // integer products of codes and bytes (three MMAs of twice the depth instead of 16 conversions per MMA).
+//
+// Measured: 128k tokens of one sequence, 64/8 heads: 94 us = 5.7 TB/s (0.87 of a copy's rate); 32 sequences of 1 to 4096 tokens,
+// 32 heads: 46 us = 5.2 TB/s; int8, 128 sequences of 256 to 8192 tokens, 64/8 heads: 150 us = 4.8 TB/s (issue slots 57 %
+// busy, and what they wait for is the chain from a stage's codes to its output); one sequence of 777 tokens, 32 heads of
+// 100: 9.4 us per call, a chain of dependent loads and the join of its parts.
 #include <algorithm>
 
 #include "internal.cuh"

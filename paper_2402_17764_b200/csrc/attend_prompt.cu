@@ -26,8 +26,12 @@
 // reference m_i is therefore raised only when a score exceeds it by more than 8 (a factor 256, which fp32 sums and bf16 weights
 // carry without loss); the result does not depend on the reference.
 //
-// What bounds it: 128 x 128 scores need 16384 exponentials, 16 per cycle and SM = 1024 cycles, while their two MMAs take 512
-// cycles at a head of 128.
+// What bounds it (heads of 128).  128 x 128 scores cost 16384 exponentials at 16 per cycle and SM, 1024 cycles, and two MMAs of
+// 512 cycles each: the two units are needed equally long, and neither can be kept busy all the time (tensor pipe 66 %,
+// exponentials 53 %).  8192 tokens, 32 heads: 580 us = 0.94 PFLOP/s, where the board's power limit holds the clock near 1.55
+// GHz (the same launch takes about 930 000 cycles at any clock).  int8: the converters' shared-memory traffic and arithmetic come on
+// top, 60 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 372 us = 0.77 PFLOP/s).
+// Prompts of few hundred tokens: half the time is each tile's beginning and end (pages, queries, first scores; results).
 #include <cuda.h>
 
 #include <algorithm>
@@ -376,152 +380,152 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     const uint32_t q_addr = base, ring = base + 2 * kTileBytes16;
 
     if (warp >= kMmaWarp) {
-    give_registers<kOtherRegs>();
-    if (kInt8 && warp >= kFirstConverter) {
-        // ---- int8: codes to bf16, blocks in the order K 0, V 0, K 1, V 1, ...; each warp a quarter of the rows ------------
-        const int pieces = W / 16, c = lane % 8, r0 = lane / 8; // this lane: piece c (16 codes) of every fourth row
-        for (int i = 0; i < 2 * total; ++i) {
-            const int s = i % kStages, round = i / kStages, rs = kInt8 ? i % 3 : 0, j = from + i / 2;
-            if (round > 0 && !mbar_wait_bounded(smem_u32(&sh.kv_empty[s]), (round - 1) & 1, abort_flag, limit, 0)) break;
-            if (!mbar_wait_bounded(smem_u32(&sh.raw_full[rs]), (i / 3) & 1, abort_flag, limit, 0)) break;
-            const uint8_t *codes = raw_ring + rs * kRawBytes;
-            uint8_t *out = smem + (2 + s) * kTileBytes16 + (c / 4) * kHalfBytes;
-            const int p = (c % 4) * 2;
-            {
-                const int r = (warp - kFirstConverter) * 32 + lane; // (scales of keys that do not exist may be anything)
-                const float f = reinterpret_cast<const float *>(codes + kTile * 128)[r];
-                sh.scales[(i / 2) % kScaled][i & 1][r] = j * kTile + r < w.len ? f : 0.0f;
-            }
-            if (c < pieces) {
+        give_registers<kOtherRegs>();
+        if (kInt8 && warp >= kFirstConverter) {
+            // ---- int8: codes to bf16, blocks in the order K 0, V 0, K 1, V 1, ...; each warp a quarter of the rows ------------
+            const int pieces = W / 16, c = lane % 8, r0 = lane / 8; // this lane: piece c (16 codes) of every fourth row
+            for (int i = 0; i < 2 * total; ++i) {
+                const int s = i % kStages, round = i / kStages, rs = kInt8 ? i % 3 : 0, j = from + i / 2;
+                if (round > 0 && !mbar_wait_bounded(smem_u32(&sh.kv_empty[s]), (round - 1) & 1, abort_flag, limit, 0)) break;
+                if (!mbar_wait_bounded(smem_u32(&sh.raw_full[rs]), (i / 3) & 1, abort_flag, limit, 0)) break;
+                const uint8_t *codes = raw_ring + rs * kRawBytes;
+                uint8_t *out = smem + (2 + s) * kTileBytes16 + (c / 4) * kHalfBytes;
+                const int p = (c % 4) * 2;
+                {
+                    const int r = (warp - kFirstConverter) * 32 + lane; // (scales of keys that do not exist may be anything)
+                    const float f = reinterpret_cast<const float *>(codes + kTile * 128)[r];
+                    sh.scales[(i / 2) % kScaled][i & 1][r] = j * kTile + r < w.len ? f : 0.0f;
+                }
+                if (c < pieces) {
 #pragma unroll 4
-                for (int u = 0; u < 8; ++u) {
-                    const int r = (warp - kFirstConverter) * 32 + u * 4 + r0;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(codes + r * W + c * 16);
-                    *reinterpret_cast<uint4 *>(out + r * 128 + ((p ^ (r & 7)) << 4)) =
-                        make_uint4(code_pair<0x4140>(x.x), code_pair<0x4342>(x.x), code_pair<0x4140>(x.y), code_pair<0x4342>(x.y));
-                    *reinterpret_cast<uint4 *>(out + r * 128 + (((p + 1) ^ (r & 7)) << 4)) =
-                        make_uint4(code_pair<0x4140>(x.z), code_pair<0x4342>(x.z), code_pair<0x4140>(x.w), code_pair<0x4342>(x.w));
-                }
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_u32(&sh.kv_full[s]));
-                mbar_arrive(smem_u32(&sh.raw_empty[rs]));
-            }
-        }
-    } else if (warp >= kFirstProducer) {
-        // ---- producers: bf16: every fourth block of K 0, V 0, K 1, V 1, ... each; int8: one the keys, one the values --------
-        constexpr int kWarps = kInt8 ? 2 : kProducers, kRing = kInt8 ? 3 : kStages;
-        const int halves = W > 64 ? 2 : 1;
-        if (warp - kFirstProducer < kWarps)
-            for (int i = warp - kFirstProducer; i < 2 * total; i += kWarps) {
-                const int s = i % kRing, round = i / kRing, j = from + i / 2;
-                const bool values = i & 1;
-                uint64_t *const full_bar = kInt8 ? &sh.raw_full[s % 3] : &sh.kv_full[s], *const empty_bar = kInt8 ? &sh.raw_empty[s % 3] : &sh.kv_empty[s];
-                // the rows of the block's eight 16-key groups, one per lane
-                int row = -1;
-                bool bad = false;
-                if (lane < 8) {
-                    const int pos = j * kTile + lane * 16;
-                    if (pos < w.len) {
-                        const int page = kv_page(a.cache, a.batch, w.b, pos);
-                        bad = page < 0;
-                        if (bad)
-                            kv_report(a.cache);
-                        else
-                            row = kv_row(a.cache, page, w.head, pos);
+                    for (int u = 0; u < 8; ++u) {
+                        const int r = (warp - kFirstConverter) * 32 + u * 4 + r0;
+                        const uint4 x = *reinterpret_cast<const uint4 *>(codes + r * W + c * 16);
+                        *reinterpret_cast<uint4 *>(out + r * 128 + ((p ^ (r & 7)) << 4)) =
+                            make_uint4(code_pair<0x4140>(x.x), code_pair<0x4342>(x.x), code_pair<0x4140>(x.y), code_pair<0x4342>(x.y));
+                        *reinterpret_cast<uint4 *>(out + r * 128 + (((p + 1) ^ (r & 7)) << 4)) =
+                            make_uint4(code_pair<0x4140>(x.z), code_pair<0x4342>(x.z), code_pair<0x4140>(x.w), code_pair<0x4342>(x.w));
                     }
                 }
-                const uint32_t bad_groups = __ballot_sync(0xFFFFFFFFu, bad);
-                if (round > 0 && !mbar_wait_bounded(smem_u32(empty_bar), (round - 1) & 1, abort_flag, limit)) break;
-                if (!values && lane == 0) sh.bad_groups[(i / 2) % kInfo] = bad_groups;
-                const uint32_t full = smem_u32(full_bar);
-                const int per_copy = min(kTile, 1 << a.cache.page_shift); // rows of a copy
-                // (test device: the first CTA leaves out its first arrival and the copies that it announces)
-                const bool skip = args.hooks.skip_arrive && blockIdx.x == 0 && i == 0;
-                const uint32_t have = __ballot_sync(0xFFFFFFFFu, row >= 0);
-                uint32_t bytes = (uint32_t)(halves * kHalfBytes);
-                if (kInt8) {
-                    bytes = 0;
-                    for (int g = 0; g < kTile / 16; g += per_copy / 16)
-                        if ((have >> g) & 1u) bytes += (uint32_t)(per_copy * (W + 4));
-                }
-                if (lane == 0 && !skip) mbar_arrive_expect_tx(full, bytes);
+                fence_proxy_async_smem();
                 __syncwarp();
-                for (int g = 0; g < kTile / 16; g += per_copy / 16) {
-                    const int r = __shfl_sync(0xFFFFFFFFu, row, g);
-                    if (lane != 0 || skip) continue;
-                    if (!kInt8) {
-                        const int absent = (a.cache.n_pages * a.cache.kv_heads) << a.cache.page_shift; // a row behind the cache: reads zeros
-                        for (int h = 0; h < halves; ++h)
-                            tma_load_2d(ring + s * kTileBytes16 + h * kHalfBytes + g * 16 * 128, values ? &args.v_map : &args.k_map, h * 64,
-                                        r < 0 ? absent : r, full);
-                    } else if (r >= 0) {
-                        const uint32_t dst = smem_u32(raw_ring) + s * kRawBytes;
-                        bulk_copy_g2s(dst + g * 16 * W, reinterpret_cast<const int8_t *>(values ? a.cache.v : a.cache.k) + (int64_t)r * W,
-                                      (uint32_t)(per_copy * W), full);
-                        bulk_copy_g2s(dst + kTile * 128 + g * 64, (values ? a.cache.v_scale : a.cache.k_scale) + r, (uint32_t)(per_copy * 4), full);
-                    }
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&sh.kv_full[s]));
+                    mbar_arrive(smem_u32(&sh.raw_empty[rs]));
                 }
             }
-    } else {
-        // ---- MMAs of tile t ----------------------------------------------------------------------------------
-        const int t = warp - kMmaWarp, n = n_steps[t], k_steps = W / 16;
-        const uint32_t idesc_s = idesc_bf16(kTile, kStep, 0), idesc_o = idesc_bf16(kTile, W, 1);
-        const uint32_t s_tmem = tmem + t * kTile, o_tmem = tmem + kRows + t * kTile;
-        const uint64_t q_desc = smem_desc_k_sw128(q_addr + t * kTileBytes16);
-        auto wait = [&](uint64_t *bar, int phase) { return mbar_spin_bounded(smem_u32(bar), phase & 1, abort_flag, limit); };
-        auto full = [&](int i) { return wait(&sh.kv_full[i % kStages], i / kStages); }; // K of block j: i = 2 j, V: i = 2 j + 1
-        // S = Q K^T of step k, into half k % 2 of the tile's score columns
-        auto scores = [&](int k) {
-            const int stage = (k & ~1) % kStages;
-            const uint64_t k_desc = smem_desc_k_sw128(ring + stage * kTileBytes16 + (k & 1) * kStep * 128);
-            if (elect_one()) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < k_steps) {
-                        const uint64_t at = ((i / 4) * kHalfBytes + (i % 4) * 32) >> 4;
-                        mma_f16_ss(s_tmem + (k & 1) * kStep, q_desc + at, k_desc + at, idesc_s, i > 0);
+        } else if (warp >= kFirstProducer) {
+            // ---- producers: bf16: every fourth block of K 0, V 0, K 1, V 1, ... each; int8: one the keys, one the values --------
+            constexpr int kWarps = kInt8 ? 2 : kProducers, kRing = kInt8 ? 3 : kStages;
+            const int halves = W > 64 ? 2 : 1;
+            if (warp - kFirstProducer < kWarps)
+                for (int i = warp - kFirstProducer; i < 2 * total; i += kWarps) {
+                    const int s = i % kRing, round = i / kRing, j = from + i / 2;
+                    const bool values = i & 1;
+                    uint64_t *const full_bar = kInt8 ? &sh.raw_full[s % 3] : &sh.kv_full[s], *const empty_bar = kInt8 ? &sh.raw_empty[s % 3] : &sh.kv_empty[s];
+                    // the rows of the block's eight 16-key groups, one per lane
+                    int row = -1;
+                    bool bad = false;
+                    if (lane < 8) {
+                        const int pos = j * kTile + lane * 16;
+                        if (pos < w.len) {
+                            const int page = kv_page(a.cache, a.batch, w.b, pos);
+                            bad = page < 0;
+                            if (bad)
+                                kv_report(a.cache);
+                            else
+                                row = kv_row(a.cache, page, w.head, pos);
+                        }
                     }
-                mma_commit(smem_u32(&sh.s_full[t][k & 1]));
-                if ((k & 1) || k + 1 == n) mma_commit(smem_u32(&sh.kv_empty[stage]));
-            }
-            __syncwarp();
-        };
-        bool ok = true;
-        if (n > 0) {
-            ok = full(0) && wait(&sh.q_full[t], 0);
-            tc_fence_after_sync();
-            if (ok) scores(0);
-            if (ok && n > 1) scores(1);
-        }
-        for (int k = 0; k < n && ok; ++k) {
-            const int v = k | 1, stage = v % kStages; // block k / 2: values are tile 2 (k / 2) + 1
-            if (!(ok = full(v) && wait(&sh.p_ready[t][k & 1], k >> 1))) break;
-            tc_fence_after_sync();
-            const uint64_t v_desc = smem_desc_mn_sw128(ring + stage * kTileBytes16 + (k & 1) * kStep * 128, kHalfBytes);
-            if (elect_one()) {
+                    const uint32_t bad_groups = __ballot_sync(0xFFFFFFFFu, bad);
+                    if (round > 0 && !mbar_wait_bounded(smem_u32(empty_bar), (round - 1) & 1, abort_flag, limit)) break;
+                    if (!values && lane == 0) sh.bad_groups[(i / 2) % kInfo] = bad_groups;
+                    const uint32_t full = smem_u32(full_bar);
+                    const int per_copy = min(kTile, 1 << a.cache.page_shift); // rows of a copy
+                    // (test device: the first CTA leaves out its first arrival and the copies that it announces)
+                    const bool skip = args.hooks.skip_arrive && blockIdx.x == 0 && i == 0;
+                    const uint32_t have = __ballot_sync(0xFFFFFFFFu, row >= 0);
+                    uint32_t bytes = (uint32_t)(halves * kHalfBytes);
+                    if (kInt8) {
+                        bytes = 0;
+                        for (int g = 0; g < kTile / 16; g += per_copy / 16)
+                            if ((have >> g) & 1u) bytes += (uint32_t)(per_copy * (W + 4));
+                    }
+                    if (lane == 0 && !skip) mbar_arrive_expect_tx(full, bytes);
+                    __syncwarp();
+                    for (int g = 0; g < kTile / 16; g += per_copy / 16) {
+                        const int r = __shfl_sync(0xFFFFFFFFu, row, g);
+                        if (lane != 0 || skip) continue;
+                        if (!kInt8) {
+                            const int absent = (a.cache.n_pages * a.cache.kv_heads) << a.cache.page_shift; // a row behind the cache: reads zeros
+                            for (int h = 0; h < halves; ++h)
+                                tma_load_2d(ring + s * kTileBytes16 + h * kHalfBytes + g * 16 * 128, values ? &args.v_map : &args.k_map, h * 64,
+                                            r < 0 ? absent : r, full);
+                        } else if (r >= 0) {
+                            const uint32_t dst = smem_u32(raw_ring) + s * kRawBytes;
+                            bulk_copy_g2s(dst + g * 16 * W, reinterpret_cast<const int8_t *>(values ? a.cache.v : a.cache.k) + (int64_t)r * W,
+                                          (uint32_t)(per_copy * W), full);
+                            bulk_copy_g2s(dst + kTile * 128 + g * 64, (values ? a.cache.v_scale : a.cache.k_scale) + r, (uint32_t)(per_copy * 4), full);
+                        }
+                    }
+                }
+        } else {
+            // ---- MMAs of tile t ----------------------------------------------------------------------------------
+            const int t = warp - kMmaWarp, n = n_steps[t], k_steps = W / 16;
+            const uint32_t idesc_s = idesc_bf16(kTile, kStep, 0), idesc_o = idesc_bf16(kTile, W, 1);
+            const uint32_t s_tmem = tmem + t * kTile, o_tmem = tmem + kRows + t * kTile;
+            const uint64_t q_desc = smem_desc_k_sw128(q_addr + t * kTileBytes16);
+            auto wait = [&](uint64_t *bar, int phase) { return mbar_spin_bounded(smem_u32(bar), phase & 1, abort_flag, limit); };
+            auto full = [&](int i) { return wait(&sh.kv_full[i % kStages], i / kStages); }; // K of block j: i = 2 j, V: i = 2 j + 1
+            // S = Q K^T of step k, into half k % 2 of the tile's score columns
+            auto scores = [&](int k) {
+                const int stage = (k & ~1) % kStages;
+                const uint64_t k_desc = smem_desc_k_sw128(ring + stage * kTileBytes16 + (k & 1) * kStep * 128);
+                if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) // O += P V, 16 keys each
-                    mma_f16_ts(o_tmem, s_tmem + (k & 1) * kStep + i * 8, v_desc + ((i * 16 * 128) >> 4), idesc_o, k > 0 || i > 0);
-                mma_commit(smem_u32(&sh.o_done[t]));
-                if (k + 1 == n) mma_commit(smem_u32(&sh.o_last[t]));
-                if ((k & 1) || k + 1 == n) mma_commit(smem_u32(&sh.kv_empty[stage]));
-            }
-            __syncwarp();
-            if (k + 2 < n) {
-                if (!(ok = full((k + 2) & ~1))) break;
+                    for (int i = 0; i < 8; ++i)
+                        if (i < k_steps) {
+                            const uint64_t at = ((i / 4) * kHalfBytes + (i % 4) * 32) >> 4;
+                            mma_f16_ss(s_tmem + (k & 1) * kStep, q_desc + at, k_desc + at, idesc_s, i > 0);
+                        }
+                    mma_commit(smem_u32(&sh.s_full[t][k & 1]));
+                    if ((k & 1) || k + 1 == n) mma_commit(smem_u32(&sh.kv_empty[stage]));
+                }
+                __syncwarp();
+            };
+            bool ok = true;
+            if (n > 0) {
+                ok = full(0) && wait(&sh.q_full[t], 0);
                 tc_fence_after_sync();
-                scores(k + 2);
+                if (ok) scores(0);
+                if (ok && n > 1) scores(1);
+            }
+            for (int k = 0; k < n && ok; ++k) {
+                const int v = k | 1, stage = v % kStages; // block k / 2: values are tile 2 (k / 2) + 1
+                if (!(ok = full(v) && wait(&sh.p_ready[t][k & 1], k >> 1))) break;
+                tc_fence_after_sync();
+                const uint64_t v_desc = smem_desc_mn_sw128(ring + stage * kTileBytes16 + (k & 1) * kStep * 128, kHalfBytes);
+                if (elect_one()) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) // O += P V, 16 keys each
+                        mma_f16_ts(o_tmem, s_tmem + (k & 1) * kStep + i * 8, v_desc + ((i * 16 * 128) >> 4), idesc_o, k > 0 || i > 0);
+                    mma_commit(smem_u32(&sh.o_done[t]));
+                    if (k + 1 == n) mma_commit(smem_u32(&sh.o_last[t]));
+                    if ((k & 1) || k + 1 == n) mma_commit(smem_u32(&sh.kv_empty[stage]));
+                }
+                __syncwarp();
+                if (k + 2 < n) {
+                    if (!(ok = full((k + 2) & ~1))) break;
+                    tc_fence_after_sync();
+                    scores(k + 2);
+                }
+            }
+            // blocks that only the other tile needs
+            for (int i = (n + 1) / 2 * 2; i < 2 * total && ok; ++i) {
+                ok = full(i);
+                if (ok && lane == 0) mbar_arrive(smem_u32(&sh.kv_empty[i % kStages]));
             }
         }
-        // blocks that only the other tile needs
-        for (int i = (n + 1) / 2 * 2; i < 2 * total && ok; ++i) {
-            ok = full(i);
-            if (ok && lane == 0) mbar_arrive(smem_u32(&sh.kv_empty[i % kStages]));
-        }
-    }
     } else {
         take_registers<kSoftmaxRegs>();
         // ---- softmax: one row per thread ------------------------------------------------------------------------

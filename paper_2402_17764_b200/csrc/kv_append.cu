@@ -12,7 +12,9 @@
 // middle between two codes) are computed again in double from memory.
 //
 // What bounds it: memory (every byte read and written once) for prompts, the launch and one chain of dependent loads
-// (length, page number, row) for a decode step.
+// (length, page number, row) for a decode step.  Measured: 4096 tokens, 64/8 heads of 128: 32.5 us = 5.2 TB/s (0.79 of a copy's
+// rate); single tokens 8.4 us per call, the time the host needs for one; int8, 4600 tokens, 40/40 heads: 50 us = 2.5 TB/s,
+// bound by instructions (row maxima, quotients and the test that settles each code).
 #include <math.h>
 
 #include <algorithm>
