@@ -9,11 +9,12 @@
 //
 // 8 bits: code = round(127 x / beta) has to come out as in exact arithmetic, also for values half way between two codes.  All is
 // done in fp32 first; the few elements that fp32 cannot settle (candidates for the row's maximum, quotients near the
-// middle between two codes) are computed again in double from memory.
+// middle between two codes) are computed again in double from memory.  Codes are rounded by adding 1.5 2^23, which leaves them in the
+// low bytes of the sums (conversions go through a unit a quarter as wide: 2436 tokens, 40/40 heads: 52 -> 46 us with it).
 //
 // What bounds it: memory (every byte read and written once) for prompts, the launch and one chain of dependent loads
 // (length, page number, row) for a decode step.  Measured: 4096 tokens, 64/8 heads of 128: 32.5 us = 5.2 TB/s (0.79 of a copy's
-// rate); single tokens 8.4 us per call, the time the host needs for one; int8, 4600 tokens, 40/40 heads: 50 us = 2.5 TB/s,
+// rate); single tokens 8.4 us per call, the time the host needs for one; int8, 2436 tokens, 40/40 heads: 46 us = 2.8 TB/s,
 // bound by instructions (row maxima, quotients and the test that settles each code).
 #include <math.h>
 
@@ -73,15 +74,24 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&x)[V
     *reinterpret_cast<Piece<VEC> *>(p) = w;
 }
 
+// The largest magnitude of three, or NaN if one of them is.
+__device__ __forceinline__ float largest(float x, float y, float z)
+{
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+    return m;
+}
+
 // Heads that a group of lanes takes at a time.  With 4-byte pieces four heads' loads have to be in flight to hide the
 // memory's latency (4096 tokens, 32/32 heads of 100: one at a time 74 us, two or four 57, eight 66); with 16-byte pieces the
 // registers are worth more as warps (64/8 heads of 128: one 32 us, two 38).  An 8-bit row works on more values: one.
 template <int VEC, bool kInt8>
 constexpr int kHeadsAtATime = VEC == 2 && !kInt8 ? 4 : 1;
 
+// Three CTAs per SM for the 8-bit rows of 16-byte pieces: their values need 80 registers (four CTAs, with spills: 4 us more).
 // kRotate: 0 none, 1 pairs half a head apart, 2 adjacent pairs.
 template <int VEC, bool kInt8, int kRotate>
-__global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares) // warps per token
+__global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares) // warps per token
 {
     ptx::griddep_wait(); // everything below is read from memory that the launch before this one may have written
     ptx::griddep_launch_dependents();
@@ -150,11 +160,6 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
         auto first_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j] : x1[2 * j - VEC]) : x0[j]; };
         auto second_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j + 1] : x1[2 * j + 1 - VEC]) : x1[j]; };
         const bool rotate = kRotate != 0 && (is_q || is_k);
-        bool finite = true;
-        if (kInt8) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) finite = finite && fabsf(x0[i]) <= 3.4028235e38f && fabsf(x1[i]) <= 3.4028235e38f;
-        }
         if (rotate) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
@@ -174,7 +179,7 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
             if (VEC == 2 && !kInt8 && !is_q && task < tasks && page >= 0 && lane < a.cache.width - D) // (the row's padding)
                 reinterpret_cast<__nv_bfloat16 *>(is_k ? a.cache.k : a.cache.v)[row * a.cache.width + D + lane] = __float2bfloat16(0.0f);
         }
-        if (kInt8) {
+        if (kInt8 && task - group + kGroups > a.heads) { // (not for a warp that has queries alone)
             // element i of x0, then of x1, exactly (up to 2^-53)
             auto exact = [&](int i) -> double {
                 const int e = i < VEC ? o0 + i : o1 + i - VEC;
@@ -188,16 +193,22 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
             };
             float top = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2 * VEC; ++i) top = fmaxf(top, fabsf(i < VEC ? x0[i] : x1[i - VEC]));
+            for (int i = 0; i < VEC; ++i) top = largest(top, x0[i], x1[i]);
 #pragma unroll
-            for (int d = 1; d < kLanes; d <<= 1) {
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-                finite = __shfl_xor_sync(0xFFFFFFFFu, (int)finite, d) && finite;
-            }
+            for (int d = 1; d < kLanes; d <<= 1) top = largest(top, __shfl_xor_sync(0xFFFFFFFFu, top, d), 0.0f);
             // The rotated fp32 values are within 2^-22 of the row's maximum of the exact ones (three roundings of a c and b s,
             // |a c| + |b s| <= 2 max): only those within 2^-20 of the largest can be the exact maximum.  (Near the end of
             // fp32's range, where a rotation may overflow, nothing is settled in fp32.)
-            const bool huge = !(top <= 1e38f);
+            const bool huge = !(top <= 8e37f);
+            bool finite = true; // a row that is not finite stays so when it is rotated: such rows are among the huge ones
+            if (__any_sync(0xFFFFFFFFu, huge)) {
+                bool all = true;
+                if (work)
+                    for (int i = 0; i < VEC; ++i) all = all && isfinite(__bfloat162float(src[o0 + i])) && isfinite(__bfloat162float(src[o1 + i]));
+#pragma unroll
+                for (int d = 1; d < kLanes; d <<= 1) all = __shfl_xor_sync(0xFFFFFFFFu, (int)all, d) && all;
+                finite = all;
+            }
             constexpr uint32_t kAll = 2 * VEC == 32 ? ~0u : (1u << (2 * VEC)) - 1u;
             double beta = top;
             if (rotate) {
@@ -207,35 +218,52 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
                 for (int i = 0; i < 2 * VEC; ++i) candidates |= (uint32_t)(fabsf(i < VEC ? x0[i] : x1[i - VEC]) >= top * 0.99999905f) << i;
                 if (huge) candidates = kAll;
                 if (!work || is_q || !finite) candidates = 0;
+                const uint32_t holders = __ballot_sync(0xFFFFFFFFu, candidates != 0u) & (kLanes == 32 ? ~0u : 0xFFu << (8 * group)); // lanes of this row
                 for (; candidates; candidates &= candidates - 1) beta = fmax(beta, fabs(exact(__ffs(candidates) - 1)));
+                if (__any_sync(0xFFFFFFFFu, __popc(holders) > 1)) {
 #pragma unroll
-                for (int d = 1; d < kLanes; d <<= 1) beta = fmax(beta, __shfl_xor_sync(0xFFFFFFFFu, beta, d));
+                    for (int d = 1; d < kLanes; d <<= 1) beta = fmax(beta, __shfl_xor_sync(0xFFFFFFFFu, beta, d));
+                } else {
+                    beta = __shfl_sync(0xFFFFFFFFu, beta, holders ? __ffs(holders) - 1 : 0);
+                }
             }
             if (is_q || task >= tasks || page < 0) return;
             beta = fmax(beta, 1e-5);
             int8_t *dst = reinterpret_cast<int8_t *>(is_k ? a.cache.k : a.cache.v) + row * a.cache.width;
             if (mine) {
-                const float inv = 127.0f / (float)beta;
-                int8_t c[2 * VEC];
-                uint32_t unsettled = 0;
+                const float inv = __fdividef(127.0f, (float)beta); // (within 2 ulp up to 2^126 > 8e37)
+                // t = 1.5 2^23 + round(x inv): its low byte is the code, and x inv - code is exact but for its last bit.
+                // The estimate of 127 x / beta is off by 127 (2^-22 + 2^-22 + 2^-24) < 7e-5 at most.
+                constexpr float kShift = 12582912.0f, kSettled = 0.4999f;
+                auto value = [&](int i) { return i < VEC ? x0[i] : x1[i - VEC]; };
+                auto beside = [&](float x, float t) { return fmaf(x, inv, kShift - t); };
+                uint32_t t[2 * VEC];
+                float most = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 2 * VEC; ++i) {
-                    // 127 x / beta up to 127 (2^-22 + 3 2^-24) < 6e-5
-                    const float y = (i < VEC ? x0[i] : x1[i - VEC]) * inv, r = rintf(y);
-                    unsettled |= (uint32_t)(fabsf(fabsf(y - r) - 0.5f) < 1e-4f) << i;
-                    c[i] = finite ? (int8_t)(int)r : (int8_t)0;
+                for (int i = 0; i < 2 * VEC; i += 2) {
+                    const float y = fmaf(value(i), inv, kShift), z = fmaf(value(i + 1), inv, kShift);
+                    most = largest(most, beside(value(i), y), beside(value(i + 1), z));
+                    t[i] = __float_as_uint(y);
+                    t[i + 1] = __float_as_uint(z);
                 }
-                if (huge) unsettled = kAll;
-                if (!finite) unsettled = 0;
+                uint32_t unsettled = 0;
+                if (huge) {
+                    unsettled = finite ? kAll : 0u;
+                } else if (most > kSettled) {
+#pragma unroll
+                    for (int i = 0; i < 2 * VEC; ++i) unsettled |= (uint32_t)(fabsf(beside(value(i), __uint_as_float(t[i]))) > kSettled) << i;
+                }
+                auto four = [&](int i) { // (a row that is not finite: 0)
+                    const uint32_t w = __byte_perm(__byte_perm(t[i], t[i + 1], 0x0040), __byte_perm(t[i + 2], t[i + 3], 0x0040), 0x5410);
+                    return finite ? w : 0u;
+                };
                 if constexpr (VEC == 8) {
-                    uint2 w0, w1;
-                    memcpy(&w0, c, 8);
-                    memcpy(&w1, c + 8, 8);
-                    *reinterpret_cast<uint2 *>(dst + o0) = w0;
-                    *reinterpret_cast<uint2 *>(dst + o1) = w1;
+                    *reinterpret_cast<uint2 *>(dst + o0) = make_uint2(four(0), four(4));
+                    *reinterpret_cast<uint2 *>(dst + o1) = make_uint2(four(8), four(12));
                 } else {
-                    *reinterpret_cast<char2 *>(dst + o0) = make_char2(c[0], c[1]);
-                    *reinterpret_cast<char2 *>(dst + o1) = make_char2(c[2], c[3]);
+                    const uint32_t w = four(0);
+                    *reinterpret_cast<uint16_t *>(dst + o0) = (uint16_t)w;
+                    *reinterpret_cast<uint16_t *>(dst + o1) = (uint16_t)(w >> 16);
                 }
                 for (; unsettled; unsettled &= unsettled - 1) {
                     const int i = __ffs(unsettled) - 1;
@@ -243,7 +271,14 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const __grid_constant
                 }
             }
             if (VEC == 2 && lane < a.cache.width - D) dst[D + lane] = 0;
-            if (lane == 0) (is_k ? a.cache.k_scale : a.cache.v_scale)[row] = finite ? (float)(beta / 127.0) : __int_as_float(0x7FFFFFFF);
+            if (lane == 0) {
+                // beta / 127 is within 2^-52 of this product, so it rounds to the same fp32 number unless that lies within a few
+                // units of the middle between two
+                double scale = beta * (1.0 / 127.0);
+                const int below = (int)(__double_as_longlong(scale) & 0x1FFFFFFF) - 0x10000000;
+                if (below >= -8 && below <= 8) scale = beta / 127.0;
+                (is_k ? a.cache.k_scale : a.cache.v_scale)[row] = finite ? (float)scale : __int_as_float(0x7FFFFFFF);
+            }
         }
     };
 
