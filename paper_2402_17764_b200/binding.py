@@ -607,14 +607,18 @@ def rope_table(n_pos: int, head_dim: int, base: float = 10000.0, device="cuda", 
     return table
 
 
-def _row_stride(t: torch.Tensor, heads: int, head_dim: int, rows: int, index: int, where: str) -> int:
+_BF16, _FP32 = torch.bfloat16, torch.float32
+
+
+def _row_stride(t: torch.Tensor, shape: tuple, index: int, where: str) -> int:
     """Row stride of bf16 [rows, heads, head_dim] in elements; refuses what the kernels cannot address."""
-    if t.shape != (rows, heads, head_dim) or t.dtype is not torch.bfloat16 or t.get_device() != index:
-        _refuse(where, f"expected bf16 [{rows}, {heads}, {head_dim}] on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.shape != shape or t.dtype is not _BF16 or t.get_device() != index:
+        _refuse(where, f"expected bf16 {list(shape)} on cuda:{index}, got {t.dtype} {list(t.shape)} on {t.device}")
     row, head, element = t.stride()
-    if (head_dim > 1 and element != 1) or (heads > 1 and head != head_dim):
-        _refuse(where, "the heads of a row are contiguous")
-    return row if rows > 1 else (heads * head_dim + 7) // 8 * 8
+    if element != 1 or head != shape[2]:
+        if element != 1 or shape[1] > 1:
+            _refuse(where, "the heads of a row are contiguous")
+    return row if shape[0] > 1 else (shape[1] * shape[2] + 7) // 8 * 8
 
 
 def _empty_rows(rows: int, heads: int, head_dim: int, device) -> torch.Tensor:
@@ -630,16 +634,8 @@ def _allocating_on(stream, device):
     return torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device))
 
 
-def _launch_device(cache: KVCache, batch: KVBatch, where: str) -> int:
-    """Index of the device that the cache and the batch are on."""
-    if batch.index != cache.index:
-        _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
-    return cache.index
-
-
-def _stream_of(stream, index: int) -> int:
-    # (what torch.cuda.current_stream(index).cuda_stream gives, without the objects in between)
-    return torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+# (what torch.cuda.current_device() and torch.cuda.current_stream(index).cuda_stream give, without the objects in between)
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def kv_append(cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor | None = None,
@@ -647,33 +643,40 @@ def kv_append(cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, 
     """bitlinear_kv_append: rotates k [T, kv_heads, head_dim] and stores it with v in the cache; rotates q [T, heads, head_dim]
     into q_out (allocated if not given, may be q itself) and returns it (None without q)."""
     where = "bitlinear_kv_append"
-    index = _launch_device(cache, batch, where)
-    if torch._C._cuda_getDevice() != index:
+    index = cache.index
+    if batch.index != index:
+        _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
+    if _current_device() != index:
         with torch.cuda.device(index):
             return kv_append(cache, batch, k, v, q, rope, interleaved, q_out, stream)
     if stream is not None and q is not None and q_out is None:
         with _allocating_on(stream, cache.device):
             return kv_append(cache, batch, k, v, q, rope, interleaved)
+    if k.dim() != 3 or (q is not None and q.dim() != 3):
+        _refuse(where, "k, v and q are [tokens, heads, head_dim]", ERR_SHAPE)
     T, D = k.shape[0], cache.head_dim
-    ks = _row_stride(k, cache.kv_heads, D, T, index, where)
-    vs = _row_stride(v, cache.kv_heads, D, T, index, where)
-    heads = qs = os_ = positions = 0
+    shape = (T, cache.kv_heads, D)
+    ks = _row_stride(k, shape, index, where)
+    vs = _row_stride(v, shape, index, where)
+    heads = qs = os_ = positions = q_at = out_at = rope_at = 0
     if q is not None:
-        heads = q.shape[1] if q.dim() == 3 else 0
-        qs = _row_stride(q, heads, D, T, index, where)
+        heads = q.shape[1]
+        shape = (T, heads, D)
+        qs = _row_stride(q, shape, index, where)
         if q_out is None:
             q_out = _empty_rows(T, heads, D, cache.device)
-        os_ = _row_stride(q_out, heads, D, T, index, where)
+        os_ = _row_stride(q_out, shape, index, where)
+        q_at, out_at = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         _refuse(where, "q_out without q")
     if rope is not None:
         positions = rope.shape[0]
-        if rope.shape != (positions, D // 2, 2) or rope.dtype is not torch.float32 or not rope.is_contiguous() or rope.get_device() != index:
+        if rope.shape != (positions, D // 2, 2) or rope.dtype is not _FP32 or not rope.is_contiguous() or rope.get_device() != index:
             _refuse(where, f"rope is a contiguous fp32 [positions, {D // 2}, 2] on {cache.device}")
-    st = (_lib or load_library()).bitlinear_kv_append(
-        cache._address, batch._address, k.data_ptr(), ks, v.data_ptr(), vs, 0 if q is None else q.data_ptr(), qs, T, heads,
-        0 if rope is None else rope.data_ptr(), positions, 1 if interleaved else 0, 0 if q_out is None else q_out.data_ptr(), os_,
-        _stream_of(stream, index))
+        rope_at = rope.data_ptr()
+    st = (_lib or load_library()).bitlinear_kv_append(cache._address, batch._address, k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, T, heads,
+                                                      rope_at, positions, 1 if interleaved else 0, out_at, os_,
+                                                      _raw_stream(index) if stream is None else _stream(stream))
     if st != OK:
         _check(st, where)
     return q_out
@@ -693,8 +696,10 @@ def alloc_attend_workspace(heads: int, kv_heads: int, head_dim: int, prompt: boo
 
 def _attend(prompt: bool, cache: KVCache, batch: KVBatch, q, scale, out, workspace, stream):
     where = "bitlinear_attend_prompt" if prompt else "bitlinear_attend_decode"
-    index = _launch_device(cache, batch, where)
-    if torch._C._cuda_getDevice() != index:
+    index = cache.index
+    if batch.index != index:
+        _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
+    if _current_device() != index:
         with torch.cuda.device(index):
             return _attend(prompt, cache, batch, q, scale, out, workspace, stream)
     if stream is not None and (out is None or workspace is None):
@@ -706,23 +711,25 @@ def _attend(prompt: bool, cache: KVCache, batch: KVBatch, q, scale, out, workspa
     D = cache.head_dim
     if not prompt and T != batch.n_seqs:
         _refuse(where, f"{batch.n_seqs} sequences and {T} tokens", ERR_SHAPE)
-    qs = _row_stride(q, heads, D, T, index, where)
+    shape = (T, heads, D)
+    qs = _row_stride(q, shape, index, where)
     if out is None:
         out = _empty_rows(T, heads, D, cache.device)
-    os_ = _row_stride(out, heads, D, T, index, where)
+    os_ = _row_stride(out, shape, index, where)
     if workspace is None:
         workspace = alloc_attend_workspace(heads, cache.kv_heads, D, prompt, cache.device)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         _refuse(where, f"the workspace is contiguous and on {cache.device}")
     scale = D ** -0.5 if scale is None else float(scale)
     nbytes = workspace.numel() * workspace.element_size()
+    stream = _raw_stream(index) if stream is None else _stream(stream)
     L = _lib or load_library()
     if prompt:
         st = L.bitlinear_attend_prompt(cache._address, batch._address, q.data_ptr(), qs, T, heads, scale, out.data_ptr(), os_,
-                                       workspace.data_ptr(), nbytes, _stream_of(stream, index))
+                                       workspace.data_ptr(), nbytes, stream)
     else:
         st = L.bitlinear_attend_decode(cache._address, batch._address, q.data_ptr(), qs, heads, scale, out.data_ptr(), os_,
-                                       workspace.data_ptr(), nbytes, _stream_of(stream, index))
+                                       workspace.data_ptr(), nbytes, stream)
     if st != OK:
         _check(st, where)
     return out
