@@ -234,7 +234,8 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int 
             make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
 }
 
-// Partial results of the CTAs that share a tile of rows: (reference, sum) of 256 rows, then their outputs.
+// Partial results of the CTAs that share a tile of rows: (reference, sum) of 256 rows, then their outputs as [four elements][row], so
+// that a row per thread writes and reads whole lines.
 __host__ __device__ constexpr size_t part_floats(int width) { return (size_t)kRows * (width + 2); }
 
 template <bool kInt8>
@@ -711,8 +712,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         if (ok) {
             const float inv = parts > 1 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
             __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + row / group) * a.out_stride + (w.head * group + row % group) * D;
-            float *part = part_of(split) + 2 * kRows + (size_t)(t * kTile + r) * W;
-            if (parts > 1) *reinterpret_cast<float2 *>(part_of(split) + 2 * (t * kTile + r)) = make_float2(n_steps[t] > 0 ? m : -INFINITY, l);
+            const int pr = t * kTile + r;
             const bool some = n_steps[t] > 0 && l != 0.0f;
             uint32_t o[4][32];
 #pragma unroll
@@ -722,9 +722,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             for (int c = 0; c < 4; ++c) tmem_ld_wait_for(o[c]);
             auto at = [&](int e) { return some ? __uint_as_float(o[e / 32][e % 32]) * inv : 0.0f; };
             if (parts > 1) {
+                if (exists) {
+                    float4 *part = reinterpret_cast<float4 *>(part_of(split) + 2 * kRows) + pr;
+                    *reinterpret_cast<float2 *>(part_of(split) + 2 * pr) = make_float2(n_steps[t] > 0 ? m : -INFINITY, l);
 #pragma unroll
-                for (int e = 0; e < kTile; e += 4)
-                    if (e < W) *reinterpret_cast<float4 *>(part + e) = make_float4(at(e), at(e + 1), at(e + 2), at(e + 3));
+                    for (int e = 0; e < kTile; e += 4)
+                        if (e < W) part[e / 4 * kRows] = make_float4(at(e), at(e + 1), at(e + 2), at(e + 3));
+                }
             } else {
                 // by way of the tile's queries, which are not needed any more, so that a warp stores whole rows
                 uint8_t *own = q_tile + (warp % 4) * 32 * 256;
@@ -738,9 +742,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                 const int c = lane % 16, left = D - c * 8;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int pr = 2 * i + lane / 16;
-                    const int64_t to = __shfl_sync(0xFFFFFFFFu, mine, pr);
-                    const uint4 y = *reinterpret_cast<const uint4 *>(own + pr * 256 + ((c ^ (pr & 7)) << 4));
+                    const int sr = 2 * i + lane / 16;
+                    const int64_t to = __shfl_sync(0xFFFFFFFFu, mine, sr);
+                    const uint4 y = *reinterpret_cast<const uint4 *>(own + sr * 256 + ((c ^ (sr & 7)) << 4));
                     if (to < 0 || left <= 0) continue;
                     if (D % 8 == 0) {
                         *reinterpret_cast<uint4 *>(a.out + to + c * 8) = y;
@@ -771,27 +775,42 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             named_barrier(1, kRows);
             if (sh.is_last) {
                 __threadfence();
-                for (int i = tid; i < kRows * (W / 4); i += kRows) {
-                    const int pr = i / (W / 4), e = i % (W / 4) * 4, rr = w.row0 + pr;
-                    if (rr >= w.rows || e >= D) continue;
-                    float M = -INFINITY;
+                const int pr = tid, rr = w.row0 + pr; // a row per thread
+                if (rr < w.rows) {
+                    float M = -INFINITY, L = 0.0f;
+#pragma unroll 4
                     for (int p = 0; p < parts; ++p) M = fmaxf(M, __ldcg(part_of(p) + 2 * pr));
                     const float ref = M == -INFINITY ? 0.0f : M;
-                    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    float L = 0.0f;
+                    float *factor = reinterpret_cast<float *>(smem) + tid; // (where the queries were)
+#pragma unroll 4
                     for (int p = 0; p < parts; ++p) {
                         const float2 ml = __ldcg(reinterpret_cast<const float2 *>(part_of(p) + 2 * pr));
-                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(part_of(p) + 2 * kRows + (size_t)pr * W + e));
                         const float f = exp2_approx(ml.x - ref);
-                        x.x += f * v.x;
-                        x.y += f * v.y;
-                        x.z += f * v.z;
-                        x.w += f * v.w;
+                        factor[p * kRows] = f;
                         L += f * ml.y;
                     }
                     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-                    __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + rr / group) * a.out_stride + (w.head * group + rr % group) * D + e;
-                    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+                    __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + rr / group) * a.out_stride + (w.head * group + rr % group) * D;
+                    for (int e0 = 0; e0 < D; e0 += 16) { // (W is a multiple of 16)
+                        float4 x[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) x[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+                        for (int p = 0; p < parts; ++p) {
+                            const float4 *src = reinterpret_cast<const float4 *>(part_of(p) + 2 * kRows) + (size_t)(e0 / 4) * kRows + pr;
+                            const float f = factor[p * kRows];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const float4 v = __ldcg(src + u * kRows);
+                                x[u] = make_float4(x[u].x + f * v.x, x[u].y + f * v.y, x[u].z + f * v.z, x[u].w + f * v.w);
+                            }
+                        }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if (e0 + 4 * u < D)
+                                *reinterpret_cast<uint2 *>(dst + e0 + 4 * u) =
+                                    make_uint2(pack_bf16(x[u].x * inv, x[u].y * inv), pack_bf16(x[u].z * inv, x[u].w * inv));
+                    }
                 }
             }
         }
@@ -876,9 +895,9 @@ cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream)
     // No more tiles of rows than this can exist: every sequence has at most one that is not full.
     const int64_t group = a.heads / a.cache.kv_heads;
     const int64_t tiles = ((int64_t)a.T * group / kRows + std::min<int64_t>(a.batch.n_seqs, a.T)) * a.cache.kv_heads;
-    // With fewer tiles than SMs the keys of a tile are split among several CTAs.
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, kPromptMaxParts / std::max<int64_t>(tiles, 1)));
-    if (tiles >= sm_count()) p.splits = 1;
+    // With fewer tiles than SMs the keys of a tile are split among several CTAs, all of which run at the same time (2 tokens behind
+    // 10994, 32 heads of 100: with five CTAs for each of the 32 tiles twelve had to wait for an SM, 87 us; with four 57).
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min(sm_count(), kPromptMaxParts) / tiles));
     return a.cache.k_scale ? launch<true>(p, (int)(tiles * p.splits), stream) : launch<false>(p, (int)(tiles * p.splits), stream);
 }
 
