@@ -60,6 +60,7 @@ constexpr int kFirstConverter = 12, kConverters = 4; // int8
 constexpr int kThreads = 16 * 32;
 constexpr uint32_t kTmemColumns = 512;
 constexpr float kRaise = 8.0f;
+constexpr int kMaxParts = 16; // of a tile's keys
 // kv heads whose tiles follow each other: the keys and values of eight heads stay in the L2 while their tiles are worked on
 // (8192 tokens, 32 heads: 134 MB in all, 590 us with all heads at a time, 576 with eight)
 constexpr int kHeadGroup = 8;
@@ -99,6 +100,7 @@ struct PromptArgs {
     CUtensorMap k_map, v_map;
     AttendArgs a;
     int splits;       // CTAs that may share the keys of a tile of rows
+    int slots;        // > 0: CTAs among which the tiles are to be split, once their number is known
     WaitHooks hooks;
 };
 
@@ -259,9 +261,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     // ---- which rows: tiles are counted sequence by sequence, the longest first, and within a sequence, for every group of kv
     // heads, the last rows (which see most) first, so that the CTAs that start last have the least to do (four chunks of 86
     // to 512 tokens behind 3300 to 12000: 459 -> 383 us) ----
-    const int split = blockIdx.x % args.splits;
+    int splits = args.splits;
     {
-        const int64_t x = blockIdx.x / args.splits;
         auto tiles_of = [&](int b) -> int64_t {
             const int64_t n = (int64_t)a.batch.cu_tokens[b + 1] - a.batch.cu_tokens[b];
             return n <= 0 || n > a.T ? 0 : (n * group + kRows - 1) / kRows * a.cache.kv_heads;
@@ -301,6 +302,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         if (tid == 0) sh.found_b = -1;
         __syncthreads();
         for (int w = 0; w < warp; ++w) upto += sh.scan[w];
+        if (args.slots > 0) {
+            int tiles = 0; // (at most one per sequence and kv head, and what the host counted)
+#pragma unroll
+            for (int w = 0; w < kThreads / 32; ++w) tiles += (int)sh.scan[w];
+            splits = min(kMaxParts, max(1, args.slots / max(tiles, 1)));
+        }
+        const int64_t x = (int)blockIdx.x / splits;
         if (x >= upto - mine && x < upto) {
             int64_t rest = x - (upto - mine);
             int b = first_b;
@@ -316,6 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         __syncthreads();
     }
     if (sh.found_b < 0) return;
+    const int split = blockIdx.x % splits;
     Work w;
     w.b = sh.found_b;
     w.group = group;
@@ -339,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     // blocks of keys of the two tiles, and this CTA's part of them (a part is at least four blocks, so that joining the parts
     // does not cost more than they save)
     const int most = (w.sees(min(w.row0 + kRows, w.rows) - 1) + kTile - 1) / kTile;
-    const int parts = max(1, min(args.splits, most / 4));
+    const int parts = max(1, min(splits, most / 4));
     if (split >= parts) return;
     const int from = (int)((int64_t)most * split / parts), to = (int)((int64_t)most * (split + 1) / parts);
     int n_steps[2];
@@ -707,8 +716,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
 
         // ---- the result, or this CTA's part of it --------------------------------------------------------------
         float *ws_parts = reinterpret_cast<float *>(reinterpret_cast<char *>(a.workspace) + prompt_counter_bytes());
-        const int tile_x = blockIdx.x / args.splits;
-        auto part_of = [&](int p) { return ws_parts + (size_t)(tile_x * args.splits + p) * part_floats(W); };
+        const int first_part = blockIdx.x - split; // of this tile
+        auto part_of = [&](int p) { return ws_parts + (size_t)(first_part + p) * part_floats(W); };
         if (ok) {
             const float inv = parts > 1 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
             __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + row / group) * a.out_stride + (w.head * group + row % group) * D;
@@ -757,7 +766,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         }
         if (parts > 1) {
             // the CTA that finishes last joins the parts in their order and leaves the counter at zero
-            uint32_t *counter = reinterpret_cast<uint32_t *>(a.workspace) + 2 * tile_x;
+            uint32_t *counter = reinterpret_cast<uint32_t *>(a.workspace) + 2 * first_part;
             __threadfence();
             named_barrier(1, kRows);
             if (tid == 0) {
@@ -895,10 +904,15 @@ cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream)
     // No more tiles of rows than this can exist: every sequence has at most one that is not full.
     const int64_t group = a.heads / a.cache.kv_heads;
     const int64_t tiles = ((int64_t)a.T * group / kRows + std::min<int64_t>(a.batch.n_seqs, a.T)) * a.cache.kv_heads;
-    // With fewer tiles than SMs the keys of a tile are split among several CTAs, all of which run at the same time (2 tokens behind
-    // 10994, 32 heads of 100: with five CTAs for each of the 32 tiles twelve had to wait for an SM, 87 us; with four 57).
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min(sm_count(), kPromptMaxParts) / tiles));
-    return a.cache.k_scale ? launch<true>(p, (int)(tiles * p.splits), stream) : launch<false>(p, (int)(tiles * p.splits), stream);
+    // With fewer tiles than SMs the keys of a tile are split among several CTAs, as many as run at the same time (2 tokens behind
+    // 10994, 32 heads of 100: with five CTAs for each of the 32 tiles twelve had to wait for an SM, 87 us; with four 57).  Of
+    // several sequences only the device knows how many tiles they have (5 sequences of 50 tokens behind 4000, 24/8 heads
+    // of 64: 48 -> 42 us against the bound above).
+    const int slots = std::min(sm_count(), kPromptMaxParts);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxParts, slots / tiles));
+    p.slots = a.batch.n_seqs > 1 && tiles < slots ? slots : 0;
+    const int ctas = p.slots > 0 ? slots : (int)tiles * p.splits;
+    return a.cache.k_scale ? launch<true>(p, ctas, stream) : launch<false>(p, ctas, stream);
 }
 
 } // namespace bitlinear

@@ -462,6 +462,34 @@ def test_two_streams_with_workspaces_of_their_own(prompt):
         check(out, want, bound)
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(24, 8, 64), (4, 4, 100), (8, 1, 128)])
+def test_chunks_whose_keys_are_split_among_as_many_ctas_as_their_number_allows(heads, kv_heads, head_dim, bits):
+    # one workspace, one captured call: how the rows belong to sequences, and with that the splits, changes between replays
+    s = R.Setup([2100, 1300, 900, 5], kv_heads, head_dim, 32, bits, seed=51)
+    T, q = 60, rows(60, heads, head_dim, 51)
+    cu = torch.tensor([0, 15, 30, 45, 60], dtype=torch.int32, device="cuda")
+    cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens, cu)
+    ws = B.alloc_attend_workspace(heads, kv_heads, head_dim, prompt=True)
+    out = torch.empty(T, heads, head_dim, dtype=torch.bfloat16, device="cuda")
+    B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+    for new in ([15, 15, 15, 15], [60, 0, 0, 0], [0, 59, 0, 1], [1, 2, 55, 2], [20, 20, 20, 0]):
+        cu.copy_(torch.tensor([sum(new[:i]) for i in range(5)], dtype=torch.int32))
+        out.fill_(0.5)
+        graph.replay()
+        want, bound = R.attend(s, q, new, weight_rounding=WEIGHT_BF16)
+        check(out, want, bound)
+        first = out.clone()
+        graph.replay()
+        assert torch.equal(out, first)
+    cache.check()
+    assert not ws[:2048].any(), "the counters are left at zero"
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(4096, 1024), (4096, 1)])
 @pytest.mark.parametrize("bits", [16, 8])
 def test_the_most_heads(heads, kv_heads, bits):
