@@ -28,9 +28,9 @@
 //
 // What bounds it (heads of 128).  128 x 128 scores cost 16384 exponentials at 16 per cycle and SM, 1024 cycles, and two MMAs of
 // 512 cycles each: the two units are needed equally long, and neither can be kept busy all the time (tensor pipe 66 %,
-// exponentials 53 %).  8192 tokens, 32 heads: 580 us = 0.94 PFLOP/s, where the board's power limit holds the clock near 1.55
+// exponentials 53 %).  8192 tokens, 32 heads: 575 us = 0.96 PFLOP/s, where the board's power limit holds the clock near 1.55
 // GHz (the same launch takes about 930 000 cycles at any clock).  int8: the converters' shared-memory traffic and arithmetic come on
-// top, 60 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 372 us = 0.77 PFLOP/s).
+// top, 60 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 380 us = 0.77 PFLOP/s).
 // Prompts of few hundred tokens: half the time is each tile's beginning and end (pages, queries, first scores; results).
 #include <cuda.h>
 
