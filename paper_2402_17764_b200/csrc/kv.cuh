@@ -131,9 +131,11 @@ size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim);
 bool attend_decode_fits(const AttendArgs &a); // the kernel counts its work in 31 bits
 cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream);
 
-// Workspace of the prompt kernel: two words per tile of rows that several CTAs share, then their partial results.
+// Workspace of the prompt kernel: two words per part (those of a tile's first part count its parts), then the partial results.  At
+// most kPromptMaxParts CTAs share tiles of rows.
 constexpr int kPromptMaxParts = 160;
 __host__ __device__ constexpr size_t prompt_counter_bytes() { return 256 * 2 * sizeof(uint32_t); }
+static_assert(kPromptMaxParts * 2 * sizeof(uint32_t) <= prompt_counter_bytes(), "a counter for every part");
 size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim);
 cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream);
 
