@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         float &x = s[q][t][2 * h + j];
-                        x = seen ? (kDigits ? x * f * column_factor[j] : x * f) : -INFINITY;
+                        x = seen ? (kDigits ? __fmul_rn(x * f, column_factor[j]) : __fmul_rn(x, f)) : -INFINITY; // (rounded here: the largest minus itself is 0)
                         top[t][j] = fmaxf(top[t][j], x);
                     }
             }

@@ -26,6 +26,12 @@
 // reference m_i is therefore raised only when a score exceeds it by more than 8 (a factor 256, which fp32 sums and bf16 weights
 // carry without loss); the result does not depend on the reference.
 //
+// Rounding of the reference.  m is a rounded product (score times scale), and one fma takes x scale - m from the exact one: all weights
+// of a row carry the factor 2^(what m's rounding cut off), which cancels out as long as it stays inside fp32's range.  From |m| = 2^31
+// on it need not (half a unit of m is 128), so beyond 2^24 a row's products are rounded first, as m was, and the largest becomes
+// exactly m.  int8: in place, in front of the exponentials.  bf16: the tile is done again row by row; the branch that the int8
+// form has costs this one 8 % (8192 tokens, 32 heads: 589 -> 642 us), and no score of a trained model comes near.
+//
 // What bounds it (heads of 128).  128 x 128 scores cost 16384 exponentials at 16 per cycle and SM, 1024 cycles, and two MMAs of
 // 512 cycles each: the two units are needed equally long, and neither can be kept busy all the time (tensor pipe 66 %,
 // exponentials 53 %).  8192 tokens, 32 heads: 575 us = 0.96 PFLOP/s, where the board's power limit holds the clock near 1.55
@@ -60,6 +66,7 @@ constexpr int kFirstConverter = 12, kConverters = 4; // int8
 constexpr int kThreads = 16 * 32;
 constexpr uint32_t kTmemColumns = 512;
 constexpr float kRaise = 8.0f;
+constexpr float kFar = 16777216.0f; // 2^24: references up to here are rounded by at most half a unit (see the header on rounding)
 constexpr int kMaxParts = 16; // of a tile's keys
 // kv heads whose tiles follow each other: the keys and values of eight heads stay in the L2 while their tiles are worked on
 // (8192 tokens, 32 heads: 134 MB in all, 590 us with all heads at a time, 576 with eight)
@@ -180,7 +187,7 @@ struct Work {
 
 // (Not inlined: the registers of the main loop are allotted without it, 584 -> 576 us for 8192 tokens, 32 heads.)
 // One row by plain arithmetic, one warp: for tiles in which a non-finite value stands behind keys that some of the rows do not
-// see (0 x NaN would reach them through the MMA).
+// see (0 x NaN would reach them through the MMA), or in which a reference lies beyond kFar.
 __device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int r, int lane)
 {
     const int D = a.cache.head_dim, t = w.first_token + r / w.group, h = w.head * w.group + r % w.group;
@@ -214,7 +221,7 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int 
             s[i] = q.x * k[i].x + q.y * k[i].y + q.z * k[i].z + q.w * k[i].w;
 #pragma unroll
             for (int d = 16; d; d >>= 1) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], d);
-            s[i] = j + i < end ? s[i] * a.scale : -INFINITY;
+            s[i] = j + i < end ? __fmul_rn(s[i], a.scale) : -INFINITY;
         }
         float mn = m;
 #pragma unroll
@@ -571,6 +578,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         const int sees = exists ? w.sees(row) : 0x7FFFFFFF; // (rows that do not exist: nothing to hide from them)
         const int least = w.sees(w.row0 + t * kTile);       // of the tile's rows
         float m = -INFINITY, l = 0.0f;                      // reference and sum of this row
+        bool far = false;                                   // a reference beyond kFar (int8: of any row of the warp, at present)
         bool ok = true;
         for (int k = 0; k < n_steps[t]; ++k) {
             if (!mbar_spin_bounded(smem_u32(&sh.s_full[t][k & 1]), (k >> 1) & 1, abort_flag, limit)) {
@@ -645,12 +653,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             // (a NaN among the scores, or an infinite one, makes the row NaN as it does by the formula; NaN is kept by max3)
             float peak = max3(max3(top[0], top[1], top[2]), top[3], top[3]) * a.scale;
             if (peak == INFINITY) peak = __int_as_float(0x7FFFFFFF);
+            auto is_far = [&] { return fabsf(m) > kFar && m != -INFINITY; };
             if (k == 0) {
                 m = peak;
+                if (kInt8) far = __any_sync(0xFFFFFFFFu, is_far());
             } else if (__any_sync(0xFFFFFFFFu, !(peak <= m + kRaise))) {
                 const float raised = peak <= m ? m : peak;
                 const float keep = raised == -INFINITY ? 1.0f : exp2_approx(m - raised);
+                if (!kInt8) far = far || is_far();
                 m = raised;
+                if (kInt8) far = __any_sync(0xFFFFFFFFu, is_far());
                 l *= keep;
                 // the P V in front of this step has to be at rest (the next one waits for this step's weights; the one before
                 // it is done, as the scores of this step were issued behind it, so the phase asked for is the current one or
@@ -670,7 +682,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                     tmem_st_32x16(o_col + c, o);
                 }
             }
-            const float nb = m == -INFINITY ? 0.0f : -m;
+            float nb = m == -INFINITY ? 0.0f : -m;
+            if (kInt8 && far) {
+                const float per_unit = 1.0f / a.scale;
+#pragma unroll
+                for (int c = 0; c < kStep; ++c) // (no fma: the product has to be rounded as m was)
+                    u[c / 32][c % 32] = __float_as_uint((__fmul_rn(__uint_as_float(u[c / 32][c % 32]), a.scale) + nb) * per_unit);
+                nb = 0.0f;
+            }
             const float2 scale2 = make_float2(a.scale, a.scale), nb2 = make_float2(nb, nb);
             float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
             const float4 *vs = reinterpret_cast<const float4 *>(sh.scales[j % kScaled][1] + (k & 1) * kStep);
@@ -713,6 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         }
         if (n_steps[t] > 0) ok = ok && mbar_spin_bounded(smem_u32(&sh.o_last[t]), 0, abort_flag, limit);
         tc_fence_after_sync();
+        if (!kInt8 && exists && (far || (fabsf(m) > kFar && m != -INFINITY))) sh.poisoned[t] = 1; // (to be done again, like a poisoned tile)
 
         // ---- the result, or this CTA's part of it --------------------------------------------------------------
         float *ws_parts = reinterpret_cast<float *>(reinterpret_cast<char *>(a.workspace) + prompt_counter_bytes());
