@@ -17,8 +17,8 @@
 // barrier between warps before the end of a pair): the ring keeps loading the next pair's keys while this one's are
 // finished.  Scores are K Q^T (keys are the 16 rows of the instruction, queries its 8 columns) and the output is
 // V^T P^T (16 elements of the head, 8 queries), so that a group of 1 to 8 query heads wastes at most the columns it does not have;
-// P^T changes from accumulator to operand by movmatrix.  The weights enter as two bf16 parts (value and remainder): the
-// tensor cores have time for it, and the result is as exact as fp32 weights would give.
+// P^T changes from accumulator to operand by movmatrix.  The weights enter as two bf16 parts (value and remainder, 16 bits
+// together): the tensor cores have time for it, and beside the rounding of the results to bf16 it does not show.
 //
 // int8 cache: a key's scale multiplies its score, a value's scale its weight.  Values become bf16 exactly (code_pair below, four
 // instructions per two elements, which is what bounds the kernel then).  Keys stay codes: the queries are written as integers of
@@ -484,9 +484,13 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
                         l[t][j] += w[j];
                         if (kInt8) w[j] *= vs;
                     }
-                    const uint32_t x = pack_bf16(w[0], w[1]);
+                    // bf16 values may be infinite: the first part is cut off, not rounded, and the second one positive where the weight
+                    // is, or infinity times the two would be NaN (with a second part of 0 or below)
+                    const uint32_t x = kInt8 ? pack_bf16(w[0], w[1]) : __byte_perm(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632);
                     rest[0] = w[0] - __uint_as_float(x << 16);
                     rest[1] = w[1] - __uint_as_float(x & 0xFFFF0000u);
+                    if (!kInt8)
+                        for (int j = 0; j < 2; ++j) rest[j] = fmaxf(rest[j], w[j] * 0x1p-24f);
                     hi[t][h] = movmatrix(x);
                     lo[t][h] = movmatrix(pack_bf16(rest[0], rest[1]));
                 }

@@ -1,4 +1,4 @@
-"""Attention over the paged cache where one key takes all, at scores of any size."""
+"""Attention over the paged cache where one key takes all (scores of any size) and where a value is infinite."""
 import math
 
 import pytest
@@ -83,3 +83,25 @@ def test_one_key_takes_all_at_scores_of_any_size(heads, kv_heads, head_dim, page
         assert decided.double().mean() > 0.4
         off = (got - want).abs()[decided] - (2.02 * 2.0 ** -8 * want.abs()[decided] + 2.0 ** -134)
         assert torch.all(off <= 0), f"size {size}: {int((~(off <= 0)).any(-1).sum())} of {off.shape[0]} rows are wrong"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("past", [50, 2850])
+@pytest.mark.parametrize("size", [0.0, 1.5])
+@pytest.mark.parametrize("prompt", [False, True])
+def test_an_infinite_value_gives_the_infinity_to_the_tokens_that_see_it(value, past, size, prompt):
+    """Every weight is positive, so the sum is infinite, whatever the weight is (size 0: 1 over the number of keys)."""
+    n, at = past + 150, past + 49
+    s = R.Setup([n, n], 1, 64, 16, 16, seed=63)
+    s.pools[1][s.table[0, at // 16].item(), 0, at % 16, 5] = value
+    counts = [150, 150] if prompt else [1, 1]
+    q = rows(sum(counts), 2, 64, 64, size=size)
+    cu = torch.tensor([0, counts[0], sum(counts)], dtype=torch.int32, device="cuda")
+    got = (B.attend_prompt if prompt else B.attend_decode)(s.cache(), B.KVBatch(s.table, s.kv_lens, cu if prompt else None), q)
+    sees = torch.zeros(sum(counts), dtype=torch.bool, device="cuda")
+    sees[49 if prompt else 0:counts[0]] = True
+    assert torch.all(got[sees][..., 5] == value)
+    assert torch.all(torch.isfinite(got[~sees]))
+    other = [d for d in range(64) if d != 5]
+    assert torch.all(torch.isfinite(got[..., other]))
