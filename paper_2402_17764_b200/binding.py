@@ -560,10 +560,13 @@ class KVCache:
         self._address = ctypes.addressof(self._desc)
 
     def check(self):
-        """Waits for the device and raises if a call met a bad page, length or position; clears the status."""
+        """Waits for the device, whatever streams the calls ran on, and raises if one of them met a bad page, length or position;
+        clears the status."""
+        torch.cuda.synchronize(self.device)
         status = int(self.status.item())
         if status != OK:
             self.status.zero_()
+            torch.cuda.synchronize(self.device)  # (or the next call on another stream could report before it is cleared)
             raise BitLinearError(status, "bitlinear_kv_cache")
 
 
