@@ -516,6 +516,13 @@ def kv_cache_bytes(n_pages: int, kv_heads: int, head_dim: int, page_size: int, b
     return int(load_library().bitlinear_kv_cache_bytes(n_pages, kv_heads, head_dim, page_size, bits))
 
 
+def _wait_for_fills(device):
+    """Waits for what was just filled on the current stream, so that calls on any stream may use it (a capturing stream cannot be
+    waited for: there the fills are part of the graph)."""
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(device).synchronize()
+
+
 class KVCache:
     """bitlinear_kv_cache: a paged cache of keys and values, bf16 (bits 16) or int8 codes with a scale per row (bits 8).
 
@@ -558,6 +565,7 @@ class KVCache:
         self._desc = KVCacheDesc(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(self.status), self.n_pages, self.kv_heads,
                                  head_dim, self.page_size, bits)
         self._address = ctypes.addressof(self._desc)
+        _wait_for_fills(k.device)
 
     def check(self):
         """Waits for the device, whatever streams the calls ran on, and raises if one of them met a bad page, length or position;
@@ -690,7 +698,14 @@ def attend_workspace_bytes(heads: int, kv_heads: int, head_dim: int, prompt: boo
 
 
 def alloc_attend_workspace(heads: int, kv_heads: int, head_dim: int, prompt: bool, device="cuda") -> torch.Tensor:
-    """A workspace for attend_decode (prompt False) or attend_prompt (prompt True), zeroed as its first use needs it."""
+    """A workspace for attend_decode (prompt False) or attend_prompt (prompt True), zeroed as its first use needs it and ready for
+    calls on any stream."""
+    workspace = _attend_workspace(heads, kv_heads, head_dim, prompt, device)
+    _wait_for_fills(workspace.device)
+    return workspace
+
+
+def _attend_workspace(heads, kv_heads, head_dim, prompt, device):
     n = attend_workspace_bytes(heads, kv_heads, head_dim, prompt)
     if n == 0:
         raise BitLinearError(ERR_SHAPE, "bitlinear_attend_workspace_bytes")
@@ -720,7 +735,7 @@ def _attend(prompt: bool, cache: KVCache, batch: KVBatch, q, scale, out, workspa
         out = _empty_rows(T, heads, D, cache.device)
     os_ = _row_stride(out, shape, index, where)
     if workspace is None:
-        workspace = alloc_attend_workspace(heads, cache.kv_heads, D, prompt, cache.device)
+        workspace = _attend_workspace(heads, cache.kv_heads, D, prompt, cache.device)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         _refuse(where, f"the workspace is contiguous and on {cache.device}")
     scale = D ** -0.5 if scale is None else float(scale)

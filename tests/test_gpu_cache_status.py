@@ -4,7 +4,7 @@ import torch
 
 import kv_reference as R
 from paper_2402_17764_b200 import binding as B
-from test_gpu_attention import rows
+from test_gpu_attention import check, error_of, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,49 @@ def test_check_waits_for_calls_on_every_stream(call):
         assert e.value.status == B.ERR_PAGE
         torch.cuda.synchronize()
         assert cache.status.item() == B.OK
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_new_cache_is_ready_for_every_stream(bits):
+    """The current stream is busy when the cache is made: what fills its tensors and its status word there must not come after a
+    call on another stream."""
+    s = R.Setup([40, 40], 2, 64, 16, bits, seed=88)
+    s.table[0, :3] = torch.tensor([0, 1, 2], dtype=torch.int32)
+    s.table[1, 2] = -1
+    kv, side = rows(2, 2, 64, 89), torch.cuda.Stream()
+    B.kv_append(s.cache(), B.KVBatch(s.table[:1], s.kv_lens[:1]), kv[:1], kv[:1])  # (a kernel's first launch loads it and waits)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)
+    cache = B.KVCache(8, 2, 64, page_size=16, bits=bits)
+    B.kv_append(cache, B.KVBatch(s.table[:1], s.kv_lens[:1]), kv[:1], kv[:1], stream=side)
+    torch.cuda.synchronize()
+    stored = kv[0] if bits == 16 else R.codes(kv[0].double())[0]
+    assert torch.equal(cache.v[2, :, 7], stored)
+    torch.cuda._sleep(100_000_000)
+    cache = s.cache()
+    B.kv_append(cache, B.KVBatch(s.table, s.kv_lens), kv, kv, stream=side)
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_PAGE
+
+
+@pytest.mark.parametrize("prompt", [False, True])
+def test_a_new_workspace_is_ready_for_every_stream(prompt):
+    """The same of a workspace: the memory it gets held ones before."""
+    new = [1, 1] if not prompt else [100, 33]
+    cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device="cuda")
+    s = R.Setup([4000, 600], 2, 128, 16, 16, seed=90)
+    cache, batch, q = s.cache(), B.KVBatch(s.table, s.kv_lens, cu if prompt else None), rows(sum(new), 8, 128, 91)
+    out, side = torch.empty(sum(new), 8, 128, dtype=torch.bfloat16, device="cuda"), torch.cuda.Stream()
+    attend = B.attend_prompt if prompt else B.attend_decode
+    attend(cache, batch, q)  # (a kernel's first launch loads it and waits)
+    out.fill_(0.5)
+    stale = torch.full((B.attend_workspace_bytes(8, 2, 128, prompt),), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    del stale
+    torch.cuda._sleep(100_000_000)
+    ws = B.alloc_attend_workspace(8, 2, 128, prompt=prompt)
+    attend(cache, batch, q, out=out, workspace=ws, stream=side)
+    cache.check()
+    want, bound = R.attend(s, q, new, **error_of(prompt, 16))
+    check(out, want, bound)
