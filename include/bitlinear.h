@@ -326,7 +326,8 @@ void bitlinear_sequence_destroy(bitlinear_sequence *seq);
  * `status` (device, one int32, set to 0 by the owner) receives BITLINEAR_ERR_PAGE when a call met a page number outside
  * 0 .. n_pages - 1, a length beyond table_pages * page_size, or a position beyond the rotary table: nothing is read or
  * written there (what that does to the results is said at each call).  BITLINEAR_ERR_TIMEOUT: a bounded wait of
- * bitlinear_attend_prompt expired, its results are unspecified.  The word keeps the code until the owner clears it.
+ * bitlinear_attend_prompt expired, its results are unspecified.  The word keeps its code until the owner clears it; only
+ * BITLINEAR_ERR_TIMEOUT replaces BITLINEAR_ERR_PAGE.
  */
 typedef struct {
     void *k, *v;             /* device, bitlinear_kv_cache_bytes(...) bytes each, 16-byte aligned */

@@ -449,13 +449,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                         if (pos < w.len) {
                             const int page = kv_page(a.cache, a.batch, w.b, pos);
                             bad = page < 0;
-                            if (bad)
-                                kv_report(a.cache);
-                            else
-                                row = kv_row(a.cache, page, w.head, pos);
+                            if (!bad) row = kv_row(a.cache, page, w.head, pos);
                         }
                     }
                     const uint32_t bad_groups = __ballot_sync(0xFFFFFFFFu, bad);
+                    if (bad_groups != 0u && lane == 0) kv_report(a.cache);
                     if (round > 0 && !mbar_wait_bounded(smem_u32(empty_bar), (round - 1) & 1, abort_flag, limit)) break;
                     if (!values && lane == 0) sh.bad_groups[(i / 2) % kInfo] = bad_groups;
                     const uint32_t full = smem_u32(full_bar);
@@ -860,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     tc_fence_before_sync();
     __syncthreads();
     if (*abort_flag) {
-        if (tid == 0) atomicExch(a.cache.status, (int32_t)BITLINEAR_ERR_TIMEOUT);
+        if (tid == 0) atomicMax(reinterpret_cast<uint32_t *>(a.cache.status), (uint32_t)BITLINEAR_ERR_TIMEOUT); // (see kv_report)
         // give copies and MMAs that may still be in flight time to land before shared and tensor memory go away
         const uint64_t t0 = globaltimer_ns();
         while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);

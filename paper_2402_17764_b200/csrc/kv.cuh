@@ -33,8 +33,10 @@ struct KvBatch {
     int64_t table_stride;
 };
 
-// Reports a bad page, length or position.
-__device__ __forceinline__ void kv_report(const KvCache &c) { *c.status = BITLINEAR_ERR_PAGE; }
+// Reports a bad page, length, position or token row.  An expired wait, which says more, stays where it is: its code is the larger
+// one of the two as unsigned numbers, and both are larger than BITLINEAR_OK.
+static_assert((uint32_t)BITLINEAR_ERR_TIMEOUT > (uint32_t)BITLINEAR_ERR_PAGE, "a timeout is not replaced");
+__device__ __forceinline__ void kv_report(const KvCache &c) { atomicMax(reinterpret_cast<uint32_t *>(c.status), (uint32_t)BITLINEAR_ERR_PAGE); }
 
 // The length of sequence b, cut to what its row of the page table covers; over_long: it was cut.
 __host__ __device__ __forceinline__ int kv_length(const KvBatch &s, int b, bool &over_long)

@@ -80,3 +80,29 @@ def test_a_new_workspace_is_ready_for_every_stream(prompt):
     cache.check()
     want, bound = R.attend(s, q, new, **error_of(prompt, 16))
     check(out, want, bound)
+
+
+def test_a_bad_page_does_not_replace_an_expired_wait():
+    """The word keeps its code until the owner clears it: a timeout, which leaves results unspecified, is not made to look like
+    a page by the calls behind it."""
+    s = R.Setup([200, 40], 1, 64, 16, 16, seed=74)
+    q = rows(60, 2, 64, 75)
+    cu = torch.tensor([0, 60, 60], dtype=torch.int32, device="cuda")
+    cache = s.cache()
+    ws = B.alloc_attend_workspace(2, 1, 64, prompt=True)
+    B.attend_prompt(cache, B.KVBatch(s.table, s.kv_lens, cu), q, workspace=ws)
+    cache.check()
+    B.test_expire_next_wait(2000, True)
+    B.attend_prompt(cache, B.KVBatch(s.table, s.kv_lens, cu), q, workspace=ws)
+    s.table[1, 1] = -1
+    one, kv = rows(2, 2, 64, 76), rows(2, 1, 64, 77)
+    s.kv_lens[1] = 20
+    B.attend_decode(cache, B.KVBatch(s.table, s.kv_lens), one)
+    B.kv_append(cache, B.KVBatch(s.table, s.kv_lens), kv, kv)
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_TIMEOUT
+    B.attend_decode(cache, B.KVBatch(s.table, s.kv_lens), one)
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_PAGE
