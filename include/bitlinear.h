@@ -53,9 +53,9 @@ enum {
     BITLINEAR_ERR_RANGE = -8,     /* a weight was non-finite or >= 2^24 in magnitude (reported on the device, as
                                      gamma = NaN; no call returns this code) */
     BITLINEAR_ERR_BADCODE = -9,   /* bitlinear_validate_packed found the 2-bit code 3, which no weight has */
-    BITLINEAR_ERR_PAGE = -10      /* a page number, a sequence length or a position outside what the cache, the page table
-                                     or the rotary table holds (reported on the device, in bitlinear_kv_cache.status; no
-                                     call returns this code) */
+    BITLINEAR_ERR_PAGE = -10      /* a page number, a sequence length, a position or token rows outside what the cache, the page
+                                     table, the rotary table or the call's rows hold (reported on the device, in
+                                     bitlinear_kv_cache.status; no call returns this code) */
 };
 
 /* Matmul code paths selectable through the test hook bitlinear_matmul_i32. */
@@ -324,8 +324,8 @@ void bitlinear_sequence_destroy(bitlinear_sequence *seq);
  *   head_dim a multiple of 4, 4 .. 128;  kv_heads 1 .. 1024;  page_size 16, 32, 64, 128 or 256;  n_pages >= 1 with
  *   n_pages * kv_heads * page_size < 2^31
  * `status` (device, one int32, set to 0 by the owner) receives BITLINEAR_ERR_PAGE when a call met a page number outside
- * 0 .. n_pages - 1, a length beyond table_pages * page_size, or a position beyond the rotary table: nothing is read or
- * written there (what that does to the results is said at each call).  BITLINEAR_ERR_TIMEOUT: a bounded wait of
+ * 0 .. n_pages - 1, a length beyond table_pages * page_size, a position beyond the rotary table, or token rows outside 0 .. T - 1:
+ * nothing is read or written there (what that does to the results is said at each call).  BITLINEAR_ERR_TIMEOUT: a bounded wait of
  * bitlinear_attend_prompt expired, its results are unspecified.  The word keeps its code until the owner clears it; only
  * BITLINEAR_ERR_TIMEOUT replaces BITLINEAR_ERR_PAGE.
  */
@@ -340,8 +340,10 @@ typedef struct {
 /*
  * The sequences of a call.  kv_lens[b] is the length of sequence b WITH the call's new tokens: the i-th of its n new tokens
  * has position kv_lens[b] - n + i.  cu_tokens [n_seqs + 1] holds the rows of the new tokens: those of sequence b are
- * cu_tokens[b] .. cu_tokens[b + 1] - 1 (0 <= cu_tokens[b] <= cu_tokens[b + 1]); NULL: one token per sequence, row b.  Rows
- * behind cu_tokens[n_seqs] (a padded batch) are left as they are.  A token whose position is negative (kv_lens[b] < n:
+ * cu_tokens[b] .. cu_tokens[b + 1] - 1 (0 <= cu_tokens[b] <= cu_tokens[b + 1] <= T); NULL: one token per sequence, row b.  Rows
+ * behind cu_tokens[n_seqs] (a padded batch) are left as they are.  Where rows of a sequence lie outside 0 .. T - 1,
+ * bitlinear_kv_append stores those that exist, bitlinear_attend_prompt computes none of them, and both set the status (T > 0; of
+ * bounds that fall only bitlinear_attend_prompt takes notice).  A token whose position is negative (kv_lens[b] < n:
  * 0 for an empty slot of a batch) is not stored and sees nothing.  All three arrays are read on the device, so a captured
  * graph follows their contents.
  *   0 <= n_seqs <= 2^20;  1 <= table_pages <= table_stride;  table_pages * page_size <= 2^30

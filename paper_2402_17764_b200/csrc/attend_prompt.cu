@@ -274,10 +274,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             const int64_t n = (int64_t)a.batch.cu_tokens[b + 1] - a.batch.cu_tokens[b];
             return n <= 0 || n > a.T ? 0 : (n * group + kRows - 1) / kRows * a.cache.kv_heads;
         };
+        // (rows that the caller did not hand over: the sequence has none then, here or where its first row is looked at below)
+        auto rows_missing = [&](int b) { return a.batch.cu_tokens[b] < 0 || a.batch.cu_tokens[b] > a.batch.cu_tokens[b + 1] || a.batch.cu_tokens[b + 1] > a.T; };
         const int per_thread = (n_seqs + kThreads - 1) / kThreads;
         const int b0 = min(n_seqs, tid * per_thread), b1 = min(n_seqs, b0 + per_thread);
         int64_t mine = 0;
-        for (int b = b0; b < b1; ++b) mine += tiles_of(b);
+        for (int b = b0; b < b1; ++b) {
+            mine += tiles_of(b);
+            if (blockIdx.x == 0 && rows_missing(b)) kv_report(a.cache);
+        }
         int first_b = b0;
         if (per_thread == 1) { // (longer lists of sequences are taken as they are)
             int64_t *tiles_by_rank = reinterpret_cast<int64_t *>(smem);
@@ -337,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     w.group = group;
     w.first_token = a.batch.cu_tokens[w.b];
     const int n_tokens = a.batch.cu_tokens[w.b + 1] - w.first_token;
-    if (w.first_token < 0 || (int64_t)w.first_token + n_tokens > a.T) return; // (rows that the caller did not hand over)
+    if (w.first_token < 0 || (int64_t)w.first_token + n_tokens > a.T) return; // (reported above)
     w.rows = n_tokens * group;
     {
         const int tiles = (w.rows + kRows - 1) / kRows;

@@ -207,7 +207,7 @@ const char *bitlinear_status_string(bitlinear_status s)
     case BITLINEAR_ERR_CUDA: return "CUDA call failed";
     case BITLINEAR_ERR_TIMEOUT: return "device-side wait timed out";
     case BITLINEAR_ERR_RANGE: return "weight out of range";
-    case BITLINEAR_ERR_PAGE: return "page, length or position out of range";
+    case BITLINEAR_ERR_PAGE: return "page, length, position or token row out of range";
     case BITLINEAR_ERR_BADCODE: return "packed weights hold the unused 2-bit code";
     default: return "unknown status";
     }

@@ -103,6 +103,8 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
     const int lane = threadIdx.x % kLanes, group = threadIdx.x % 32 / kLanes;
     if (t >= a.T) return;
 
+    // rows that the caller did not hand over (those of the same sequence that exist are stored)
+    if (a.batch.cu_tokens && ((t == 0 && a.batch.cu_tokens[0] < 0) || (t == a.T - 1 && a.batch.cu_tokens[a.batch.n_seqs] > a.T))) kv_report(a.cache);
     int first, count;
     const int b = kv_sequence_of(a.batch, t, first, count);
     if (b < 0) return;

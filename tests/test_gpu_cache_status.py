@@ -4,7 +4,7 @@ import torch
 
 import kv_reference as R
 from paper_2402_17764_b200 import binding as B
-from test_gpu_attention import check, error_of, rows
+from test_gpu_attention import WEIGHT_BF16, check, error_of, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,64 @@ def test_a_bad_page_does_not_replace_an_expired_wait():
     with pytest.raises(B.BitLinearError) as e:
         cache.check()
     assert e.value.status == B.ERR_PAGE
+
+
+# bounds of two sequences of a call with five token rows; the rows of each that attend_prompt and kv_append serve
+ROWS = [
+    ([0, 4, 9], [range(0, 4), []], [range(0, 4), range(4, 5)]),
+    ([0, 4, 2 ** 31 - 1], [range(0, 4), []], [range(0, 4), range(4, 5)]),
+    ([0, 7, 7], [[], []], [range(0, 5), []]),
+    ([-3, 2, 5], [[], range(2, 5)], [range(0, 2), range(2, 5)]),
+    ([0, 5, 6], [range(0, 5), []], [range(0, 5), []]),
+    ([-2, 0, 5], [[], range(0, 5)], [[], range(0, 5)]),
+]
+
+
+@pytest.mark.parametrize("cu,attended,appended", ROWS)
+@pytest.mark.parametrize("bits", [16, 8])
+def test_sequences_whose_rows_were_not_all_handed_over_are_reported(cu, attended, appended, bits):
+    """attend_prompt leaves such a sequence out, kv_append stores the rows that it was given; both say so."""
+    s = R.Setup([30, 21], 2, 64, 16, bits, seed=78)
+    bounds = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    batch, cache = B.KVBatch(s.table, s.kv_lens, bounds), s.cache()
+    q, out = rows(5, 4, 64, 79), torch.full((5, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    B.attend_prompt(cache, batch, q, out=out)
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_PAGE
+    served = [t for b in (0, 1) for t in attended[b]]
+    for b in (0, 1):
+        if len(attended[b]):
+            alone = [0, 0]
+            alone[b] = len(attended[b])
+            want, bound = R.attend(s, q[list(attended[b])], alone, weight_rounding=WEIGHT_BF16)
+            check(out[list(attended[b])], want, bound)
+    assert torch.all(out[[t for t in range(5) if t not in served]] == 3.0)
+
+    kv = rows(5, 2, 64, 80)
+    before = s.pools[1].clone()
+    B.kv_append(cache, batch, kv, kv)
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_PAGE
+    expected = before.clone()
+    for b in (0, 1):
+        for t in appended[b]:
+            pos = s.lens[b] - (cu[b + 1] - cu[b]) + t - cu[b]
+            if pos >= 0:
+                value = kv[t] if bits == 16 else R.codes(kv[t].double())[0]
+                expected[s.table[b, pos // 16].item(), :, pos % 16] = value
+    kind = torch.int16 if bits == 16 else torch.int8
+    assert torch.equal(s.pools[1].view(kind), expected.view(kind))
+
+
+@pytest.mark.parametrize("cu", [[0, 3, 3], [0, 0, 2], [1, 3, 5]])
+def test_rows_behind_the_last_sequence_and_in_front_of_the_first_are_no_error(cu):
+    s = R.Setup([30, 21], 2, 64, 16, 16, seed=81)
+    cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens, torch.tensor(cu, dtype=torch.int32, device="cuda"))
+    out = torch.full((5, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    kv = rows(5, 2, 64, 82)
+    B.kv_append(cache, batch, kv, kv)
+    B.attend_prompt(cache, batch, rows(5, 4, 64, 83), out=out)
+    cache.check()
+    assert torch.all(out[:cu[0]] == 3.0) and torch.all(out[cu[2]:] == 3.0)
