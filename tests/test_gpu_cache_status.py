@@ -1,4 +1,4 @@
-"""What the cache's status word reports, and when."""
+"""What the cache's status word reports, when, and what a call does with pages, lengths and token rows that do not exist."""
 import pytest
 import torch
 
@@ -167,3 +167,83 @@ def test_rows_behind_the_last_sequence_and_in_front_of_the_first_are_no_error(cu
     B.attend_prompt(cache, batch, rows(5, 4, 64, 83), out=out)
     cache.check()
     assert torch.all(out[:cu[0]] == 3.0) and torch.all(out[cu[2]:] == 3.0)
+
+
+def attend_without(s, b, dropped, q, length, prompt, bits):
+    """(out, bound) of the new tokens q of sequence b over its keys but those of the dropped pages, the last token at length - 1.
+    The bound is that of kv_reference.attend, with the keys that are left as the only ones."""
+    n, H, D = q.shape
+    G = H // s.kv_heads
+    k, v = s.rows(0, b, length), s.rows(1, b, length)
+    gone = torch.zeros(length, dtype=torch.bool, device=q.device)
+    for p in dropped:
+        gone[p * s.page_size:(p + 1) * s.page_size] = True
+    scale = D ** -0.5
+    x = q.double().reshape(n, s.kv_heads, G, D).permute(1, 2, 0, 3)
+    score, size = scale * torch.einsum("hgnd,hld->hgnl", x, k), scale * torch.einsum("hgnd,hld->hgnl", x.abs(), k.abs())
+    hidden = gone[None] | (torch.arange(length, device=q.device)[None] > (length - n + torch.arange(n, device=q.device))[:, None])
+    w = torch.softmax(score.masked_fill(hidden, -float("inf")), -1).nan_to_num(0.0)
+    y, A = torch.einsum("hgnl,hld->hgnd", w, v), torch.einsum("hgnl,hld->hgnd", w, v.abs())
+    e = error_of(prompt, bits)
+    worst = size.masked_fill(hidden, 0.0).amax(-1, keepdim=True) * (D + 4) * 2.0 ** -24
+    fixed = scale * x.abs().amax(-1)[..., None] * k.abs().sum(-1)[:, None, None]
+    worst = worst + e.get("query_rounding", 0.0) * fixed.masked_fill(hidden, 0.0).amax(-1, keepdim=True)
+    d = 2 * worst + 2.0 ** -21 + e["weight_rounding"] + (length + 64) * 2.0 ** -24
+    bound = 1.01 * 2 * d * A + 2.0 ** -8 * y.abs() + 2.0 ** -134 + length * 2.0 ** -119 * max(1.0, v.abs().max().item())
+    return y.permute(2, 0, 1, 3).reshape(n, H, D), bound.permute(2, 0, 1, 3).reshape(n, H, D)
+
+
+@pytest.mark.parametrize("prompt", [False, True])
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("heads,kv_heads,head_dim,page,length,new,dropped", [
+    (4, 2, 64, 16, 130, 30, [3]),
+    (4, 2, 64, 16, 130, 30, [0, 7]),    # a page inside the new tokens: some of them do not see it
+    (4, 1, 64, 16, 130, 130, [0]),      # the first 16 tokens are left with nothing
+    (2, 2, 100, 32, 200, 40, [1, 2]),
+    (8, 1, 128, 64, 300, 20, [4]),      # the last, partial page
+    (2, 1, 128, 256, 700, 60, [1]),     # two whole blocks of keys
+    (2, 2, 64, 16, 3000, 20, [5, 90, 187]),  # split among several CTAs
+])
+@pytest.mark.parametrize("size", [1.5, 30.0])
+def test_keys_of_bad_pages_alone_are_missing(heads, kv_heads, head_dim, page, length, new, dropped, bits, prompt, size):
+    """The keys of those pages are the largest ones: they would take over where they took part.  Also with a sharp softmax, which
+    shows single keys that are lost."""
+    s = R.Setup([50, length], kv_heads, head_dim, page, bits, seed=84)
+    for p in dropped:
+        (s.pools if bits == 16 else s.scales)[0][s.table[1, p].item()] *= 4.0
+    n = new if prompt else 1
+    q = rows(20 + n if prompt else 2, heads, head_dim, 85, size=size)
+    counts = [20, n] if prompt else [1, 1]
+    cu = torch.tensor([0, counts[0], sum(counts)], dtype=torch.int32, device="cuda")
+    table = s.table.clone()
+    for p, bad in zip(dropped, (s.n_pages, -1, 2 ** 31 - 1)):
+        table[1, p] = bad
+    cache = s.cache()
+    got = (B.attend_prompt if prompt else B.attend_decode)(cache, B.KVBatch(table, s.kv_lens, cu if prompt else None), q)
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_PAGE
+    want, bound = attend_without(s, 1, dropped, q[counts[0]:], length, prompt, bits)
+    check(got[counts[0]:], want, bound)
+    want, bound = attend_without(s, 0, [], q[:counts[0]], 50, prompt, bits)
+    check(got[:counts[0]], want, bound)
+
+
+@pytest.mark.parametrize("prompt", [False, True])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_length_beyond_the_table_counts_as_far_as_the_table_goes(prompt, bits):
+    """Every key that the table covers takes part; the tokens behind it see all of them, those inside it their own part."""
+    s = R.Setup([128], 2, 64, 16, bits, seed=86, table_extra=0)
+    n = 40 if prompt else 1
+    over = 25
+    q = rows(n, 4, 64, 87)
+    s.kv_lens[0] = 128 + over
+    cache, cu = s.cache(), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    got = (B.attend_prompt if prompt else B.attend_decode)(cache, B.KVBatch(s.table, s.kv_lens, cu if prompt else None), q)
+    with pytest.raises(B.BitLinearError) as e:
+        cache.check()
+    assert e.value.status == B.ERR_PAGE
+    for i in range(n):  # the token at position 128 + over - n + i
+        sees = min(128, 128 + over - n + i + 1)
+        want, bound = attend_without(s, 0, [], q[i:i + 1], sees, prompt, bits)
+        check(got[i:i + 1], want, bound)
