@@ -312,7 +312,8 @@ void bitlinear_sequence_destroy(bitlinear_sequence *seq);
  * names it and gives no formula; this is the textbook one), a paged cache of keys and values, in bf16 or in 8 bits (the
  * outlook of Section 4 on long sequences expects 8-bit activations and with them a cache of half the size), and the softmax
  * attention over it.  Queries, keys and values are what the BitLinear projections wrote: bf16 [tokens, heads, head_dim]
- * with any row stride (a multiple of 8 elements, at least heads * head_dim), e.g. slices of one fused q/k/v output.
+ * with any row stride (a multiple of 8 elements, at least heads * head_dim), e.g. slices of one fused q/k/v output.  Each of
+ * q, k, v, q_out and out starts on a 16-byte boundary.
  *
  * The cache.  Row (page, h, slot) of `k` and `v` holds the key and the value of one token for kv head h: W = head_dim
  * rounded up to a multiple of 16 elements (the elements behind head_dim are 0: bitlinear_kv_append writes them so, and
@@ -403,7 +404,9 @@ size_t bitlinear_attend_workspace_bytes(int heads, int kv_heads, int head_dim, i
  * Sums, maxima and the softmax's denominators are fp32.  Roundings to fewer bits: the prompt kernel rounds the weights to
  * bf16 before they meet the values; the decode kernel splits them into two bf16 parts (16 bits) and, over an 8-bit cache, takes
  * the queries to integers of 22 bits relative to the row's largest element; the results are rounded to bf16.  A token that
- * sees nothing (an empty slot) gets zeros.  Keys on a bad page, or behind the page table, take no part and the status is
+ * sees nothing (an empty slot) gets zeros, and so does one whose scores are all -infinity.  A score beyond fp32's range counts
+ * as infinite, and one that is NaN or +infinity makes the result NaN.  A value that is NaN or infinite reaches those tokens alone
+ * that see it (as NaN where its weight is below 2^-126).  Keys on a bad page, or behind the page table, take no part and the status is
  * set.  Calls with the same arguments on the same contents give the same bits.
  */
 bitlinear_status bitlinear_attend_decode(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q,

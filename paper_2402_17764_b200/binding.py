@@ -568,8 +568,8 @@ class KVCache:
         _wait_for_fills(k.device)
 
     def check(self):
-        """Waits for the device, whatever streams the calls ran on, and raises if one of them met a bad page, length or position;
-        clears the status."""
+        """Waits for the device, whatever streams the calls ran on, and raises if one of them met a bad page, length, position or
+        token row; clears the status."""
         torch.cuda.synchronize(self.device)
         status = int(self.status.item())
         if status != OK:

@@ -25,10 +25,10 @@
 // 23 bits, relative to the power of two above their row's largest, in three signed bytes, and the scores are exact
 // integer products of codes and bytes (three MMAs of twice the depth instead of 16 conversions per MMA).
 //
-// Measured: 128k tokens of one sequence, 64/8 heads: 94 us = 5.7 TB/s (0.87 of a copy's rate); 32 sequences of 1 to 4096 tokens,
-// 32 heads: 46 us = 5.2 TB/s; int8, 128 sequences of 256 to 8192 tokens, 64/8 heads: 150 us = 4.8 TB/s (issue slots 57 %
-// busy, and what they wait for is the chain from a stage's codes to its output); one sequence of 777 tokens, 32 heads of
-// 100: 9.4 us per call, a chain of dependent loads and the join of its parts.
+// Measured: 128k tokens of one sequence, 64/8 heads: 94-95 us = 5.7 TB/s (0.86 of a copy's rate); 32 sequences of 1 to 4096 tokens,
+// 32 heads: 46.5 us = 5.2 TB/s; int8, 128 sequences of 256 to 8192 tokens, 64/8 heads: 157-159 us = 4.5 TB/s (issue slots 57 %
+// busy, so not at a limit; what they wait for is the chain from a stage's codes to its output); one sequence of 777 tokens, 32
+// heads of 100: 9.5 us per call, a chain of dependent loads and the join of its parts.
 #include <algorithm>
 
 #include "internal.cuh"
@@ -49,7 +49,7 @@ constexpr int kMaxSplits = 2;     // partial results of a CTA: of the pair it be
 template <bool kInt8, int WT, int NT>
 struct Shape {
     // int8 keys stay codes and need fewer registers, and the conversion of the values more warps to hide its latency: three
-    // CTAs of two stages per warp instead of two CTAs of three (128 sequences, 64/8 heads: 158 -> 144 us)
+    // CTAs of two stages per warp instead of two CTAs of three (128 sequences, 64/8 heads: 167 -> 158 us)
     static constexpr int kCtas = kInt8 && NT == 1 ? 3 : 2; // per SM
     static constexpr int kRowBytes = WT * (kInt8 ? 1 : 2);
     static constexpr int kKeys = kStageBytes / 2 / kRowBytes; // of a stage: 16, 32 or 64

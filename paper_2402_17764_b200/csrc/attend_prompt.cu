@@ -24,7 +24,8 @@
 //
 // Rescaling.  The output stands in tensor memory, and moving it for every new maximum would cost as much as the softmax.  The
 // reference m_i is therefore raised only when a score exceeds it by more than 8 (a factor 256, which fp32 sums and bf16 weights
-// carry without loss); the result does not depend on the reference.
+// carry without loss); the result does not depend on the reference.  (A known refinement of the softmax in one pass, whose running
+// maximum and sum are Milakov and Gimelshein's, "Online normalizer calculation for softmax", 2018.)
 //
 // Rounding of the reference.  m is a rounded product (score times scale), and one fma takes x scale - m from the exact one: all weights
 // of a row carry the factor 2^(what m's rounding cut off), which cancels out as long as it stays inside fp32's range.  From |m| = 2^31
@@ -32,12 +33,15 @@
 // exactly m.  int8: in place, in front of the exponentials.  bf16: the tile is done again row by row; the branch that the int8
 // form has costs this one 8 % (8192 tokens, 32 heads: 589 -> 642 us), and no score of a trained model comes near.
 //
-// What bounds it (heads of 128).  128 x 128 scores cost 16384 exponentials at 16 per cycle and SM, 1024 cycles, and two MMAs of
-// 512 cycles each: the two units are needed equally long, and neither can be kept busy all the time (tensor pipe 66 %,
-// exponentials 53 %).  8192 tokens, 32 heads: 575 us = 0.96 PFLOP/s, where the board's power limit holds the clock near 1.55
-// GHz (the same launch takes about 930 000 cycles at any clock).  int8: the converters' shared-memory traffic and arithmetic come on
-// top, 60 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 380 us = 0.77 PFLOP/s).
+// What bounds it (heads of 128).  64 keys for 256 rows cost 16384 exponentials at 16 per cycle and SM, 1024 cycles, and 1280 cycles of
+// the tensor pipe: P V 512, and Q K^T 768 instead of 512, because an MMA of 64 columns reads 4 KB of queries and 2 KB of keys from
+// shared memory, at 128 bytes per cycle, for 32 cycles of arithmetic.  They take about 2040: neither unit is busy all the time
+// (tensor pipe 67 %, exponentials 53 %), since a softmax warp loads its scores, finds their maximum and only then begins its
+// exponentials.  8192 tokens, 32 heads: 586-594 us = 0.93 PFLOP/s, where the board's power limit holds the clock near 1.55 GHz
+// (the same launch takes about 930 000 cycles at any clock).  int8: the converters' shared-memory traffic and arithmetic come on
+// top, 57 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 393-401 us = 0.74 PFLOP/s).
 // Prompts of few hundred tokens: half the time is each tile's beginning and end (pages, queries, first scores; results).
+// Registers: the bf16 form spills 4 bytes (12 loaded), the int8 form none.
 #include <cuda.h>
 
 #include <algorithm>
@@ -69,7 +73,8 @@ constexpr float kRaise = 8.0f;
 constexpr float kFar = 16777216.0f; // 2^24: references up to here are rounded by at most half a unit (see the header on rounding)
 constexpr int kMaxParts = 16; // of a tile's keys
 // kv heads whose tiles follow each other: the keys and values of eight heads stay in the L2 while their tiles are worked on
-// (8192 tokens, 32 heads: 134 MB in all, 590 us with all heads at a time, 576 with eight)
+// (8192 tokens, 32 heads: 134 MB in all, 590 us with all heads at a time, 576 with eight; at 128k tokens eight heads are
+// 0.5 GB and do not stay there either, and of short prompts all heads would)
 constexpr int kHeadGroup = 8;
 template <bool kInt8>
 struct Shared {
@@ -924,13 +929,15 @@ cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream)
     p.hooks = take_wait_hooks();
     if (!a.cache.k_scale && (!encode_cache_map(&p.k_map, a.cache.k, a.cache) || !encode_cache_map(&p.v_map, a.cache.v, a.cache)))
         return cudaErrorInvalidValue;
-    // No more tiles of rows than this can exist: every sequence has at most one that is not full.
+    // No more tiles of rows than this can exist: every sequence has at most one that is not full.  (Of one sequence whose rows fill
+    // their tiles exactly this is one per kv head too many: some CTAs find no tile, and the keys of the others are split less.)
     const int64_t group = a.heads / a.cache.kv_heads;
     const int64_t tiles = ((int64_t)a.T * group / kRows + std::min<int64_t>(a.batch.n_seqs, a.T)) * a.cache.kv_heads;
-    // With fewer tiles than SMs the keys of a tile are split among several CTAs, as many as run at the same time (2 tokens behind
+    // With fewer tiles than SMs the keys of a tile are split among several CTAs, no more than run at the same time (2 tokens behind
     // 10994, 32 heads of 100: with five CTAs for each of the 32 tiles twelve had to wait for an SM, 87 us; with four 57).  Of
     // several sequences only the device knows how many tiles they have (5 sequences of 50 tokens behind 4000, 24/8 heads
-    // of 64: 48 -> 42 us against the bound above).
+    // of 64: 48 -> 42 us against the bound above); it is asked where the bound is below the number of SMs, so a batch with many
+    // empty slots is not split.
     const int slots = std::min(sm_count(), kPromptMaxParts);
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxParts, slots / tiles));
     p.slots = a.batch.n_seqs > 1 && tiles < slots ? slots : 0;

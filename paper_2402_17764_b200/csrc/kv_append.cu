@@ -4,8 +4,9 @@
 // A pair (a, b) of a head becomes (a c - b s, b c + a s) with (c, s) of its position and its place i in the head.  Every
 // (token, head) is one group of lanes: 8 lanes with 16-byte pieces where the head is a multiple of 16 elements, a warp with
 // 4-byte pieces otherwise (the 100-wide heads of the 3B shape are only 8-byte aligned).  A lane holds both halves of
-// its pairs, so nothing but the 8-bit cache's row maximum crosses lanes.  A CTA serves one token: its sequence, position, page
-// and angles are looked up once, and its groups walk the token's heads; with few tokens several CTAs share a token.
+// its pairs, so nothing but the 8-bit cache's row maximum crosses lanes.  A warp serves one token: its sequence, position, page
+// and angles are looked up once, and its groups walk the token's heads; with few tokens several warps share a token.  The warps
+// of a CTA may serve different tokens.
 //
 // 8 bits: code = round(127 x / beta) has to come out as in exact arithmetic, also for values half way between two codes.  All is
 // done in fp32 first; the few elements that fp32 cannot settle (candidates for the row's maximum, quotients near the
@@ -13,9 +14,10 @@
 // low bytes of the sums (conversions go through a unit a quarter as wide: 2436 tokens, 40/40 heads: 52 -> 46 us with it).
 //
 // What bounds it: memory (every byte read and written once) for prompts, the launch and one chain of dependent loads
-// (length, page number, row) for a decode step.  Measured: 4096 tokens, 64/8 heads of 128: 32.5 us = 5.2 TB/s (0.79 of a copy's
-// rate); single tokens 8.4 us per call, the time the host needs for one; int8, 2436 tokens, 40/40 heads: 46 us = 2.8 TB/s,
-// bound by instructions (row maxima, quotients and the test that settles each code).
+// (length, page number, row) for a decode step.  Measured: 4096 tokens, 64/8 heads of 128: 32.2 us = 5.3 TB/s (0.80 of a copy's
+// rate); heads of 100, 32/32 of them: 57 us = 2.8 TB/s, held by the 4-byte accesses; single tokens 8.4 us per call, the time the
+// host needs for one; int8, 2436 tokens, 40/40 heads: 46 us = 2.8 TB/s: issue slots 66 % busy (row maxima, quotients and the test
+// that settles each code), not at a limit.  Registers: nothing is spilled but 4 bytes in the rotating int8 form of 4-byte pieces.
 #include <math.h>
 
 #include <algorithm>
