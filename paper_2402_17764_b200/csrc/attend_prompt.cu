@@ -256,7 +256,6 @@ template <bool kInt8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args)
 {
     griddep_wait(); // everything below is read from memory that the launch before this one may have written
-    if (kInt8) griddep_launch_dependents();
     const AttendArgs &a = args.a;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -740,6 +739,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         }
         if (n_steps[t] > 0) ok = ok && mbar_spin_bounded(smem_u32(&sh.o_last[t]), 0, abort_flag, limit);
         tc_fence_after_sync();
+        // The next launch may start when all tiles are at their ends, not before: what it lets in early in its turn may be a matmul,
+        // whose bounded waits would run while a long tile is worked on.  (bf16: below, when no row has to be done again.)
+        if (kInt8 && tid == 0) griddep_launch_dependents();
         if (!kInt8 && exists && (far || (fabsf(m) > kFar && m != -INFINITY))) sh.poisoned[t] = 1; // (to be done again, like a poisoned tile)
 
         // ---- the result, or this CTA's part of it --------------------------------------------------------------

@@ -247,3 +247,34 @@ def test_a_length_beyond_the_table_counts_as_far_as_the_table_goes(prompt, bits)
         sees = min(128, 128 + over - n + i + 1)
         want, bound = attend_without(s, 0, [], q[i:i + 1], sees, prompt, bits)
         check(got[i:i + 1], want, bound)
+
+
+@pytest.mark.parametrize("tokens", [3, 40, 130])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_long_prompt_does_not_use_up_the_waits_of_the_matmul_behind_it(bits, tokens):
+    """A tile over 2^24 keys takes several ms.  The matmul launched next, whose waits are allowed 1 ms here, may not be resident
+    meanwhile: its quantiser lets it in early, but is itself let in by the prompt kernel only when that is at its end."""
+    from paper_2402_17764_b200 import synthetic as S
+    keys, N, K = 1 << 24, 512, 1536
+    cache = B.KVCache(keys // 256, 1, 4, page_size=256, bits=bits)
+    table = torch.arange(keys // 256, dtype=torch.int32, device="cuda")[None]
+    batch = B.KVBatch(table, torch.tensor([keys], dtype=torch.int32, device="cuda"), torch.tensor([0, 256], dtype=torch.int32, device="cuda"))
+    q, out, ws = rows(256, 1, 4, 92), rows(256, 1, 4, 93), B.alloc_attend_workspace(1, 1, 4, prompt=True)
+    packed, gamma = B.quantize_weights(S.latent_weights(N, K, 1).cuda())
+    X, Y, matmul_ws = S.activations(tokens, K, 2).cuda(), torch.empty(tokens, N, dtype=torch.bfloat16, device="cuda"), B.alloc_workspace(tokens, N, K)
+    B.forward(packed, gamma, X, N, workspace=matmul_ws, Y=Y)
+    want = Y.clone()
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+    start.record()
+    B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+    end.record()
+    cache.check()
+    assert start.elapsed_time(end) > 3.0
+    Y.zero_()
+    B.attend_prompt(cache, batch, q, out=out, workspace=ws)
+    B.test_expire_next_wait(1000, False)
+    B.forward(packed, gamma, X, N, workspace=matmul_ws, Y=Y)
+    assert B.poll_status(matmul_ws) == B.OK
+    cache.check()
+    assert torch.equal(Y, want)
