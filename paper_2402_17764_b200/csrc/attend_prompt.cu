@@ -39,7 +39,7 @@
 // (tensor pipe 67 %, exponentials 53 %), since a softmax warp loads its scores, finds their maximum and only then begins its
 // exponentials.  8192 tokens, 32 heads: 586-594 us = 0.93 PFLOP/s, where the board's power limit holds the clock near 1.55 GHz
 // (the same launch takes about 930 000 cycles at any clock).  int8: the converters' shared-memory traffic and arithmetic come on
-// top, 57 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 393-401 us = 0.74 PFLOP/s).
+// top, 57 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 393-405 us = 0.73 PFLOP/s).
 // Prompts of few hundred tokens: half the time is each tile's beginning and end (pages, queries, first scores; results).
 // Registers: the bf16 form spills 4 bytes (12 loaded), the int8 form none.
 #include <cuda.h>
