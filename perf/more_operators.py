@@ -208,7 +208,7 @@ def prepare(case, seed):
             s["out"] = torch.empty(T, H, D, dtype=torch.bfloat16, device="cuda")
             s["workspace"] = binding.alloc_attend_weigh_workspace(H, Hk, D, case["bits"], B, sum(lens))
         if op == "shared":
-            s["groups"] = binding.KVGroups(s["bounds"], s["spans"])
+            s["groups"] = binding.KVBatch(table[s["bounds"][:-1].long()], s["spans"], cu_tokens=s["bounds"])
             s["out"] = torch.empty(T, H, D, dtype=torch.bfloat16, device="cuda")
             s["workspace"] = binding.alloc_attend_shared_workspace(H, Hk, D, B)
     return s
