@@ -417,6 +417,93 @@ bitlinear_status bitlinear_attend_prompt(const bitlinear_kv_cache *cache, const 
                                          int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * What is kept about every row of a cache beside its key and value, for caches that rows are evicted from: `mass`, the attention
+ * weight that the row has received, and `pos`, the position of its token, which is no longer its place in the sequence once
+ * rows have been moved.  Both [n_pages][kv_heads][page_size], both written by bitlinear_kv_append_rmsnorm for new rows (0, and the
+ * token's position).
+ */
+typedef struct {
+    float *mass;  /* device */
+    int32_t *pos; /* device */
+} bitlinear_kv_marks;
+
+/*
+ * Appends as bitlinear_kv_append does, with an RMS norm of every query and key head in front of the rotation, all in one pass:
+ *   y_i = x_i g_i / sqrt(max(mean_i x_i^2 + norm_eps, 2^-126)),  over the head_dim elements of the head,
+ * then rotated and rounded, or stored as codes, as there.  In fp32 (head by head the squares' sum, 1 / sqrt, two products); the
+ * factor 1 / rms cancels out of an 8-bit row's codes, which are those of the exact x_i g_i rotated (where beta is above its
+ * floor 1e-5), and enters its scale, in fp32.
+ *   q_gain, k_gain  in  fp32 [head_dim], 16-byte aligned; NULL: the queries, or the keys, are not normalised
+ *   norm_eps            >= 0 and finite
+ *   positions       in  int32 [T], or NULL: the position of each token, for its angles and its mark, where that is not its place
+ *                       kv_lens[b] - n + i in the sequence (a cache that rows were evicted from).  With a rotary table it
+ *                       has to lie inside the table, else the token is skipped and the status set
+ *   marks               or NULL; the marks of the new rows are set
+ */
+bitlinear_status bitlinear_kv_append_rmsnorm(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *k,
+                                             int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                                             int64_t T, int heads, const float *q_gain, const float *k_gain, float norm_eps,
+                                             const float *rope, int64_t rope_positions, int interleaved, const int32_t *positions,
+                                             const bitlinear_kv_marks *marks, void *q_out, int64_t q_out_stride, void *stream);
+
+/*
+ * bitlinear_attend_decode that also adds every row's weight to its mark: mass_j += sum over the query heads h of the row's kv head
+ * of p_h,j, the weights of the softmax.  Two launches: the attention, which keeps the scores of all keys in the workspace, and the
+ * sum of their weights.  All else as there, with
+ *   workspace  >= bitlinear_attend_weigh_workspace_bytes(heads, kv_heads, head_dim, bits, n_seqs, max_keys) bytes, its start
+ *              zeroed as there, where max_keys is the most keys that a call's sequences have in all (the sum of kv_lens).
+ *              The weights of keys that there is no room for are not added, and the status is set.
+ * Weights are added in fp32, one addition per row and call; a row that several sequences of the call share gets one for each, in an
+ * order that is not fixed.  Rows on a bad page get nothing, and where a result is NaN the weights are.
+ */
+size_t bitlinear_attend_weigh_workspace_bytes(int heads, int kv_heads, int head_dim, int bits, int64_t n_seqs, int64_t max_keys);
+bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,
+                                               const bitlinear_kv_marks *marks, const void *q, int64_t q_stride, int heads,
+                                               float softmax_scale, void *out, int64_t out_stride, void *workspace,
+                                               size_t workspace_bytes, void *stream);
+
+/*
+ * Which rows stay when the sequences of a batch are cut to `keep` rows: for every sequence longer than that and every kv head, the
+ * rows whose position is among the `recent` newest (above pos of the sequence's last row - recent) and, for the rest, the
+ * rows of the largest mass; of equal ones the first (a negative mass or NaN counts as 0, as does a row on a bad page, which sets the status).
+ *   source    out  int32 [n_seqs][kv_heads][keep]: the place that row i's new contents come from: i itself where the row at i
+ *                  stays; the j-th of the rows at or behind `keep` that stay, for the j-th place below `keep` whose row goes;
+ *                  -1 behind the end of a sequence of fewer rows
+ *   new_lens  out  int32 [n_seqs]: min(kv_lens[b], keep); must not be kv_lens itself
+ *   0 <= recent <= keep, 1 <= keep <= 2^30;  table_pages * page_size <= 2^21;  n_seqs * kv_heads <= 2^27
+ * cu_tokens is not looked at.
+ */
+bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
+                                     int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream);
+
+/*
+ * Moves the rows that `source` (as bitlinear_kv_select writes it, or the caller's own) names: keys, values, scales and marks (if not
+ * NULL) of row source[b][h][i] of sequence b to row i, where the two differ.  A source is i, -1 (nothing), or lies at or behind
+ * `keep` and inside the sequence; others, and rows on bad pages, are left out and set the status.  kv_lens holds the lengths before
+ * the move; afterwards the first min(kv_lens[b], keep) rows are the sequence's, and pages behind them are free.  Pages that
+ * are written to must not serve another sequence.  No row is read and written in one call, so the order does not matter.
+ */
+bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const int32_t *source,
+                                      int64_t keep, const bitlinear_kv_marks *marks, void *stream);
+
+/*
+ * bitlinear_attend_decode for sequences that begin with the same rows: what a group of sequences shares is read once for all of them
+ * (tcgen05, the queries of all its sequences as rows of one tile), the rest sequence by sequence, and the two are joined.
+ * The result is that of bitlinear_attend_decode, up to the rounding of the shared part's weights to bf16 (as in
+ * bitlinear_attend_prompt).  `batch` is as there: its page table covers the shared rows too.
+ *   groups  n_seqs groups: cu_tokens[g] .. cu_tokens[g + 1] - 1 are the SEQUENCES of group g (not NULL; sequences may belong to
+ *           none), kv_lens[g] the number of rows they share, cut to whole pages, and row g of its page_table those pages.  Each
+ *           sequence of the group sees them as far as its own length goes.  A group of one sequence shares nothing.  With bounds that
+ *           fall or lie outside 0 .. n_seqs of the batch the status is set and all is attended to sequence by sequence.
+ *   workspace  >= bitlinear_attend_shared_workspace_bytes(..., n_seqs of the batch), zeroed once
+ */
+size_t bitlinear_attend_shared_workspace_bytes(int heads, int kv_heads, int head_dim, int64_t n_seqs);
+bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,
+                                                const bitlinear_kv_batch *groups, const void *q, int64_t q_stride, int heads,
+                                                float softmax_scale, void *out, int64_t out_stride, void *workspace,
+                                                size_t workspace_bytes, void *stream);
+
+/*
  * Test hooks.
  * bitlinear_matmul_i32: acc[t, n] = sum_k Xq[t, k] * T[n, k] as int32 [M, N] through the chosen path
  * (the integer matmul of Section 1 in isolation).  Xq int8 [M, K] with values in [-127, 127].

@@ -56,6 +56,13 @@ EXPORTS = [
     "bitlinear_attend_workspace_bytes",
     "bitlinear_attend_decode",
     "bitlinear_attend_prompt",
+    "bitlinear_kv_append_rmsnorm",
+    "bitlinear_attend_weigh_workspace_bytes",
+    "bitlinear_attend_decode_weigh",
+    "bitlinear_kv_select",
+    "bitlinear_kv_compact",
+    "bitlinear_attend_shared_workspace_bytes",
+    "bitlinear_attend_decode_shared",
     "bitlinear_probe_int8_peak",
     "bitlinear_test_expire_next_wait",
     "bitlinear_poll_status",
@@ -93,6 +100,10 @@ class KVCacheDesc(ctypes.Structure):
         ("page_size", ctypes.c_int32),
         ("bits", ctypes.c_int32),
     ]
+
+
+class KVMarksDesc(ctypes.Structure):
+    _fields_ = [("mass", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
 
 
 class KVBatchDesc(ctypes.Structure):
@@ -170,6 +181,15 @@ def load_library() -> ctypes.CDLL:
     L.bitlinear_attend_workspace_bytes.restype = sz
     L.bitlinear_attend_decode.argtypes = [vp, vp, vp, i64, ci, cf, vp, i64, vp, sz, vp]
     L.bitlinear_attend_prompt.argtypes = [vp, vp, vp, i64, i64, ci, cf, vp, i64, vp, sz, vp]
+    L.bitlinear_kv_append_rmsnorm.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, i64, ci, vp, vp, cf, vp, i64, ci, vp, vp, vp, i64, vp]
+    L.bitlinear_attend_weigh_workspace_bytes.argtypes = [ci, ci, ci, ci, i64, i64]
+    L.bitlinear_attend_weigh_workspace_bytes.restype = sz
+    L.bitlinear_attend_decode_weigh.argtypes = [vp, vp, vp, vp, i64, ci, cf, vp, i64, vp, sz, vp]
+    L.bitlinear_kv_select.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp]
+    L.bitlinear_kv_compact.argtypes = [vp, vp, vp, i64, vp, vp]
+    L.bitlinear_attend_shared_workspace_bytes.argtypes = [ci, ci, ci, i64]
+    L.bitlinear_attend_shared_workspace_bytes.restype = sz
+    L.bitlinear_attend_decode_shared.argtypes = [vp, vp, vp, vp, i64, ci, cf, vp, i64, vp, sz, vp]
     _lib = L
     return L
 
@@ -603,6 +623,37 @@ class KVBatch:
         self._address = ctypes.addressof(self._desc)
 
 
+class KVMarks:
+    """bitlinear_kv_marks of a cache that rows are evicted from: of every row the attention weight it has received (`mass`, fp32)
+    and the position of its token (`pos`, int32), both [n_pages, kv_heads, page_size]."""
+
+    def __init__(self, cache: KVCache):
+        shape = (cache.n_pages, cache.kv_heads, cache.page_size)
+        self._set(cache, torch.zeros(shape, dtype=torch.float32, device=cache.device), torch.zeros(shape, dtype=torch.int32, device=cache.device))
+        _wait_for_fills(cache.device)
+
+    @classmethod
+    def from_tensors(cls, cache: KVCache, mass: torch.Tensor, pos: torch.Tensor) -> "KVMarks":
+        """Marks over tensors that the caller allocated."""
+        self = cls.__new__(cls)
+        self._set(cache, mass, pos)
+        return self
+
+    def _set(self, cache, mass, pos):
+        for t, dtype in ((mass, torch.float32), (pos, torch.int32)):
+            if t.shape != cache.k.shape[:3] or t.dtype != dtype or t.device != cache.device or not t.is_contiguous():
+                _refuse("bitlinear_kv_marks", "mass (fp32) and pos (int32) are contiguous [n_pages, kv_heads, page_size] on the cache's device")
+        self.mass, self.pos, self.shape, self.index = mass, pos, tuple(mass.shape), cache.index
+        self._desc = KVMarksDesc(_ptr(mass), _ptr(pos))
+        self._address = ctypes.addressof(self._desc)
+
+
+def _marks_of(cache: KVCache, marks: KVMarks, where: str) -> int:
+    if marks.index != cache.index or marks.shape != (cache.n_pages, cache.kv_heads, cache.page_size):
+        _refuse(where, "the marks belong to a cache of another shape or device")
+    return marks._address
+
+
 def rope_table(n_pos: int, head_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
     """bitlinear_rope_table: -> fp32 [n_pos, head_dim / 2, 2], (cos, sin) of every position and pair."""
     if stream is not None:
@@ -765,3 +816,203 @@ def attend_prompt(cache: KVCache, batch: KVBatch, q: torch.Tensor, scale: float 
     """bitlinear_attend_prompt: causal attention of the new tokens of prompts and prompt chunks, bf16 [T, heads, head_dim] ->
     the same; rows of out behind the last sequence keep what they held."""
     return _attend(True, cache, batch, q, scale, out, workspace, stream)
+
+
+def _gain(gain, head_dim: int, index: int, where: str) -> int:
+    if gain is None:
+        return 0
+    if gain.shape != (head_dim,) or gain.dtype is not _FP32 or gain.get_device() != index or gain.stride(0) != 1:
+        _refuse(where, f"a gain is a contiguous fp32 [{head_dim}] on cuda:{index}")
+    return gain.data_ptr()
+
+
+def kv_append_rmsnorm(cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor | None = None,
+                      q_gain: torch.Tensor | None = None, k_gain: torch.Tensor | None = None, norm_eps: float = 1e-5,
+                      rope: torch.Tensor | None = None, interleaved: bool = False, positions: torch.Tensor | None = None,
+                      marks: KVMarks | None = None, q_out: torch.Tensor | None = None, stream=None):
+    """bitlinear_kv_append_rmsnorm: kv_append with an RMS norm of every query and key head (gains fp32 [head_dim], None: not
+    normalised) in front of the rotation.  positions: int32 [T], the positions of the tokens where they are not their places in the
+    sequences; marks: the new rows' are set."""
+    where = "bitlinear_kv_append_rmsnorm"
+    index = cache.index
+    if batch.index != index:
+        _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
+    if _current_device() != index:
+        with torch.cuda.device(index):
+            return kv_append_rmsnorm(cache, batch, k, v, q, q_gain, k_gain, norm_eps, rope, interleaved, positions, marks, q_out, stream)
+    if stream is not None and q is not None and q_out is None:
+        with _allocating_on(stream, cache.device):
+            return kv_append_rmsnorm(cache, batch, k, v, q, q_gain, k_gain, norm_eps, rope, interleaved, positions, marks)
+    if k.dim() != 3 or (q is not None and q.dim() != 3):
+        _refuse(where, "k, v and q are [tokens, heads, head_dim]", ERR_SHAPE)
+    T, D = k.shape[0], cache.head_dim
+    shape = (T, cache.kv_heads, D)
+    ks = _row_stride(k, shape, index, where)
+    vs = _row_stride(v, shape, index, where)
+    heads = qs = os_ = n_angles = q_at = out_at = rope_at = positions_at = marks_at = 0
+    if q is not None:
+        heads = q.shape[1]
+        shape = (T, heads, D)
+        qs = _row_stride(q, shape, index, where)
+        if q_out is None:
+            q_out = _empty_rows(T, heads, D, cache.device)
+        os_ = _row_stride(q_out, shape, index, where)
+        q_at, out_at = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None or q_gain is not None:
+        _refuse(where, "q_out or q_gain without q")
+    if rope is not None:
+        n_angles = rope.shape[0]
+        if rope.shape != (n_angles, D // 2, 2) or rope.dtype is not _FP32 or not rope.is_contiguous() or rope.get_device() != index:
+            _refuse(where, f"rope is a contiguous fp32 [positions, {D // 2}, 2] on {cache.device}")
+        rope_at = rope.data_ptr()
+    if positions is not None:
+        if positions.shape != (T,) or positions.dtype is not torch.int32 or positions.get_device() != index or (T > 1 and positions.stride(0) != 1):
+            _refuse(where, f"positions is a contiguous int32 [{T}] on {cache.device}")
+        positions_at = positions.data_ptr()
+    if marks is not None:
+        marks_at = _marks_of(cache, marks, where)
+    st = (_lib or load_library()).bitlinear_kv_append_rmsnorm(
+        cache._address, batch._address, k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, T, heads, _gain(q_gain, D, index, where),
+        _gain(k_gain, D, index, where), norm_eps, rope_at, n_angles, 1 if interleaved else 0, positions_at, marks_at, out_at, os_,
+        _raw_stream(index) if stream is None else _stream(stream))
+    if st != OK:
+        _check(st, where)
+    return q_out
+
+
+def attend_weigh_workspace_bytes(heads: int, kv_heads: int, head_dim: int, bits: int, n_seqs: int, max_keys: int) -> int:
+    return int(load_library().bitlinear_attend_weigh_workspace_bytes(heads, kv_heads, head_dim, bits, n_seqs, max_keys))
+
+
+def attend_shared_workspace_bytes(heads: int, kv_heads: int, head_dim: int, n_seqs: int) -> int:
+    return int(load_library().bitlinear_attend_shared_workspace_bytes(heads, kv_heads, head_dim, n_seqs))
+
+
+def _zeroed(nbytes: int, where: str, device) -> torch.Tensor:
+    if nbytes == 0:
+        raise BitLinearError(ERR_SHAPE, where)
+    workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+    _wait_for_fills(workspace.device)
+    return workspace
+
+
+def alloc_attend_weigh_workspace(heads: int, kv_heads: int, head_dim: int, bits: int, n_seqs: int, max_keys: int, device="cuda") -> torch.Tensor:
+    """A workspace for attend_decode_weigh of up to n_seqs sequences with max_keys rows in all, zeroed and ready for calls on any stream."""
+    return _zeroed(attend_weigh_workspace_bytes(heads, kv_heads, head_dim, bits, n_seqs, max_keys), "bitlinear_attend_weigh_workspace_bytes", device)
+
+
+def alloc_attend_shared_workspace(heads: int, kv_heads: int, head_dim: int, n_seqs: int, device="cuda") -> torch.Tensor:
+    """A workspace for attend_decode_shared of up to n_seqs sequences, zeroed and ready for calls on any stream."""
+    return _zeroed(attend_shared_workspace_bytes(heads, kv_heads, head_dim, n_seqs), "bitlinear_attend_shared_workspace_bytes", device)
+
+
+def _attend_more(where: str, call, cache: KVCache, batch: KVBatch, other, q, scale, out, workspace, stream):
+    """What attend_decode_weigh and attend_decode_shared have in common: call(.., address of `other` (marks or groups), ..)."""
+    index = cache.index
+    if batch.index != index or other.index != index:
+        _refuse(where, f"not everything is on {cache.device}")
+    if _current_device() != index:
+        with torch.cuda.device(index):
+            return _attend_more(where, call, cache, batch, other, q, scale, out, workspace, stream)
+    if stream is not None and out is None:
+        with _allocating_on(stream, cache.device):
+            return _attend_more(where, call, cache, batch, other, q, scale, out, workspace, None)
+    if q.dim() != 3:
+        _refuse(where, "q is [tokens, heads, head_dim]", ERR_SHAPE)
+    T, heads, _ = q.shape
+    D = cache.head_dim
+    if T != batch.n_seqs:
+        _refuse(where, f"{batch.n_seqs} sequences and {T} tokens", ERR_SHAPE)
+    shape = (T, heads, D)
+    qs = _row_stride(q, shape, index, where)
+    if out is None:
+        out = _empty_rows(T, heads, D, cache.device)
+    os_ = _row_stride(out, shape, index, where)
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        _refuse(where, f"the workspace is contiguous and on {cache.device}")
+    st = call(cache._address, batch._address, other._address, q.data_ptr(), qs, heads, D ** -0.5 if scale is None else float(scale),
+              out.data_ptr(), os_, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+              _raw_stream(index) if stream is None else _stream(stream))
+    if st != OK:
+        _check(st, where)
+    return out
+
+
+def attend_decode_weigh(cache: KVCache, batch: KVBatch, marks: KVMarks, q: torch.Tensor, scale: float | None = None,
+                        out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """bitlinear_attend_decode_weigh: attend_decode that also adds every row's weight to marks.mass.  The workspace
+    (alloc_attend_weigh_workspace) depends on how many rows there are, so it has to be given."""
+    where = "bitlinear_attend_decode_weigh"
+    if workspace is None:
+        _refuse(where, "a workspace is needed (alloc_attend_weigh_workspace)", ERR_WORKSPACE)
+    _marks_of(cache, marks, where)
+    return _attend_more(where, (_lib or load_library()).bitlinear_attend_decode_weigh, cache, batch, marks, q, scale, out, workspace, stream)
+
+
+def attend_decode_shared(cache: KVCache, batch: KVBatch, groups: KVBatch, q: torch.Tensor, scale: float | None = None,
+                         out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """bitlinear_attend_decode_shared: attend_decode for sequences that begin with the same rows.  groups: KVBatch(page_table [groups,
+    pages] of the shared rows, kv_lens [groups] how many they are, cu_tokens [groups + 1] the bounds of each group's sequences)."""
+    where = "bitlinear_attend_decode_shared"
+    if workspace is None:
+        if stream is not None:
+            with _allocating_on(stream, cache.device):
+                return attend_decode_shared(cache, batch, groups, q, scale, out)
+        workspace = torch.zeros(max(1, attend_shared_workspace_bytes(q.shape[1] if q.dim() == 3 else 0, cache.kv_heads, cache.head_dim, batch.n_seqs)),
+                                dtype=torch.uint8, device=cache.device)
+    return _attend_more(where, (_lib or load_library()).bitlinear_attend_decode_shared, cache, batch, groups, q, scale, out, workspace, stream)
+
+
+def _int32(t: torch.Tensor, shape: tuple, index: int, where: str, name: str) -> int:
+    if t.shape != shape or t.dtype is not torch.int32 or t.get_device() != index or not t.is_contiguous():
+        _refuse(where, f"{name} is a contiguous int32 {list(shape)} on cuda:{index}")
+    return t.data_ptr()
+
+
+def kv_select(cache: KVCache, batch: KVBatch, marks: KVMarks, keep: int, recent: int = 0, source: torch.Tensor | None = None,
+              new_lens: torch.Tensor | None = None, stream=None):
+    """bitlinear_kv_select: -> (source int32 [n_seqs, kv_heads, keep], new_lens int32 [n_seqs]), which rows stay when the sequences are
+    cut to `keep` rows: those of the `recent` newest positions, then those of the largest mass."""
+    where = "bitlinear_kv_select"
+    index = cache.index
+    if batch.index != index:
+        _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
+    if _current_device() != index:
+        with torch.cuda.device(index):
+            return kv_select(cache, batch, marks, keep, recent, source, new_lens, stream)
+    if stream is not None and (source is None or new_lens is None):
+        with _allocating_on(stream, cache.device):
+            return kv_select(cache, batch, marks, keep, recent, source, new_lens)
+    if not 1 <= keep <= 1 << 30:
+        _refuse(where, "keep is 1 .. 2^30", ERR_SHAPE)
+    shape = (batch.n_seqs, cache.kv_heads, keep)
+    if source is None:
+        source = torch.empty(shape, dtype=torch.int32, device=cache.device)
+    if new_lens is None:
+        new_lens = torch.empty(shape[:1], dtype=torch.int32, device=cache.device)
+    st = (_lib or load_library()).bitlinear_kv_select(
+        cache._address, batch._address, _marks_of(cache, marks, where), keep, recent, _int32(source, shape, index, where, "source"),
+        _int32(new_lens, shape[:1], index, where, "new_lens"), _raw_stream(index) if stream is None else _stream(stream))
+    if st != OK:
+        _check(st, where)
+    return source, new_lens
+
+
+def kv_compact(cache: KVCache, batch: KVBatch, source: torch.Tensor, marks: KVMarks | None = None, stream=None):
+    """bitlinear_kv_compact: moves the rows that `source` (from kv_select) names to the front; batch.kv_lens still holds the lengths
+    before."""
+    where = "bitlinear_kv_compact"
+    index = cache.index
+    if batch.index != index:
+        _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
+    if _current_device() != index:
+        with torch.cuda.device(index):
+            return kv_compact(cache, batch, source, marks, stream)
+    if source.dim() != 3:
+        _refuse(where, "source is [n_seqs, kv_heads, keep]", ERR_SHAPE)
+    keep = source.shape[2]
+    st = (_lib or load_library()).bitlinear_kv_compact(
+        cache._address, batch._address, _int32(source, (batch.n_seqs, cache.kv_heads, keep), index, where, "source"), keep,
+        0 if marks is None else _marks_of(cache, marks, where), _raw_stream(index) if stream is None else _stream(stream))
+    if st != OK:
+        _check(st, where)

@@ -10,7 +10,7 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libbitlinear_b200.so"
 SOURCES = ["bitlinear_api.cu", "pack_weights.cu", "quantize_acts.cu", "decode_gemv.cu", "prefill_gemm.cu", "decode_tc.cu", "peak_probe.cu",
-           "kv_api.cu", "kv_append.cu", "attend_decode.cu", "attend_prompt.cu"]
+           "kv_api.cu", "kv_append.cu", "kv_evict.cu", "attend_decode.cu", "attend_prompt.cu"]
 
 
 def _nvcc() -> str:

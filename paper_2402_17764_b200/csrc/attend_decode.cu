@@ -168,8 +168,22 @@ struct Plan {
     }
 };
 
-template <bool kInt8, int WT, int NT>
-__global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads)
+// What the kernel does besides.
+enum : int {
+    kPlain = 0,
+    kWeigh = 1,  // keeps the scores of its blocks and every softmax's maximum and sum for the kernel that adds up the weights
+    kBehind = 2, // the sequences' first rows have been dealt with: begins behind them and joins their results to its own
+};
+template <int kMode>
+struct More {};
+template <>
+struct More<kWeigh> : WeighArgs {};
+template <>
+struct More<kBehind> : SharedArgs {};
+
+template <bool kInt8, int WT, int NT, int kMode>
+__global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas)
+attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads, const __grid_constant__ More<kMode> more)
 {
     griddep_wait(); // everything below is read from memory that the launch before this one may have written
     griddep_launch_dependents();
@@ -182,9 +196,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
     const int pairs = a.cache.kv_heads * chunks, n_seqs = a.batch.n_seqs;
 
     // ---- the row: its length (the host made sure that it fits 31 bits), and where this CTA's share begins --------------
+    auto start_of = [&](int b) { // the first row that is this kernel's
+        if constexpr (kMode == kBehind) return more.starts[b];
+        return 0;
+    };
     auto length = [&](int b) {
         bool over;
-        return kv_length(a.batch, b, over);
+        const int n = kv_length(a.batch, b, over);
+        return kMode == kBehind ? max(0, n - start_of(b)) : n;
     };
     auto blocks_of = [&](int len) { return (len + kBlock - 1) / kBlock; };
     auto units_of = [&](int len) { return len > 0 ? (blocks_of(len) + kPairCost) * pairs : 0; };
@@ -195,7 +214,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
         bool over;
         const int n = kv_length(a.batch, b, over);
         if (over && blockIdx.x == 0) kv_report(a.cache);
-        mine += units_of(n);
+        mine += units_of(kMode == kBehind ? max(0, n - start_of(b)) : n);
     }
     int upto = mine;
 #pragma unroll
@@ -265,7 +284,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
         if (lane < kKeys / 16) {
             const int pos = p.blk * kBlock + warp * kKeys + lane * 16;
             if (pos < p.len) {
-                page = kv_page(a.cache, a.batch, p.b, pos);
+                page = kv_page(a.cache, a.batch, p.b, start_of(p.b) + pos);
                 if (page < 0) kv_report(a.cache);
             }
         }
@@ -450,6 +469,20 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
                         top[t][j] = fmaxf(top[t][j], x);
                     }
             }
+        if constexpr (kMode == kWeigh) {
+            if (p.unit < more.max_units) {
+                float *to = more.scores + ((int64_t)p.unit * kBlock + warp * kKeys) * chunk_heads;
+#pragma unroll
+                for (int q = 0; q < kGroups; ++q)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int column = t * 8 + 2 * tq + c % 2;
+                            if (column < chunk_heads) to[(q * 16 + c / 2 * 8 + g) * chunk_heads + column] = s[q][t][c];
+                        }
+            }
+        }
         float base[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -536,11 +569,26 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
     uint32_t *counters = reinterpret_cast<uint32_t *>(ws);
     float *parts = reinterpret_cast<float *>(ws + decode_counter_bytes());
     auto part_of = [&](int share, int which) { return parts + (int64_t)(share * kMaxSplits + which) * S::kPartFloats; };
-    auto store_out = [&](const Place &p, int q, int e, const float4 &x, float inv) { // four neighbours of a query head's output
+    auto store_out = [&](const Place &p, int q, int e, float4 x, float M, float L) { // four neighbours of a query head's output
         const int head = p.pair / chunks, i = (p.pair % chunks) * chunk_heads + q;
-        if (i < group && e < D)
-            *reinterpret_cast<uint2 *>(a.out + (int64_t)p.b * a.out_stride + (int64_t)(head * group + i) * D + e) =
-                make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+        if (i >= group || e >= D) return;
+        if constexpr (kMode == kWeigh) {
+            if (e == 0) more.sums[(int64_t)p.b * a.heads + head * group + i] = make_float2(M, L);
+        }
+        if constexpr (kMode == kBehind) {
+            if (start_of(p.b) > 0) {
+                const int64_t at = (int64_t)p.b * a.heads + head * group + i;
+                const float2 ml = more.ml[at];
+                const float top = fmaxf(M, ml.x), base = top == -INFINITY ? 0.0f : top;
+                const float f = exp2_approx(M - base), f2 = exp2_approx(ml.x - base);
+                x = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+                add_scaled(x, f2, *reinterpret_cast<const float4 *>(more.o + at * W + e));
+                L = L * f + f2 * ml.y;
+            }
+        }
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        *reinterpret_cast<uint2 *>(a.out + (int64_t)p.b * a.out_stride + (int64_t)(head * group + i) * D + e) =
+            make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
     };
     // The warps lay their outputs down as [query][element] in the stage they have just used up (the next fetch into it
     // comes after this); element e of query q stands at e ^ 8 (q / 2 % 4), so that the lanes of a store hit 32 banks.
@@ -590,8 +638,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
                 L += f * ml[w].y;
             }
             if (whole) {
-                const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-                store_out(p, q, e, x, inv);
+                store_out(p, q, e, x, M, L);
             } else {
                 *reinterpret_cast<float4 *>(part + 2 * S::kQ + q * WT + e) = x;
                 if (e == 0) *reinterpret_cast<float2 *>(part + 2 * q) = make_float2(M, L);
@@ -659,7 +706,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
                         L = L * f + L2 * f2;
                         M = top;
                     }
-                    if (i < items && tid % lanes == 0) store_out(p, q, e, x, L == 0.0f ? 0.0f : 1.0f / L);
+                    if (i < items && tid % lanes == 0) store_out(p, q, e, x, M, L);
                 }
             }
         }
@@ -710,13 +757,138 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<kInt8, WT, NT>::kCtas) atte
     // empty slots of the batch get zeros
     for (int b = blockIdx.x; b < n_seqs; b += gridDim.x) {
         if (length(b) > 0) continue;
+        if constexpr (kMode == kBehind) { // (or what the shared rows gave, for one that has no others)
+            if (start_of(b) > 0) {
+                for (int i = tid; i < a.heads * D / 4; i += kThreads) {
+                    const int h = i / (D / 4), e = i % (D / 4) * 4;
+                    const int64_t at = (int64_t)b * a.heads + h;
+                    const float L = more.ml[at].y, inv = L == 0.0f ? 0.0f : 1.0f / L;
+                    const float4 x = *reinterpret_cast<const float4 *>(more.o + at * W + e);
+                    *reinterpret_cast<uint2 *>(a.out + (int64_t)b * a.out_stride + (int64_t)h * D + e) =
+                        make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+                }
+                continue;
+            }
+        }
         uint32_t *row = reinterpret_cast<uint32_t *>(a.out + (int64_t)b * a.out_stride);
         for (int i = tid; i < a.heads * D / 2; i += kThreads) row[i] = 0u;
     }
 }
 
-template <bool kInt8, int WT, int NT>
-cudaError_t launch(const AttendArgs &a, int chunks, int chunk_heads, cudaStream_t stream)
+// The weights of all keys, from the scores that attend_decode_kernel kept: mass_j += sum over the kv head's queries of
+// 2^(s_j - m) / l.  A warp takes an equal share of the blocks, a lane a key; the chunks of a kv head's queries are added up in their
+// order, so every row gets one addition per call and sequence (atomic, as sequences may share a page).
+constexpr int kWeighWarps = 4, kWeighCtas = 8; // of a CTA, per SM
+
+template <int kBlock>
+__global__ void __launch_bounds__(kWeighWarps * 32, kWeighCtas)
+add_weights_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads, const __grid_constant__ WeighArgs more)
+{
+    griddep_wait();
+    griddep_launch_dependents();
+    constexpr int kThreads = kWeighWarps * 32;
+    __shared__ int upto_of[kThreads];
+    __shared__ int scan[kWeighWarps];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int Hk = a.cache.kv_heads, group = a.heads / Hk, n_seqs = a.batch.n_seqs;
+    auto length = [&](int b) {
+        bool over;
+        return kv_length(a.batch, b, over);
+    };
+    auto blocks_of = [&](int len) { return (len + kBlock - 1) / kBlock; };
+    // the units in front of a sequence (as attend_decode_kernel counts them), and its blocks
+    const int per_thread = (n_seqs + kThreads - 1) / kThreads;
+    const int b0 = min(n_seqs, tid * per_thread), b1 = min(n_seqs, b0 + per_thread);
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) {
+        const int blocks = blocks_of(length(b));
+        mine += blocks > 0 ? (blocks + kPairCost) * Hk * chunks : 0;
+    }
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= d) upto += x;
+    }
+    if (lane == 31) scan[warp] = upto;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kWeighWarps; ++w) {
+        if (w < warp) upto += scan[w];
+        total += scan[w];
+    }
+    upto_of[tid] = upto;
+    __syncthreads();
+    const Plan plan(total, (int)gridDim.x * kWeighWarps);
+    const int share = (int)blockIdx.x * kWeighWarps + warp;
+    if (share >= plan.shares) return;
+    int unit = plan.begin_of(share);
+    const int end = plan.begin_of(share + 1);
+    // the thread whose sequences the first unit lies in, then the sequence
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < kWeighWarps; ++i) before += __popc(__ballot_sync(0xFFFFFFFFu, upto_of[i * 32 + lane] <= unit));
+    int rest = unit - (before > 0 ? upto_of[before - 1] : 0), b = before * per_thread, len, nblk;
+    for (;; ++b) {
+        len = length(b);
+        nblk = blocks_of(len);
+        const int units = nblk > 0 ? (nblk + kPairCost) * Hk * chunks : 0;
+        if (rest < units) break;
+        rest -= units;
+    }
+    int pair = rest / (nblk + kPairCost), blk = rest - pair * (nblk + kPairCost);
+    while (unit < end) {
+        const int chunk = pair % chunks, head = pair / chunks;
+        if (chunk != 0 || blk >= nblk) { // (the other chunks are added to the first one's keys; the end of a pair)
+            const int step = min(end - unit, nblk + kPairCost - blk);
+            unit += step;
+            blk += step;
+        } else {
+            float sum[kBlock / 32] = {};
+            bool room = true;
+            for (int c = 0; c < chunks; ++c) {
+                const int u = unit + c * (nblk + kPairCost), heads_here = min(chunk_heads, group - c * chunk_heads);
+                if (u >= more.max_units) {
+                    room = false;
+                    break;
+                }
+                float2 ml = make_float2(0.0f, 0.0f);
+                if (lane < heads_here) ml = more.sums[(int64_t)b * a.heads + head * group + c * chunk_heads + lane];
+                const float m = ml.x == -INFINITY ? 0.0f : ml.x, inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
+                const float *from = more.scores + (int64_t)u * kBlock * chunk_heads;
+                for (int q = 0; q < heads_here; ++q) {
+                    const float mq = __shfl_sync(0xFFFFFFFFu, m, q), iq = __shfl_sync(0xFFFFFFFFu, inv, q);
+#pragma unroll
+                    for (int i = 0; i < kBlock / 32; ++i)
+                        if (blk * kBlock + i * 32 + lane < len) sum[i] += exp2_approx(from[(i * 32 + lane) * chunk_heads + q] - mq) * iq;
+                }
+            }
+            if (!room && lane == 0) kv_report(a.cache);
+#pragma unroll
+            for (int i = 0; i < kBlock / 32; ++i) {
+                const int pos = blk * kBlock + i * 32 + lane;
+                if (!room || pos >= len) continue;
+                const int page = kv_page(a.cache, a.batch, b, pos);
+                if (page >= 0) atomicAdd(more.marks.mass + kv_row(a.cache, page, head, pos), sum[i]);
+            }
+            ++unit;
+            ++blk;
+        }
+        if (blk >= nblk + kPairCost) {
+            blk = 0;
+            if (++pair == Hk * chunks && unit < end) {
+                pair = 0;
+                do len = length(++b);
+                while (len == 0);
+                nblk = blocks_of(len);
+            }
+        }
+    }
+}
+
+template <bool kInt8, int WT, int NT, int kMode>
+cudaError_t launch(const AttendArgs &a, int chunks, int chunk_heads, const More<kMode> &more, cudaStream_t stream)
 {
     using S = Shape<kInt8, WT, NT>;
     static bool ready[64] = {false};
@@ -725,15 +897,19 @@ cudaError_t launch(const AttendArgs &a, int chunks, int chunk_heads, cudaStream_
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
-        e = cudaFuncSetAttribute(attend_decode_kernel<kInt8, WT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+        e = cudaFuncSetAttribute(attend_decode_kernel<kInt8, WT, NT, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
-    return launch_dependent(attend_decode_kernel<kInt8, WT, NT>, std::min(S::kCtas * sm_count(), kDecodeMaxCtas), kWarps * 32, S::kSmem, stream,
-                            a, chunks, chunk_heads);
+    e = launch_dependent(attend_decode_kernel<kInt8, WT, NT, kMode>, std::min(S::kCtas * sm_count(), kDecodeMaxCtas), kWarps * 32, S::kSmem, stream,
+                         a, chunks, chunk_heads, more);
+    if constexpr (kMode == kWeigh) {
+        if (e == cudaSuccess)
+            e = launch_dependent(add_weights_kernel<kWarps * S::kKeys>, kWeighCtas * sm_count(), kWeighWarps * 32, 0, stream, a, chunks, chunk_heads,
+                                 static_cast<const WeighArgs &>(more));
+    }
+    return e;
 }
-
-} // namespace
 
 // Query heads of a kv head are taken up to 16 at a time (two tiles of 8 columns; a single tile where at most 8 are left).
 void decode_chunks(int group, int &chunks, int &chunk_heads)
@@ -742,12 +918,46 @@ void decode_chunks(int group, int &chunks, int &chunk_heads)
     chunk_heads = (group + chunks - 1) / chunks;
 }
 
+template <int kMode>
+cudaError_t launch_mode(const AttendArgs &a, const More<kMode> &more, cudaStream_t stream)
+{
+    int chunks, chunk_heads;
+    decode_chunks(a.heads / a.cache.kv_heads, chunks, chunk_heads);
+    const bool narrow = a.cache.width <= 64, one = chunk_heads <= 8;
+    if (a.cache.k_scale) {
+        if (narrow) return one ? launch<true, 64, 1, kMode>(a, chunks, chunk_heads, more, stream) : launch<true, 64, 2, kMode>(a, chunks, chunk_heads, more, stream);
+        return one ? launch<true, 128, 1, kMode>(a, chunks, chunk_heads, more, stream) : launch<true, 128, 2, kMode>(a, chunks, chunk_heads, more, stream);
+    }
+    if (narrow) return one ? launch<false, 64, 1, kMode>(a, chunks, chunk_heads, more, stream) : launch<false, 64, 2, kMode>(a, chunks, chunk_heads, more, stream);
+    return one ? launch<false, 128, 1, kMode>(a, chunks, chunk_heads, more, stream) : launch<false, 128, 2, kMode>(a, chunks, chunk_heads, more, stream);
+}
+
+// Keys of a block: a stage of each warp.
+int block_keys(bool int8, int head_dim) { return kWarps * kStageBytes / 2 / ((kv_row_width(head_dim) <= 64 ? 64 : 128) * (int8 ? 1 : 2)); }
+
+// Of the workspace of the weighing form: behind the decode kernel's own, the softmaxes' maxima and sums, then the scores.
+size_t weigh_fixed_bytes(int heads, int kv_heads, int head_dim, int64_t n_seqs)
+{
+    return attend_decode_workspace_bytes(heads, kv_heads, head_dim) + align_up((size_t)n_seqs * heads * sizeof(float2), 256);
+}
+
+} // namespace
+
 size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim)
 {
     int chunks, chunk_heads;
     decode_chunks(heads / kv_heads, chunks, chunk_heads);
     const size_t q = chunk_heads <= 8 ? 8 : 16, width = kv_row_width(head_dim) <= 64 ? 64 : 128;
     return align_up(decode_counter_bytes() + (size_t)kDecodeMaxCtas * kMaxSplits * q * (width + 2) * 4, 256);
+}
+
+size_t attend_weigh_workspace_bytes(int heads, int kv_heads, int head_dim, bool int8, int64_t n_seqs, int64_t max_keys)
+{
+    int chunks, chunk_heads;
+    decode_chunks(heads / kv_heads, chunks, chunk_heads);
+    // every sequence has at most one block that is not full, and a unit behind its last one
+    const int64_t keys = block_keys(int8, head_dim), units = (max_keys / keys + n_seqs * (1 + kPairCost)) * kv_heads * chunks;
+    return align_up(weigh_fixed_bytes(heads, kv_heads, head_dim, n_seqs) + (size_t)units * keys * chunk_heads * 4, 256);
 }
 
 bool attend_decode_fits(const AttendArgs &a)
@@ -758,17 +968,29 @@ bool attend_decode_fits(const AttendArgs &a)
     return units * a.cache.kv_heads * chunks <= 0x7FFFFFFF / std::max(a.batch.n_seqs, 1);
 }
 
-cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream)
+cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream) { return launch_mode<kPlain>(a, More<kPlain>{}, stream); }
+
+cudaError_t launch_attend_decode_weigh(const AttendArgs &a, const KvMarks &marks, size_t workspace_bytes, cudaStream_t stream)
 {
     int chunks, chunk_heads;
     decode_chunks(a.heads / a.cache.kv_heads, chunks, chunk_heads);
-    const bool narrow = a.cache.width <= 64, one = chunk_heads <= 8;
-    if (a.cache.k_scale) {
-        if (narrow) return one ? launch<true, 64, 1>(a, chunks, chunk_heads, stream) : launch<true, 64, 2>(a, chunks, chunk_heads, stream);
-        return one ? launch<true, 128, 1>(a, chunks, chunk_heads, stream) : launch<true, 128, 2>(a, chunks, chunk_heads, stream);
-    }
-    if (narrow) return one ? launch<false, 64, 1>(a, chunks, chunk_heads, stream) : launch<false, 64, 2>(a, chunks, chunk_heads, stream);
-    return one ? launch<false, 128, 1>(a, chunks, chunk_heads, stream) : launch<false, 128, 2>(a, chunks, chunk_heads, stream);
+    const bool int8 = a.cache.k_scale != nullptr;
+    const size_t own = attend_decode_workspace_bytes(a.heads, a.cache.kv_heads, a.cache.head_dim);
+    const size_t fixed = weigh_fixed_bytes(a.heads, a.cache.kv_heads, a.cache.head_dim, a.batch.n_seqs);
+    char *ws = reinterpret_cast<char *>(a.workspace);
+    More<kWeigh> more;
+    more.sums = reinterpret_cast<float2 *>(ws + own);
+    more.scores = reinterpret_cast<float *>(ws + fixed);
+    more.max_units = (int64_t)((workspace_bytes - fixed) / ((size_t)block_keys(int8, a.cache.head_dim) * chunk_heads * 4));
+    more.marks = marks;
+    return launch_mode<kWeigh>(a, more, stream);
+}
+
+cudaError_t launch_attend_decode_behind(const AttendArgs &a, const SharedArgs &shared, cudaStream_t stream)
+{
+    More<kBehind> more;
+    static_cast<SharedArgs &>(more) = shared;
+    return launch_mode<kBehind>(a, more, stream);
 }
 
 } // namespace bitlinear

@@ -87,6 +87,7 @@ struct Shared {
     uint32_t tmem_base;
     int abort_flag;
     int poisoned[2];
+    int least[2];
     int is_last;
     int found_b;
     int64_t found_local, scan[kThreads / 32];
@@ -115,6 +116,22 @@ struct PromptArgs {
     int slots;        // > 0: CTAs among which the tiles are to be split, once their number is known
     WaitHooks hooks;
 };
+
+// The shared form: the "sequences" of a.batch are groups of sequences, a group's new tokens are one token of each of its
+// sequences (token row = sequence), and all of them see the rows that the group shares, as far as their own lengths go.  References,
+// sums and outputs stay fp32 and are handed on.
+template <bool kShared>
+struct PromptMore {};
+template <>
+struct PromptMore<true> : SharedArgs {};
+
+// How many rows group g shares, a whole number of pages; none for a group of a single sequence (nothing is saved).
+__device__ __forceinline__ int shared_rows(const AttendArgs &a, int g, bool &over)
+{
+    const int n = max(0, a.batch.kv_lens[g]) >> a.cache.page_shift << a.cache.page_shift;
+    over = n > a.batch.capacity;
+    return a.batch.cu_tokens[g + 1] - a.batch.cu_tokens[g] < 2 ? 0 : min(n, a.batch.capacity);
+}
 
 __device__ __forceinline__ float exp2_approx(float x)
 {
@@ -182,10 +199,11 @@ struct Work {
     int len;              // keys of the sequence
     int offset;           // position of the first new token (may be negative)
     int group;
+    const int32_t *own_lens; // shared form: the lengths of the group's sequences
     // keys that row r of the sequence sees
     __device__ __forceinline__ int sees(int r) const
     {
-        const int n = offset + r / group + 1;
+        const int n = own_lens ? own_lens[r / group] : offset + r / group + 1;
         return n < 0 ? 0 : (n > len ? len : n);
     }
 };
@@ -193,7 +211,8 @@ struct Work {
 // (Not inlined: the registers of the main loop are allotted without it, 584 -> 576 us for 8192 tokens, 32 heads.)
 // One row by plain arithmetic, one warp: for tiles in which a non-finite value stands behind keys that some of the rows do not
 // see (0 x NaN would reach them through the MMA), or in which a reference lies beyond kFar.
-__device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int r, int lane)
+template <bool kShared>
+__device__ __noinline__ void attend_row(const AttendArgs &a, const PromptMore<kShared> &more, const Work &w, int r, int lane)
 {
     const int D = a.cache.head_dim, t = w.first_token + r / w.group, h = w.head * w.group + r % w.group;
     const bool mine = 4 * lane < D;
@@ -242,6 +261,12 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int 
         }
         m = mn;
     }
+    if constexpr (kShared) {
+        const int64_t at = (int64_t)t * a.heads + h;
+        if (lane == 0) more.ml[at] = make_float2(m, l);
+        if (4 * lane < a.cache.width) *reinterpret_cast<float4 *>(more.o + at * a.cache.width + 4 * lane) = o;
+        return;
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (mine)
         *reinterpret_cast<uint2 *>(a.out + (int64_t)t * a.out_stride + h * D + 4 * lane) =
@@ -252,8 +277,8 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int 
 // that a row per thread writes and reads whole lines.
 __host__ __device__ constexpr size_t part_floats(int width) { return (size_t)kRows * (width + 2); }
 
-template <bool kInt8>
-__global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args)
+template <bool kInt8, bool kShared>
+__global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args, const __grid_constant__ PromptMore<kShared> more)
 {
     griddep_wait(); // everything below is read from memory that the launch before this one may have written
     const AttendArgs &a = args.a;
@@ -276,13 +301,33 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     {
         auto tiles_of = [&](int b) -> int64_t {
             const int64_t n = (int64_t)a.batch.cu_tokens[b + 1] - a.batch.cu_tokens[b];
+            if constexpr (kShared) {
+                bool over;
+                if (shared_rows(a, b, over) == 0) return 0;
+            }
             return n <= 0 || n > a.T ? 0 : (n * group + kRows - 1) / kRows * a.cache.kv_heads;
         };
+
         // (rows that the caller did not hand over: the sequence has none then, here or where its first row is looked at below)
         auto rows_missing = [&](int b) { return a.batch.cu_tokens[b] < 0 || a.batch.cu_tokens[b] > a.batch.cu_tokens[b + 1] || a.batch.cu_tokens[b + 1] > a.T; };
         const int per_thread = (n_seqs + kThreads - 1) / kThreads;
         const int b0 = min(n_seqs, tid * per_thread), b1 = min(n_seqs, b0 + per_thread);
         int64_t mine = 0;
+        if constexpr (kShared) { // with bounds that fall, or lie outside the batch, nothing is shared at all
+            bool bad = false;
+            for (int b = b0; b < b1; ++b) bad = bad || rows_missing(b);
+            const bool none = __syncthreads_or(bad);
+            for (int b = blockIdx.x * kThreads + tid; b < a.T; b += gridDim.x * kThreads) {
+                int first, count;
+                bool over;
+                const int g = none ? -1 : kv_sequence_of(a.batch, b, first, count);
+                more.starts[b] = g < 0 ? 0 : shared_rows(a, g, over);
+            }
+            if (none) {
+                if (blockIdx.x == 0 && tid == 0) kv_report(a.cache);
+                return;
+            }
+        }
         for (int b = b0; b < b1; ++b) {
             mine += tiles_of(b);
             if (blockIdx.x == 0 && rows_missing(b)) kv_report(a.cache);
@@ -357,20 +402,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         w.row0 = (tiles - 1 - rest / heads_here) * kRows;
     }
     bool over;
-    w.len = kv_length(a.batch, w.b, over);
+    w.len = kShared ? shared_rows(a, w.b, over) : kv_length(a.batch, w.b, over);
     if (over && tid == 0) kv_report(a.cache);
     w.offset = a.batch.kv_lens[w.b] - n_tokens;
+    w.own_lens = nullptr;
+    if constexpr (kShared) w.own_lens = more.kv_lens + w.first_token;
 
     // blocks of keys of the two tiles, and this CTA's part of them (a part is at least four blocks, so that joining the parts
     // does not cost more than they save)
-    const int most = (w.sees(min(w.row0 + kRows, w.rows) - 1) + kTile - 1) / kTile;
+    const int most = ((kShared ? w.len : w.sees(min(w.row0 + kRows, w.rows) - 1)) + kTile - 1) / kTile;
     const int parts = max(1, min(splits, most / 4));
     if (split >= parts) return;
     const int from = (int)((int64_t)most * split / parts), to = (int)((int64_t)most * (split + 1) / parts);
     int n_steps[2];
     for (int t = 0; t < 2; ++t) {
         const int first = w.row0 + t * kTile, last = min(first + kTile, w.rows) - 1;
-        n_steps[t] = first < w.rows ? max(0, min((w.sees(last) + kStep - 1) / kStep, 2 * to) - 2 * from) : 0;
+        n_steps[t] = first < w.rows ? max(0, min(((kShared ? w.len : w.sees(last)) + kStep - 1) / kStep, 2 * to) - 2 * from) : 0;
     }
     const int total = (max(n_steps[0], n_steps[1]) + 1) / 2; // blocks
 
@@ -384,6 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             mbar_init(smem_u32(&sh.o_done[t]), 1);
             mbar_init(smem_u32(&sh.o_last[t]), 1);
             sh.poisoned[t] = 0;
+            sh.least[t] = w.len;
         }
         for (int s = 0; s < kStages; ++s) {
             mbar_init(smem_u32(&sh.kv_full[s]), kInt8 ? kConverters : 1);
@@ -583,7 +631,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             if (lane == 0) mbar_arrive(smem_u32(&sh.q_full[t]));
         }
         const int sees = exists ? w.sees(row) : 0x7FFFFFFF; // (rows that do not exist: nothing to hide from them)
-        const int least = w.sees(w.row0 + t * kTile);       // of the tile's rows
+        int least; // of the tile's rows
+        if constexpr (kShared) {
+            const int of_warp = __reduce_min_sync(0xFFFFFFFFu, sees);
+            if (lane == 0) atomicMin(&sh.least[t], of_warp);
+            named_barrier(2 + t, kTile);
+            least = sh.least[t];
+        } else {
+            least = w.sees(w.row0 + t * kTile);
+        }
         float m = -INFINITY, l = 0.0f;                      // reference and sum of this row
         bool far = false;                                   // a reference beyond kFar (int8: of any row of the warp, at present)
         bool ok = true;
@@ -749,7 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         const int first_part = blockIdx.x - split; // of this tile
         auto part_of = [&](int p) { return ws_parts + (size_t)(first_part + p) * part_floats(W); };
         if (ok) {
-            const float inv = parts > 1 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
+            const float inv = kShared || parts > 1 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
             __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + row / group) * a.out_stride + (w.head * group + row % group) * D;
             const int pr = t * kTile + r;
             const bool some = n_steps[t] > 0 && l != 0.0f;
@@ -767,6 +823,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
 #pragma unroll
                     for (int e = 0; e < kTile; e += 4)
                         if (e < W) part[e / 4 * kRows] = make_float4(at(e), at(e + 1), at(e + 2), at(e + 3));
+                }
+            } else if constexpr (kShared) {
+                if (exists) {
+                    const int64_t to = (int64_t)(w.first_token + row / group) * a.heads + w.head * group + row % group;
+                    more.ml[to] = make_float2(n_steps[t] > 0 ? m : -INFINITY, l);
+                    float4 *out = reinterpret_cast<float4 *>(more.o + to * W);
+#pragma unroll
+                    for (int e = 0; e < kTile; e += 4)
+                        if (e < W) out[e / 4] = make_float4(at(e), at(e + 1), at(e + 2), at(e + 3));
                 }
             } else {
                 // by way of the tile's queries, which are not needed any more, so that a warp stores whole rows
@@ -830,6 +895,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                     }
                     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
                     __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + rr / group) * a.out_stride + (w.head * group + rr % group) * D;
+                    const int64_t at = (int64_t)(w.first_token + rr / group) * a.heads + w.head * group + rr % group; // shared form
+                    if constexpr (kShared) more.ml[at] = make_float2(M, L);
                     for (int e0 = 0; e0 < D; e0 += 16) { // (W is a multiple of 16)
                         float4 x[4];
 #pragma unroll
@@ -843,6 +910,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                                 const float4 v = __ldcg(src + u * kRows);
                                 x[u] = make_float4(x[u].x + f * v.x, x[u].y + f * v.y, x[u].z + f * v.z, x[u].w + f * v.w);
                             }
+                        }
+                        if constexpr (kShared) {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) *reinterpret_cast<float4 *>(more.o + at * W + e0 + 4 * u) = x[u];
+                            continue;
                         }
 #pragma unroll
                         for (int u = 0; u < 4; ++u)
@@ -861,7 +933,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             if (parts == 1 || sh.is_last) {
                 if (sh.poisoned[t])
                     for (int i = warp % 4; i < kTile; i += 4)
-                        if (w.row0 + t * kTile + i < w.rows) attend_row(a, w, w.row0 + t * kTile + i, lane);
+                        if (w.row0 + t * kTile + i < w.rows) attend_row<kShared>(a, more, w, w.row0 + t * kTile + i, lane);
             }
         }
     }
@@ -895,8 +967,8 @@ bool encode_cache_map(CUtensorMap *map, void *pool, const KvCache &c)
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool kInt8>
-cudaError_t launch(const PromptArgs &p, int ctas, cudaStream_t stream)
+template <bool kInt8, bool kShared>
+cudaError_t launch(const PromptArgs &p, const PromptMore<kShared> &more, int ctas, cudaStream_t stream)
 {
     static bool ready[64] = {false};
     int dev = 0;
@@ -905,26 +977,18 @@ cudaError_t launch(const PromptArgs &p, int ctas, cudaStream_t stream)
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
         cudaFuncAttributes have;
-        e = cudaFuncGetAttributes(&have, attend_prompt_kernel<kInt8>);
+        e = cudaFuncGetAttributes(&have, attend_prompt_kernel<kInt8, kShared>);
         if (e != cudaSuccess) return e;
         if (have.numRegs != kLaunchRegs) return cudaErrorInvalidConfiguration; // (the split of the registers would not add up)
-        e = cudaFuncSetAttribute(attend_prompt_kernel<kInt8>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shared<kInt8>::bytes());
+        e = cudaFuncSetAttribute(attend_prompt_kernel<kInt8, kShared>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shared<kInt8>::bytes());
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
-    return launch_dependent(attend_prompt_kernel<kInt8>, (unsigned)ctas, kThreads, Shared<kInt8>::bytes(), stream, p);
+    return launch_dependent(attend_prompt_kernel<kInt8, kShared>, (unsigned)ctas, kThreads, Shared<kInt8>::bytes(), stream, p, more);
 }
 
-} // namespace
-
-size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim)
-{
-    (void)heads;
-    (void)kv_heads;
-    return align_up(prompt_counter_bytes() + kPromptMaxParts * part_floats(kv_row_width(head_dim)) * 4, 256);
-}
-
-cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream)
+template <bool kShared>
+cudaError_t launch_tiles(const AttendArgs &a, const PromptMore<kShared> &more, cudaStream_t stream)
 {
     PromptArgs p{};
     p.a = a;
@@ -944,7 +1008,25 @@ cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream)
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxParts, slots / tiles));
     p.slots = a.batch.n_seqs > 1 && tiles < slots ? slots : 0;
     const int ctas = p.slots > 0 ? slots : (int)tiles * p.splits;
-    return a.cache.k_scale ? launch<true>(p, ctas, stream) : launch<false>(p, ctas, stream);
+    return a.cache.k_scale ? launch<true, kShared>(p, more, ctas, stream) : launch<false, kShared>(p, more, ctas, stream);
+}
+
+} // namespace
+
+size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim)
+{
+    (void)heads;
+    (void)kv_heads;
+    return align_up(prompt_counter_bytes() + kPromptMaxParts * part_floats(kv_row_width(head_dim)) * 4, 256);
+}
+
+cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream) { return launch_tiles<false>(a, PromptMore<false>{}, stream); }
+
+cudaError_t launch_attend_prefix(const AttendArgs &a, const SharedArgs &shared, cudaStream_t stream)
+{
+    PromptMore<true> more;
+    static_cast<SharedArgs &>(more) = shared;
+    return launch_tiles<true>(a, more, stream);
 }
 
 } // namespace bitlinear

@@ -26,6 +26,12 @@ struct KvCache {
     int32_t n_pages, kv_heads, head_dim, width, page_shift;
 };
 
+// What is kept about every row of a cache beside its key and value: [n_pages][kv_heads][page_size].
+struct KvMarks {
+    float *mass;  // the attention weight it has received
+    int32_t *pos; // the position of its token
+};
+
 struct KvBatch {
     const int32_t *page_table, *kv_lens, *cu_tokens;
     int32_t n_seqs;
@@ -112,8 +118,14 @@ struct AppendArgs {
     int64_t k_stride, v_stride, q_stride, q_out_stride;
     const float2 *rope;
     int32_t rope_positions, T, heads, interleaved;
+    // of the form that normalises (and takes positions and marks) alone
+    const float *q_gain, *k_gain; // fp32 [head_dim], or null: not normalised
+    const int32_t *positions;     // of the token rows, or null: the rows' places in their sequences
+    KvMarks marks;                // null pointers: none
+    float norm_eps;
 };
 cudaError_t launch_kv_append(const AppendArgs &a, cudaStream_t stream);
+cudaError_t launch_kv_append_rmsnorm(const AppendArgs &a, cudaStream_t stream);
 
 struct AttendArgs {
     KvCache cache;
@@ -126,12 +138,33 @@ struct AttendArgs {
     void *workspace;
 };
 
+// What the decode kernel that passes its weights on (to the marks) has besides.
+struct WeighArgs {
+    float *scores;     // of every unit of work with room for it: [kBlock keys][query heads of the chunk], scaled
+    int64_t max_units; // units that there is room for
+    float2 *sums;      // [n_seqs][heads]: reference and denominator of every softmax
+    KvMarks marks;
+};
+
+// What the kernels that attend to shared beginnings hand to each other.
+struct SharedArgs {
+    int32_t *starts; // [n_seqs]: rows of the sequence that the shared part has dealt with
+    float2 *ml;      // [n_seqs][heads]: reference and sum of the shared part of every softmax
+    float *o;        // [n_seqs][heads][width]: its weighted sum of the values
+    const int32_t *kv_lens; // of the sequences
+};
+
 // Workspace of the decode kernel: a counter per CTA, then the partial results.  The grid has at most kDecodeMaxCtas CTAs.
 constexpr int kDecodeMaxCtas = 512;
 __host__ __device__ constexpr size_t decode_counter_bytes() { return kDecodeMaxCtas * sizeof(uint32_t); }
 size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim);
 bool attend_decode_fits(const AttendArgs &a); // the kernel counts its work in 31 bits
 cudaError_t launch_attend_decode(const AttendArgs &a, cudaStream_t stream);
+// The same, adding the weights to the marks: room for scores of max_keys keys in all, more in a workspace of more bytes.
+size_t attend_weigh_workspace_bytes(int heads, int kv_heads, int head_dim, bool int8, int64_t n_seqs, int64_t max_keys);
+cudaError_t launch_attend_decode_weigh(const AttendArgs &a, const KvMarks &marks, size_t workspace_bytes, cudaStream_t stream);
+// The same for sequences whose first rows the call before it has dealt with.
+cudaError_t launch_attend_decode_behind(const AttendArgs &a, const SharedArgs &shared, cudaStream_t stream);
 
 // Workspace of the prompt kernel: two words per part (those of a tile's first part count its parts), then the partial results.  At
 // most kPromptMaxParts CTAs share tiles of rows.
@@ -140,5 +173,27 @@ __host__ __device__ constexpr size_t prompt_counter_bytes() { return 256 * 2 * s
 static_assert(kPromptMaxParts * 2 * sizeof(uint32_t) <= prompt_counter_bytes(), "a counter for every part");
 size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim);
 cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream);
+// The part of a decode step that groups of sequences share: a.batch holds the groups (their pages, how many rows they share, which
+// sequences they are), a.T sequences in all.
+cudaError_t launch_attend_prefix(const AttendArgs &a, const SharedArgs &shared, cudaStream_t stream);
+
+struct SelectArgs {
+    KvCache cache;
+    KvBatch batch;
+    KvMarks marks;
+    int32_t *source, *new_lens;
+    int32_t keep, recent;
+};
+constexpr int64_t kSelectMaxRows = (int64_t)1 << 21; // of a sequence
+cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream);
+
+struct CompactArgs {
+    KvCache cache;
+    KvBatch batch;
+    KvMarks marks; // null pointers: none
+    const int32_t *source;
+    int32_t keep;
+};
+cudaError_t launch_kv_compact(const CompactArgs &a, cudaStream_t stream);
 
 } // namespace bitlinear

@@ -87,12 +87,13 @@ bitlinear_status bitlinear_rope_table(float *table, int64_t n_pos, int head_dim,
     return launch_rope_table(table, n_pos, head_dim, base, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }
 
-bitlinear_status bitlinear_kv_append(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *k,
-                                     int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
-                                     int64_t T, int heads, const float *rope, int64_t rope_positions, int interleaved,
-                                     void *q_out, int64_t q_out_stride, void *stream)
+namespace {
+
+// Checks what the two forms of appending have in common; `idle`: there is nothing to do.
+bitlinear_status take_append(AppendArgs &a, bool &idle, const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *k,
+                             int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride, int64_t T, int heads,
+                             const float *rope, int64_t rope_positions, int interleaved, void *q_out, int64_t q_out_stride)
 {
-    AppendArgs a{};
     bitlinear_status st = take_views(cache, batch, a.cache, a.batch);
     if (st != BITLINEAR_OK) return st;
     if (T < 0 || T > (1 << 20) || (!batch->cu_tokens && T != batch->n_seqs)) return BITLINEAR_ERR_SHAPE;
@@ -110,8 +111,7 @@ bitlinear_status bitlinear_kv_append(const bitlinear_kv_cache *cache, const bitl
         if (rope_positions < 1 || rope_positions > (1 << 30)) return BITLINEAR_ERR_SHAPE;
         if (!aligned(rope, 16)) return BITLINEAR_ERR_ALIGN;
     }
-    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
-    if (T == 0 || batch->n_seqs == 0) return BITLINEAR_OK;
+    idle = T == 0 || batch->n_seqs == 0;
     a.k = reinterpret_cast<const __nv_bfloat16 *>(k);
     a.v = reinterpret_cast<const __nv_bfloat16 *>(v);
     a.q = reinterpret_cast<const __nv_bfloat16 *>(q);
@@ -125,7 +125,56 @@ bitlinear_status bitlinear_kv_append(const bitlinear_kv_cache *cache, const bitl
     a.T = (int32_t)T;
     a.heads = q ? heads : 0;
     a.interleaved = interleaved;
+    return BITLINEAR_OK;
+}
+
+bitlinear_status take_marks(const bitlinear_kv_marks *marks, KvMarks &m)
+{
+    if (!marks || !marks->mass || !marks->pos) return BITLINEAR_ERR_ARG;
+    if (!aligned(marks->mass, 4) || !aligned(marks->pos, 4)) return BITLINEAR_ERR_ALIGN;
+    m.mass = marks->mass;
+    m.pos = marks->pos;
+    return BITLINEAR_OK;
+}
+
+} // namespace
+
+bitlinear_status bitlinear_kv_append(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *k,
+                                     int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                                     int64_t T, int heads, const float *rope, int64_t rope_positions, int interleaved,
+                                     void *q_out, int64_t q_out_stride, void *stream)
+{
+    AppendArgs a{};
+    bool idle;
+    const bitlinear_status st = take_append(a, idle, cache, batch, k, k_stride, v, v_stride, q, q_stride, T, heads, rope, rope_positions,
+                                            interleaved, q_out, q_out_stride);
+    if (st != BITLINEAR_OK) return st;
+    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
+    if (idle) return BITLINEAR_OK;
     return launch_kv_append(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+}
+
+bitlinear_status bitlinear_kv_append_rmsnorm(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *k,
+                                             int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                                             int64_t T, int heads, const float *q_gain, const float *k_gain, float norm_eps,
+                                             const float *rope, int64_t rope_positions, int interleaved, const int32_t *positions,
+                                             const bitlinear_kv_marks *marks, void *q_out, int64_t q_out_stride, void *stream)
+{
+    AppendArgs a{};
+    bool idle;
+    bitlinear_status st = take_append(a, idle, cache, batch, k, k_stride, v, v_stride, q, q_stride, T, heads, rope, rope_positions,
+                                      interleaved, q_out, q_out_stride);
+    if (st != BITLINEAR_OK) return st;
+    if (!(norm_eps >= 0.0f) || !std::isfinite(norm_eps)) return BITLINEAR_ERR_ARG;
+    if (!aligned(q_gain, 16) || !aligned(k_gain, 16) || !aligned(positions, 4)) return BITLINEAR_ERR_ALIGN;
+    if (marks && (st = take_marks(marks, a.marks)) != BITLINEAR_OK) return st;
+    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
+    if (idle) return BITLINEAR_OK;
+    a.q_gain = q ? q_gain : nullptr;
+    a.k_gain = k_gain;
+    a.norm_eps = norm_eps;
+    a.positions = positions;
+    return launch_kv_append_rmsnorm(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }
 
 namespace {
@@ -141,11 +190,10 @@ size_t workspace_for(int heads, int kv_heads, int head_dim, bool prompt)
     return prompt ? attend_prompt_workspace_bytes(heads, kv_heads, head_dim) : attend_decode_workspace_bytes(heads, kv_heads, head_dim);
 }
 
-bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q, int64_t q_stride, int64_t T,
-                        int heads, float softmax_scale, void *out, int64_t out_stride, void *workspace, size_t workspace_bytes,
-                        void *stream, bool prompt)
+// Checks what the attentions have in common and fills their view.
+bitlinear_status take_attend(AttendArgs &a, const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q, int64_t q_stride,
+                             int64_t T, int heads, float softmax_scale, void *out, int64_t out_stride, void *workspace, bool prompt)
 {
-    AttendArgs a{};
     bitlinear_status st = take_views(cache, batch, a.cache, a.batch);
     if (st != BITLINEAR_OK) return st;
     if (T < 0 || T > (1 << 20) || !heads_ok(heads, a.cache.kv_heads, a.cache.head_dim)) return BITLINEAR_ERR_SHAPE;
@@ -155,19 +203,29 @@ bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batc
     if ((st = check_rows(q, q_stride, heads, a.cache.head_dim)) != BITLINEAR_OK) return st;
     if ((st = check_rows(out, out_stride, heads, a.cache.head_dim)) != BITLINEAR_OK) return st;
     if (!aligned(workspace, 256)) return BITLINEAR_ERR_ALIGN;
-    if (workspace_bytes < workspace_for(heads, a.cache.kv_heads, a.cache.head_dim, prompt)) return BITLINEAR_ERR_WORKSPACE;
     a.heads = heads;
     if (!prompt && !attend_decode_fits(a)) return BITLINEAR_ERR_SHAPE;
     a.scale = (float)((double)softmax_scale * 1.4426950408889634074); // log2 e
     if (!std::isfinite(a.scale)) return BITLINEAR_ERR_ARG;
-    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
-    if (T == 0 || batch->n_seqs == 0) return BITLINEAR_OK;
     a.q = reinterpret_cast<const __nv_bfloat16 *>(q);
     a.out = reinterpret_cast<__nv_bfloat16 *>(out);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.T = (int32_t)T;
     a.workspace = workspace;
+    return BITLINEAR_OK;
+}
+
+bitlinear_status attend(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const void *q, int64_t q_stride, int64_t T,
+                        int heads, float softmax_scale, void *out, int64_t out_stride, void *workspace, size_t workspace_bytes,
+                        void *stream, bool prompt)
+{
+    AttendArgs a{};
+    const bitlinear_status st = take_attend(a, cache, batch, q, q_stride, T, heads, softmax_scale, out, out_stride, workspace, prompt);
+    if (st != BITLINEAR_OK) return st;
+    if (workspace_bytes < workspace_for(heads, a.cache.kv_heads, a.cache.head_dim, prompt)) return BITLINEAR_ERR_WORKSPACE;
+    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
+    if (T == 0 || batch->n_seqs == 0) return BITLINEAR_OK;
     return (prompt ? launch_attend_prompt(a, (cudaStream_t)stream) : launch_attend_decode(a, (cudaStream_t)stream)) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }
 
@@ -192,6 +250,121 @@ bitlinear_status bitlinear_attend_prompt(const bitlinear_kv_cache *cache, const 
                                          int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream)
 {
     return attend(cache, batch, q, q_stride, T, heads, softmax_scale, out, out_stride, workspace, workspace_bytes, stream, true);
+}
+
+size_t bitlinear_attend_weigh_workspace_bytes(int heads, int kv_heads, int head_dim, int bits, int64_t n_seqs, int64_t max_keys)
+{
+    if (!heads_ok(heads, kv_heads, head_dim) || (bits != 16 && bits != 8) || n_seqs < 0 || n_seqs > (1 << 20) || max_keys < 0 ||
+        max_keys > ((int64_t)1 << 40))
+        return 0;
+    return attend_weigh_workspace_bytes(heads, kv_heads, head_dim, bits == 8, n_seqs, max_keys);
+}
+
+bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,
+                                               const bitlinear_kv_marks *marks, const void *q, int64_t q_stride, int heads,
+                                               float softmax_scale, void *out, int64_t out_stride, void *workspace,
+                                               size_t workspace_bytes, void *stream)
+{
+    AttendArgs a{};
+    KvMarks m{};
+    const int64_t T = batch ? batch->n_seqs : 0;
+    bitlinear_status st = take_attend(a, cache, batch, q, q_stride, T, heads, softmax_scale, out, out_stride, workspace, false);
+    if (st != BITLINEAR_OK) return st;
+    if ((st = take_marks(marks, m)) != BITLINEAR_OK) return st;
+    if (workspace_bytes < attend_weigh_workspace_bytes(heads, a.cache.kv_heads, a.cache.head_dim, a.cache.k_scale != nullptr, T, 0))
+        return BITLINEAR_ERR_WORKSPACE;
+    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
+    if (T == 0) return BITLINEAR_OK;
+    return launch_attend_decode_weigh(a, m, workspace_bytes, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+}
+
+namespace {
+
+// Workspace of the attention over shared beginnings: the prompt kernel's, the decode kernel's, then what the one hands to the other.
+struct SharedLayout {
+    size_t decode, starts, ml, o, bytes;
+    SharedLayout(int heads, int kv_heads, int head_dim, int64_t n_seqs)
+    {
+        decode = attend_prompt_workspace_bytes(heads, kv_heads, head_dim);
+        starts = decode + attend_decode_workspace_bytes(heads, kv_heads, head_dim);
+        ml = starts + align_up((size_t)n_seqs * sizeof(int32_t), 256);
+        o = ml + align_up((size_t)n_seqs * heads * sizeof(float2), 256);
+        bytes = o + align_up((size_t)n_seqs * heads * kv_row_width(head_dim) * sizeof(float), 256);
+    }
+};
+
+} // namespace
+
+size_t bitlinear_attend_shared_workspace_bytes(int heads, int kv_heads, int head_dim, int64_t n_seqs)
+{
+    if (!heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || n_seqs > (1 << 20)) return 0;
+    return SharedLayout(heads, kv_heads, head_dim, n_seqs).bytes;
+}
+
+bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,
+                                                const bitlinear_kv_batch *groups, const void *q, int64_t q_stride, int heads,
+                                                float softmax_scale, void *out, int64_t out_stride, void *workspace,
+                                                size_t workspace_bytes, void *stream)
+{
+    AttendArgs a{}, p{};
+    const int64_t T = batch ? batch->n_seqs : 0;
+    bitlinear_status st = take_attend(a, cache, batch, q, q_stride, T, heads, softmax_scale, out, out_stride, workspace, false);
+    if (st != BITLINEAR_OK) return st;
+    p = a;
+    if ((st = take_views(cache, groups, p.cache, p.batch)) != BITLINEAR_OK) return st;
+    if (!groups->cu_tokens) return BITLINEAR_ERR_ARG;
+    if (T * (heads / a.cache.kv_heads) > (1 << 30)) return BITLINEAR_ERR_SHAPE;
+    const SharedLayout at(heads, a.cache.kv_heads, a.cache.head_dim, T);
+    if (workspace_bytes < at.bytes) return BITLINEAR_ERR_WORKSPACE;
+    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
+    if (T == 0) return BITLINEAR_OK;
+    char *ws = reinterpret_cast<char *>(workspace);
+    a.workspace = ws + at.decode;
+    SharedArgs shared;
+    shared.starts = reinterpret_cast<int32_t *>(ws + at.starts);
+    shared.ml = reinterpret_cast<float2 *>(ws + at.ml);
+    shared.o = reinterpret_cast<float *>(ws + at.o);
+    shared.kv_lens = a.batch.kv_lens;
+    if (groups->n_seqs == 0) return launch_attend_decode(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+    if (launch_attend_prefix(p, shared, (cudaStream_t)stream) != cudaSuccess) return BITLINEAR_ERR_CUDA;
+    return launch_attend_decode_behind(a, shared, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+}
+
+bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
+                                     int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream)
+{
+    SelectArgs a{};
+    bitlinear_status st = take_views(cache, batch, a.cache, a.batch);
+    if (st != BITLINEAR_OK) return st;
+    if ((st = take_marks(marks, a.marks)) != BITLINEAR_OK) return st;
+    if (keep < 1 || keep > ((int64_t)1 << 30) || recent < 0 || recent > keep) return BITLINEAR_ERR_SHAPE;
+    if (a.batch.capacity > kSelectMaxRows || batch->n_seqs * a.cache.kv_heads > (1 << 27)) return BITLINEAR_ERR_SHAPE;
+    if (batch->n_seqs > 0 && (!source || !new_lens || new_lens == batch->kv_lens)) return BITLINEAR_ERR_ARG;
+    if (!aligned(source, 4) || !aligned(new_lens, 4)) return BITLINEAR_ERR_ALIGN;
+    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
+    if (batch->n_seqs == 0) return BITLINEAR_OK;
+    a.source = source;
+    a.new_lens = new_lens;
+    a.keep = (int32_t)keep;
+    a.recent = (int32_t)recent;
+    return launch_kv_select(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+}
+
+bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const int32_t *source,
+                                      int64_t keep, const bitlinear_kv_marks *marks, void *stream)
+{
+    CompactArgs a{};
+    bitlinear_status st = take_views(cache, batch, a.cache, a.batch);
+    if (st != BITLINEAR_OK) return st;
+    if (marks && (st = take_marks(marks, a.marks)) != BITLINEAR_OK) return st;
+    if (keep < 1 || keep > ((int64_t)1 << 30)) return BITLINEAR_ERR_SHAPE;
+    if (batch->n_seqs > 0 && !source) return BITLINEAR_ERR_ARG;
+    if (!aligned(source, 4)) return BITLINEAR_ERR_ALIGN;
+    if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
+    if (batch->n_seqs == 0) return BITLINEAR_OK;
+    a.source = source;
+    a.keep = (int32_t)keep;
+    return launch_kv_compact(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }
 
 } // extern "C"

@@ -91,8 +91,9 @@ template <int VEC, bool kInt8>
 constexpr int kHeadsAtATime = VEC == 2 && !kInt8 ? 4 : 1;
 
 // Three CTAs per SM for the 8-bit rows of 16-byte pieces: their values need 80 registers (four CTAs, with spills: 4 us more).
-// kRotate: 0 none, 1 pairs half a head apart, 2 adjacent pairs.
-template <int VEC, bool kInt8, int kRotate>
+// kRotate: 0 none, 1 pairs half a head apart, 2 adjacent pairs.  kNorm: query and key heads may be normalised first, the
+// positions of the angles may be the caller's, and rows may be marked.
+template <int VEC, bool kInt8, int kRotate, bool kNorm>
 __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kernel(const __grid_constant__ AppendArgs a, const int shares) // warps per token
 {
     ptx::griddep_wait(); // everything below is read from memory that the launch before this one may have written
@@ -112,7 +113,8 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
     if (b < 0) return;
     const int pos = a.batch.kv_lens[b] - count + (t - first);
     if (pos < 0) return;
-    if (pos >= a.batch.capacity || (kRotate != 0 && pos >= a.rope_positions)) {
+    const int angle_pos = kNorm && a.positions ? a.positions[t] : pos;
+    if (pos >= a.batch.capacity || (kRotate != 0 && (angle_pos >= a.rope_positions || (kNorm && angle_pos < 0)))) {
         kv_report(a.cache);
         return;
     }
@@ -124,7 +126,7 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
     const int o1 = kRotate == 2 ? o0 + VEC : half + lane * VEC;
     float2 cs[VEC] = {};
     if (kRotate != 0 && mine) {
-        const float4 *p = reinterpret_cast<const float4 *>(a.rope + (int64_t)pos * half + lane * VEC);
+        const float4 *p = reinterpret_cast<const float4 *>(a.rope + (int64_t)angle_pos * half + lane * VEC);
 #pragma unroll
         for (int i = 0; i < VEC / 2; ++i) {
             const float4 w = p[i];
@@ -163,6 +165,44 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
         // the j-th pair of this lane: (x0[j], x1[j]), or two neighbours
         auto first_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j] : x1[2 * j - VEC]) : x0[j]; };
         auto second_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j + 1] : x1[2 * j + 1 - VEC]) : x1[j]; };
+        // The norm.  An 8-bit row's factor 1 / rms cancels out of its codes, so its key is only multiplied by the gain here.
+        const float *gain = nullptr;
+        float over_rms = 1.0f;
+        if (kNorm && (a.q_gain || a.k_gain)) {
+            gain = is_q ? a.q_gain : (is_k ? a.k_gain : nullptr);
+            const bool normed = gain != nullptr && task < tasks;
+            float squares = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) squares = fmaf(x1[i], x1[i], fmaf(x0[i], x0[i], squares));
+#pragma unroll
+            for (int d = 1; d < kLanes; d <<= 1) squares += __shfl_xor_sync(0xFFFFFFFFu, squares, d);
+            float mean = squares / (float)D + a.norm_eps;
+            // squares near the ends of fp32's range (or of a row that is not finite, or all zero): again in double
+            if (__any_sync(0xFFFFFFFFu, normed && !(squares >= 1e-30f && squares <= 1e37f))) {
+                double wide = 0.0;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) wide += (double)x0[i] * x0[i] + (double)x1[i] * x1[i];
+#pragma unroll
+                for (int d = 1; d < kLanes; d <<= 1) wide += __shfl_xor_sync(0xFFFFFFFFu, wide, d);
+                wide = wide / D + (double)a.norm_eps;
+                if (!(squares >= 1e-30f && squares <= 1e37f)) {
+                    mean = 1.0f;
+                    over_rms = (float)(1.0 / sqrt(wide < 0x1p-126 ? 0x1p-126 : wide)); // (a NaN stays one)
+                }
+            }
+            if (squares >= 1e-30f && squares <= 1e37f) over_rms = 1.0f / sqrtf(mean < 0x1p-126f ? 0x1p-126f : mean);
+            if (normed && work) {
+                const float f = kInt8 && !is_q ? 1.0f : over_rms;
+#pragma unroll
+                for (int i = 0; i < VEC; i += 2) {
+                    const float2 g0 = *reinterpret_cast<const float2 *>(gain + o0 + i), g1 = *reinterpret_cast<const float2 *>(gain + o1 + i);
+                    x0[i] = x0[i] * f * g0.x;
+                    x0[i + 1] = x0[i + 1] * f * g0.y;
+                    x1[i] = x1[i] * f * g1.x;
+                    x1[i + 1] = x1[i + 1] * f * g1.y;
+                }
+            }
+        }
         const bool rotate = kRotate != 0 && (is_q || is_k);
         if (rotate) {
 #pragma unroll
@@ -173,6 +213,10 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
             }
         }
         const int64_t row = is_q || page < 0 ? 0 : kv_row(a.cache, page, h, pos);
+        if (kNorm && a.marks.mass && is_k && page >= 0 && lane == 0) {
+            a.marks.mass[row] = 0.0f;
+            a.marks.pos[row] = angle_pos;
+        }
         if (!kInt8 || is_q) {
             if (work) {
                 __nv_bfloat16 *dst = is_q ? a.q_out + (int64_t)t * a.q_out_stride + h * D
@@ -184,15 +228,19 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
                 reinterpret_cast<__nv_bfloat16 *>(is_k ? a.cache.k : a.cache.v)[row * a.cache.width + D + lane] = __float2bfloat16(0.0f);
         }
         if (kInt8 && task - group + kGroups > a.heads) { // (not for a warp that has queries alone)
-            // element i of x0, then of x1, exactly (up to 2^-53)
+            // element i of x0, then of x1, exactly (up to 2^-53; with a gain, whose product with an element is exact, 2^-51)
+            auto element = [&](int e) -> double {
+                const double x = __bfloat162float(src[e]);
+                return kNorm && gain ? x * gain[e] : x;
+            };
             auto exact = [&](int i) -> double {
                 const int e = i < VEC ? o0 + i : o1 + i - VEC;
-                const double x = __bfloat162float(src[e]);
+                const double x = element(e);
                 if (!rotate) return x;
                 const int pair = kRotate == 2 ? e >> 1 : (e < half ? e : e - half);
                 const bool second = kRotate == 2 ? (e & 1) != 0 : e >= half;
-                const float2 w = a.rope[(int64_t)pos * half + pair];
-                const double y = __bfloat162float(src[kRotate == 2 ? e ^ 1 : (second ? e - half : e + half)]);
+                const float2 w = a.rope[(int64_t)angle_pos * half + pair];
+                const double y = element(kRotate == 2 ? e ^ 1 : (second ? e - half : e + half));
                 return second ? x * (double)w.x + y * (double)w.y : x * (double)w.x - y * (double)w.y;
             };
             float top = 0.0f;
@@ -201,21 +249,27 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
 #pragma unroll
             for (int d = 1; d < kLanes; d <<= 1) top = largest(top, __shfl_xor_sync(0xFFFFFFFFu, top, d), 0.0f);
             // The rotated fp32 values are within 2^-22 of the row's maximum of the exact ones (three roundings of a c and b s,
-            // |a c| + |b s| <= 2 max): only those within 2^-20 of the largest can be the exact maximum.  (Near the end of
+            // |a c| + |b s| <= 2 max; with a gain, two more, 5 2^-24 in all): only those within 2^-20 of the largest can be the exact
+            // maximum.  (Near the end of
             // fp32's range, where a rotation may overflow, nothing is settled in fp32.)
             const bool huge = !(top <= 8e37f);
             bool finite = true; // a row that is not finite stays so when it is rotated: such rows are among the huge ones
             if (__any_sync(0xFFFFFFFFu, huge)) {
                 bool all = true;
                 if (work)
-                    for (int i = 0; i < VEC; ++i) all = all && isfinite(__bfloat162float(src[o0 + i])) && isfinite(__bfloat162float(src[o1 + i]));
+                    for (int i = 0; i < VEC; ++i) {
+                        all = all && isfinite(__bfloat162float(src[o0 + i])) && isfinite(__bfloat162float(src[o1 + i]));
+                        if (kNorm && gain) all = all && isfinite(gain[o0 + i]) && isfinite(gain[o1 + i]);
+                    }
 #pragma unroll
                 for (int d = 1; d < kLanes; d <<= 1) all = __shfl_xor_sync(0xFFFFFFFFu, (int)all, d) && all;
                 finite = all;
             }
             constexpr uint32_t kAll = 2 * VEC == 32 ? ~0u : (1u << (2 * VEC)) - 1u;
             double beta = top;
-            if (rotate) {
+            // (asked of the whole warp, whose rows may be keys and values: the values of a row that is neither rotated nor
+            // multiplied are exact, and so is what comes out here)
+            if (__any_sync(0xFFFFFFFFu, rotate || (kNorm && gain != nullptr))) {
                 beta = 0.0;
                 uint32_t candidates = 0;
 #pragma unroll
@@ -232,12 +286,16 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
                 }
             }
             if (is_q || task >= tasks || page < 0) return;
-            beta = fmax(beta, 1e-5);
+            if (kNorm && gain) {
+                if (!((float)beta * over_rms > 1.01e-5f)) beta = fmax(beta, 1e-5 / (double)over_rms);
+            } else {
+                beta = fmax(beta, 1e-5);
+            }
             int8_t *dst = reinterpret_cast<int8_t *>(is_k ? a.cache.k : a.cache.v) + row * a.cache.width;
             if (mine) {
                 const float inv = __fdividef(127.0f, (float)beta); // (within 2 ulp up to 2^126 > 8e37)
                 // t = 1.5 2^23 + round(x inv): its low byte is the code, and x inv - code is exact but for its last bit.
-                // The estimate of 127 x / beta is off by 127 (2^-22 + 2^-22 + 2^-24) < 7e-5 at most.
+                // The estimate of 127 x / beta is off by 127 (2^-22 + 2^-22 + 2^-24) < 7e-5 at most (with a gain by 8e-5).
                 constexpr float kShift = 12582912.0f, kSettled = 0.4999f;
                 auto value = [&](int i) { return i < VEC ? x0[i] : x1[i - VEC]; };
                 auto beside = [&](float x, float t) { return fmaf(x, inv, kShift - t); };
@@ -279,8 +337,9 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
                 // beta / 127 is within 2^-52 of this product, so it rounds to the same fp32 number unless that lies within a few
                 // units of the middle between two
                 double scale = beta * (1.0 / 127.0);
+                if (kNorm && gain) scale *= (double)over_rms;
                 const int below = (int)(__double_as_longlong(scale) & 0x1FFFFFFF) - 0x10000000;
-                if (below >= -8 && below <= 8) scale = beta / 127.0;
+                if (below >= -8 && below <= 8 && !(kNorm && gain)) scale = beta / 127.0;
                 (is_k ? a.cache.k_scale : a.cache.v_scale)[row] = finite ? (float)scale : __int_as_float(0x7FFFFFFF);
             }
         }
@@ -301,15 +360,25 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
     }
 }
 
-template <int VEC, bool kInt8>
+template <int VEC, bool kInt8, bool kNorm>
 cudaError_t launch_append(const AppendArgs &a, cudaStream_t stream)
 {
     // Warps per token: one round of heads per warp while that does not make more warps than the GPU holds.
     const int groups = (VEC == 8 ? 4 : 1) * kHeadsAtATime<VEC, kInt8>, rounds = (a.heads + 2 * a.cache.kv_heads + groups - 1) / groups;
     const int shares = std::max(1, std::min(rounds, 64 * sm_count() / a.T));
     const unsigned blocks = (unsigned)(((int64_t)a.T * shares + 7) / 8);
-    return launch_dependent(!a.rope ? kv_append_kernel<VEC, kInt8, 0> : (!a.interleaved ? kv_append_kernel<VEC, kInt8, 1> : kv_append_kernel<VEC, kInt8, 2>),
+    return launch_dependent(!a.rope ? kv_append_kernel<VEC, kInt8, 0, kNorm>
+                                    : (!a.interleaved ? kv_append_kernel<VEC, kInt8, 1, kNorm> : kv_append_kernel<VEC, kInt8, 2, kNorm>),
                             blocks, 256, 0, stream, a, shares);
+}
+
+template <bool kNorm>
+cudaError_t launch_append(const AppendArgs &a, cudaStream_t stream)
+{
+    // 16-byte pieces need halves of a head that are multiples of 8 elements
+    const bool wide = a.cache.head_dim % 16 == 0;
+    if (a.cache.k_scale) return wide ? launch_append<8, true, kNorm>(a, stream) : launch_append<2, true, kNorm>(a, stream);
+    return wide ? launch_append<8, false, kNorm>(a, stream) : launch_append<2, false, kNorm>(a, stream);
 }
 
 } // namespace
@@ -321,12 +390,7 @@ cudaError_t launch_rope_table(float *table, int64_t n_pos, int head_dim, double 
     return cudaGetLastError();
 }
 
-cudaError_t launch_kv_append(const AppendArgs &a, cudaStream_t stream)
-{
-    // 16-byte pieces need halves of a head that are multiples of 8 elements
-    const bool wide = a.cache.head_dim % 16 == 0;
-    if (a.cache.k_scale) return wide ? launch_append<8, true>(a, stream) : launch_append<2, true>(a, stream);
-    return wide ? launch_append<8, false>(a, stream) : launch_append<2, false>(a, stream);
-}
+cudaError_t launch_kv_append(const AppendArgs &a, cudaStream_t stream) { return launch_append<false>(a, stream); }
+cudaError_t launch_kv_append_rmsnorm(const AppendArgs &a, cudaStream_t stream) { return launch_append<true>(a, stream); }
 
 } // namespace bitlinear
