@@ -423,8 +423,8 @@ bitlinear_status bitlinear_attend_prompt(const bitlinear_kv_cache *cache, const 
  * token's position).
  */
 typedef struct {
-    float *mass;  /* device */
-    int32_t *pos; /* device */
+    float *mass;  /* device, 16-byte aligned */
+    int32_t *pos; /* device, 16-byte aligned */
 } bitlinear_kv_marks;
 
 /*
@@ -470,7 +470,7 @@ bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, 
  *                  stays; the j-th of the rows at or behind `keep` that stay, for the j-th place below `keep` whose row goes;
  *                  -1 behind the end of a sequence of fewer rows
  *   new_lens  out  int32 [n_seqs]: min(kv_lens[b], keep); must not be kv_lens itself
- *   0 <= recent <= keep, 1 <= keep <= 2^30;  table_pages * page_size <= 2^21;  n_seqs * kv_heads <= 2^27
+ *   0 <= recent <= keep, 1 <= keep <= 2^30;  table_pages * page_size <= 2^18;  n_seqs * kv_heads <= 2^27
  * cu_tokens is not looked at.
  */
 bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,

@@ -184,7 +184,7 @@ struct SelectArgs {
     int32_t *source, *new_lens;
     int32_t keep, recent;
 };
-constexpr int64_t kSelectMaxRows = (int64_t)1 << 21; // of a sequence
+constexpr int64_t kSelectMaxRows = (int64_t)1 << 18; // of a sequence
 cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream);
 
 struct CompactArgs {

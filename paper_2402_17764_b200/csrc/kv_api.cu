@@ -131,7 +131,7 @@ bitlinear_status take_append(AppendArgs &a, bool &idle, const bitlinear_kv_cache
 bitlinear_status take_marks(const bitlinear_kv_marks *marks, KvMarks &m)
 {
     if (!marks || !marks->mass || !marks->pos) return BITLINEAR_ERR_ARG;
-    if (!aligned(marks->mass, 4) || !aligned(marks->pos, 4)) return BITLINEAR_ERR_ALIGN;
+    if (!aligned(marks->mass, 16) || !aligned(marks->pos, 16)) return BITLINEAR_ERR_ALIGN;
     m.mass = marks->mass;
     m.pos = marks->pos;
     return BITLINEAR_OK;

@@ -2,12 +2,20 @@
 //
 // Selection, for every (sequence, kv head) of n rows of which `keep` stay.  A row's worth is a 32-bit number: the bits of its
 // weight (not negative, so they order as the weights do), or the largest number for the rows of the `recent` newest positions.
-// The keep-th largest worth is found digit by digit (11, 11 and 10 bits: a histogram of the rows that agree with the digits found so
-// far, summed from above); rows above it stay, and of the rows equal to it the first ones.  Which rows stay is kept as a bit per
-// row, with the number of bits in front of every word, so that the j-th hole (a row below `keep` that goes) finds the j-th row to be
-// moved (at or behind `keep`) by a search in those numbers.  Nothing depends on the order in which threads run.
+// The keep-th largest worth is found digit by digit (10, 11 and 11 bits: a histogram of the rows that agree with the digits found so
+// far, summed from above, until the rows from there on are `keep` in all); rows above it stay, and of the rows equal to it the first
+// ones.  Which rows stay is kept as a bit per row, with the number of holes (rows below `keep` that go) and of rows to be moved (at
+// or behind `keep`) in front of every word; the j-th row to be moved takes its hole from a list of the holes in order.  Nothing
+// depends on the order in which threads run.
 //
-// A cluster of CTAs shares a (sequence, kv head), each of them a contiguous stretch of the rows.
+// A cluster of CTAs shares a (sequence, kv head), each of them a contiguous stretch of the rows, whose marks are read once and
+// kept in shared memory.  Histograms are added up by atomics into every CTA's shared memory (of the few bins that hold anything: reading
+// all bins of the others took 1000 cycles for each of them); the list of holes goes by way of the output array (gathering it from
+// another CTA's shared memory took 2 cycles a row).
+//
+// What bounds it: latency.  1 x 32 heads of 2064 rows: 9.5 us, 17000 cycles, of which 2400 load the marks and the rest are barriers and
+// chains of a few dependent accesses in ten steps.  16 sequences of 6000 to 65535 rows, 8 heads: 42-45 us where the marks' 28 MB take
+// 4.4: two waves of CTAs, each 40000 cycles, 12000 of them (at 5.7 TB/s) loading.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -21,21 +29,31 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kDigits = 3, kBins = 2048;
-__device__ __forceinline__ int digit_shift(int d) { return d == 0 ? 21 : (d == 1 ? 10 : 0); }
+constexpr size_t kSelectSmem = 220 * 1024;
+constexpr int kDigits = 3;    // of 10, 11 and 11 bits
+constexpr int kBins = 2048;
+constexpr int kFirstBins = 1024, kCopies = 4; // the first digit's bins, exponents above all, are few, and so are kept four times
+__device__ __forceinline__ int digit_shift(int d) { return d == 0 ? 22 : (d == 1 ? 11 : 0); }
 
-struct SelectShared {
-    uint32_t bins[kDigits][kBins];
-    int scan[kSelectWarps];
-    int digit, above;        // found: the digit, and how many rows are above it
-    int ties, holes, movers; // of this CTA's stretch
+struct alignas(16) SelectShared {
+    union {
+        uint32_t first[kFirstBins][kCopies];
+        uint32_t sums[kDigits - 1][kBins]; // of the other digits' bins, over all CTAs
+    };
+    uint32_t first_sums[kFirstBins]; // of the first digit's bins, over the copies and all CTAs
+    uint32_t bins[kDigits - 1][kBins];
+    int scan[32];
+    int4 found;           // the digit, how many rows are above it, and how many have it
+    int ties[kMaxCluster]; // of every CTA's stretch
+    int2 moves[kMaxCluster]; // the same: holes, and rows to be moved
 };
 
 // Sum over the CTA of x of the threads in front of this one; total: of all of them.
+template <int kThreads>
 __device__ __forceinline__ int scan_block(int x, int *scan, int &total)
 {
+    constexpr int kWarps = kThreads / 32;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     int upto = x;
 #pragma unroll
@@ -46,45 +64,60 @@ __device__ __forceinline__ int scan_block(int x, int *scan, int &total)
     __syncthreads(); // (scan may still be read from the call before)
     if (lane == 31) scan[warp] = upto;
     __syncthreads();
-    int before = 0;
-    total = 0;
+    const int own = lane < kWarps ? scan[lane] : 0;
+    int sums = own;
 #pragma unroll
-    for (int w = 0; w < kSelectWarps; ++w) {
-        if (w < warp) before += scan[w];
-        total += scan[w];
+    for (int d = 1; d < kWarps; d <<= 1) {
+        const int y = __shfl_up_sync(0xFFFFFFFFu, sums, d);
+        if (lane >= d) sums += y;
     }
-    return before + upto - x;
+    total = __shfl_sync(0xFFFFFFFFu, sums, kWarps - 1);
+    return __shfl_sync(0xFFFFFFFFu, sums - own, warp) + upto - x;
 }
 
-// Replaces counts[0 .. n) by the sums in front of each; returns the sum of all.
-__device__ __forceinline__ int scan_words(int *counts, int n, int *scan)
+// before[w] = the sum of count(0 .. w - 1); returns the sum of all n.
+template <int kThreads, typename Count>
+__device__ __forceinline__ int scan_words(int *before, int n, int *scan, Count &&count)
 {
     int sum = 0;
-    for (int w0 = 0; w0 < n; w0 += kSelectThreads) {
+    for (int w0 = 0; w0 < n; w0 += kThreads) {
         const int w = w0 + (int)threadIdx.x;
         int total;
-        const int before = scan_block(w < n ? counts[w] : 0, scan, total);
-        if (w < n) counts[w] = sum + before;
+        const int own = scan_block<kThreads>(w < n ? count(w) : 0, scan, total);
+        if (w < n) before[w] = sum + own;
         sum += total;
     }
-    __syncthreads();
     return sum;
 }
 
 // Words of 32 rows in a CTA's stretch of a sequence of so many rows.
 int stretch_words(int64_t rows, int cluster) { return (int)(((rows + 31) / 32 + cluster - 1) / cluster); }
 
-__global__ void __launch_bounds__(kSelectThreads) kv_select_kernel(const __grid_constant__ SelectArgs a, const int max_words)
+// C: CTAs that share a (sequence, kv head).
+template <int C, int kThreads>
+__global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_constant__ SelectArgs a, const int max_words)
 {
     ptx::griddep_wait(); // everything below is read from memory that the launch before this one may have written
     ptx::griddep_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
-    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int rank = C > 1 ? (int)cluster.block_rank() : 0;
+    auto sync_all = [&] {
+        if (C > 1)
+            cluster.sync();
+        else
+            __syncthreads();
+    };
+    auto for_all = [&](auto &&f) { // f(of): what `of` gives of a place in shared memory is that place of one CTA after the other
+#pragma unroll
+        for (int r = 0; r < C; ++r) f([&](auto *p) { return C > 1 ? cluster.map_shared_rank(p, r) : p; });
+    };
     extern __shared__ __align__(16) uint8_t smem[];
     SelectShared &sh = *reinterpret_cast<SelectShared *>(smem);
-    uint32_t *stays = reinterpret_cast<uint32_t *>(smem + sizeof(SelectShared)); // a bit per row of the stretch
-    int *before = reinterpret_cast<int *>(stays + max_words);                     // per word: what is in front of it in the stretch
-    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    uint4 *cached = reinterpret_cast<uint4 *>(smem + sizeof(SelectShared)); // the worth of the stretch's rows
+    int *list = reinterpret_cast<int *>(cached);                             // and later the holes that its rows are moved to
+    uint32_t *stays = reinterpret_cast<uint32_t *>(cached + max_words * 8);  // a bit per row of the stretch
+    int *before = reinterpret_cast<int *>(stays + max_words);                // per word: what is in front of it in the stretch
+    const int tid = threadIdx.x;
     const int Hk = a.cache.kv_heads, keep = a.keep;
     const int pair = (int)blockIdx.x / C, b = pair / Hk, h = pair - b * Hk;
     bool over;
@@ -95,7 +128,7 @@ __global__ void __launch_bounds__(kSelectThreads) kv_select_kernel(const __grid_
     }
     int32_t *source = a.source + (int64_t)pair * keep;
     if (n <= keep) { // (the whole cluster)
-        for (int i = rank * kSelectThreads + tid; i < keep; i += C * kSelectThreads) source[i] = i < n ? i : -1;
+        for (int i = rank * kThreads + tid; i < keep; i += C * kThreads) source[i] = i < n ? i : -1;
         return;
     }
     auto row_of = [&](int i) {
@@ -103,143 +136,195 @@ __global__ void __launch_bounds__(kSelectThreads) kv_select_kernel(const __grid_
         return page < 0 ? -1 : kv_row(a.cache, page, h, i);
     };
     const int last = row_of(n - 1);
-    const int64_t oldest = last < 0 ? INT64_MAX : (int64_t)a.marks.pos[last] - a.recent; // what is newer stays
-    auto worth = [&](int i, bool report) -> uint32_t {
-        const int row = row_of(i);
-        if (row < 0) {
-            if (report) kv_report(a.cache);
-            return 0u;
-        }
-        if ((int64_t)a.marks.pos[row] > oldest) return 0xFFFFFFFFu;
-        const float w = a.marks.mass[row];
-        return w > 0.0f ? __float_as_uint(w) : 0u; // (nothing, or not a number: 0)
-    };
+    const int64_t after = last < 0 ? INT32_MAX : (int64_t)a.marks.pos[last] - a.recent + 1;
+    const int newest = (int)(after < INT32_MIN ? INT32_MIN : (after > INT32_MAX ? INT32_MAX : after)); // what is as new as this stays
+    const bool some_new = last >= 0;
     const int all_words = (n + 31) / 32, each = (all_words + C - 1) / C;
     const int word0 = min(all_words, rank * each), words = min(all_words, word0 + each) - word0; // of this stretch
+    const int row0 = word0 * 32, rows = min(n, row0 + words * 32) - row0;
+    auto worth_of = [&](float mass, int pos) { // (nothing, or not a number: 0)
+        return some_new && pos >= newest ? 0xFFFFFFFFu : (mass > 0.0f ? __float_as_uint(mass) : 0u);
+    };
+    // Rows are taken in pieces of four, which lie in one page and may reach behind the sequence's end.
+    auto load_four = [&](int row) {
+        if (row < 0) return make_uint4(0u, 0u, 0u, 0u);
+        const float4 m = *reinterpret_cast<const float4 *>(a.marks.mass + row);
+        const int4 p = *reinterpret_cast<const int4 *>(a.marks.pos + row);
+        return make_uint4(worth_of(m.x, p.x), worth_of(m.y, p.y), worth_of(m.z, p.z), worth_of(m.w, p.w));
+    };
+    const int pieces = words * 8, lane = tid % 32;
+    auto real_of = [&](int p) { return rows - p * 4 >= 4 ? 15u : (rows > p * 4 ? (1u << (rows - p * 4)) - 1u : 0u); }; // rows of a piece that exist
+    auto bits_of = [&](int p, auto &&holds) { // the rows of a piece for which it holds
+        const uint4 x = cached[p];
+        return ((uint32_t)holds(x.x) | (uint32_t)holds(x.y) << 1 | (uint32_t)holds(x.z) << 2 | (uint32_t)holds(x.w) << 3) & real_of(p);
+    };
+    auto word_of = [&](uint32_t bits) { // the word whose pieces eight neighbouring lanes have
+        bits <<= lane % 8 * 4;
+        bits |= __shfl_xor_sync(0xFFFFFFFFu, bits, 1);
+        bits |= __shfl_xor_sync(0xFFFFFFFFu, bits, 2);
+        return bits | __shfl_xor_sync(0xFFFFFFFFu, bits, 4);
+    };
 
     // ---- the keep-th largest worth, and how many rows are above it -----------------------------------------
-    for (int i = tid; i < kDigits * kBins; i += kSelectThreads) (&sh.bins[0][0])[i] = 0u;
+    for (int i = tid; i < (kFirstBins * (kCopies + 1) + (kDigits - 1) * kBins) / 4; i += kThreads) reinterpret_cast<uint4 *>(&sh)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 0) sh.found = make_int4(0, 0, 0, 0);
     __syncthreads();
-    uint32_t least = 0u; // its digits found so far
-    int above = 0;
-    for (int d = 0; d < kDigits; ++d) {
-        const int shift = digit_shift(d);
-        for (int w = warp; w < words; w += kSelectWarps) {
-            const int i = (word0 + w) * 32 + lane;
-            if (i >= n) continue;
-            const uint32_t x = worth(i, d == 0);
-            if (d == 0 || ((x ^ least) >> digit_shift(d - 1)) == 0u) atomicAdd(&sh.bins[d][(x >> shift) & (d == 2 ? 1023u : 2047u)], 1u);
-        }
-        cluster.sync();
-        int mine[kBins / kSelectThreads], sum = 0; // from the largest digit down
+    if (C > 1) cluster.barrier_arrive(); // (the others may add to these bins)
+    constexpr int kInFlight = 4; // pieces of a thread whose marks are being loaded
+    for (int i0 = tid * 4; i0 < rows; i0 += kInFlight * kThreads * 4) {
+        int row[kInFlight];
+        uint4 x[kInFlight];
 #pragma unroll
-        for (int u = 0; u < kBins / kSelectThreads; ++u) {
-            const int bin = kBins - 1 - (tid * (kBins / kSelectThreads) + u);
-            int x = 0;
-            for (int r = 0; r < C; ++r) x += (int)*cluster.map_shared_rank(&sh.bins[d][bin], r);
-            mine[u] = x;
-            sum += x;
+        for (int u = 0; u < kInFlight; ++u) {
+            const int i = i0 + u * kThreads * 4;
+            row[u] = i < rows ? row_of(row0 + i) : -1;
+            if (i < rows && row[u] < 0) kv_report(a.cache);
+        }
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) x[u] = load_four(row[u]);
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) {
+            const int i = i0 + u * kThreads * 4;
+            if (i >= rows) break;
+            cached[i / 4] = x[u];
+            const uint32_t y[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < rows) atomicAdd(&sh.first[y[e] >> digit_shift(0)][lane % kCopies], 1u);
+        }
+    }
+    uint32_t least = 0u; // its digits found so far, zeros behind them
+    int above = 0;
+    bool exact = false;  // the rows with a worth of `least` or more are `keep` in all
+    for (int d = 0; d < kDigits && !exact; ++d) {
+        const int shift = digit_shift(d);
+        if (d > 0) {
+            const uint32_t span = 1u << digit_shift(d - 1); // (least begins with the digits found: those that agree are less than this above it)
+            for (int p = tid; p < pieces; p += kThreads) {
+                const uint32_t real = real_of(p);
+                const uint4 x = cached[p];
+                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (y[e] - least < span && ((real >> e) & 1u)) atomicAdd(&sh.bins[d - 1][(y[e] - least) >> shift], 1u);
+            }
+        }
+        // the bins of all CTAs are added up in each of them, by those that have something in them
+        __syncthreads();
+        if (d == 0) {
+            if (C > 1) cluster.barrier_wait();
+            for (int i = tid; i < kFirstBins; i += kThreads) {
+                const uint4 y = *reinterpret_cast<const uint4 *>(sh.first[i]);
+                const uint32_t x = y.x + y.y + y.z + y.w;
+                *reinterpret_cast<uint4 *>(sh.first[i]) = make_uint4(0u, 0u, 0u, 0u); // (as the sums of the other digits)
+                if (x != 0u) for_all([&](auto &&of) { atomicAdd(of(&sh.first_sums[i]), x); });
+            }
+        } else if (C > 1) {
+            for (int i = tid; i < kBins; i += kThreads) {
+                const uint32_t x = sh.bins[d - 1][i];
+                if (x != 0u) for_all([&](auto &&of) { atomicAdd(of(&sh.sums[d - 1][i]), x); });
+            }
+        }
+        if (C > 1 || d == 0) sync_all();
+        const uint32_t *sums = d == 0 ? sh.first_sums : (C > 1 ? sh.sums[d - 1] : sh.bins[d - 1]);
+        constexpr int kMine = kBins / kThreads;
+        int mine[kMine], sum = 0; // from the largest digit down
+#pragma unroll
+        for (int u = 0; u < kMine; ++u) {
+            const int bin = kBins - 1 - (tid * kMine + u);
+            mine[u] = d > 0 || bin < kFirstBins ? (int)sums[bin] : 0;
+            sum += mine[u];
         }
         int total;
-        int upto = above + scan_block(sum, sh.scan, total);
+        int upto = above + scan_block<kThreads>(sum, sh.scan, total);
 #pragma unroll
-        for (int u = 0; u < kBins / kSelectThreads; ++u) {
-            if (upto < keep && upto + mine[u] >= keep) { // (of exactly one thread)
-                sh.digit = kBins - 1 - (tid * (kBins / kSelectThreads) + u);
-                sh.above = upto;
-            }
+        for (int u = 0; u < kMine; ++u) {
+            if (upto < keep && upto + mine[u] >= keep) sh.found = make_int4(kBins - 1 - (tid * kMine + u), upto, mine[u], 0); // (one thread's)
             upto += mine[u];
         }
         __syncthreads();
-        least |= (uint32_t)sh.digit << shift;
-        above = sh.above;
-        __syncthreads();
+        const int4 found = sh.found;
+        least |= (uint32_t)found.x << shift;
+        above = found.y;
+        exact = above + found.z == keep; // (read again only behind the next round's barriers)
     }
 
     // ---- which rows stay: those above, and the first of those equal to it --------------------------------------
-    for (int w = warp; w < words; w += kSelectWarps) {
-        const int i = (word0 + w) * 32 + lane;
-        const uint32_t equal = __ballot_sync(0xFFFFFFFFu, i < n && worth(i, false) == least);
-        if (lane == 0) before[w] = __popc(equal);
-    }
-    __syncthreads();
-    const int ties = scan_words(before, words, sh.scan);
-    if (tid == 0) sh.ties = ties;
-    cluster.sync();
-    int wanted = keep - above; // of the rows equal to it, from this stretch on
-    for (int r = 0; r < rank; ++r) wanted -= *cluster.map_shared_rank(&sh.ties, r);
-    for (int w = warp; w < words; w += kSelectWarps) {
-        const int i = (word0 + w) * 32 + lane;
-        const uint32_t x = i < n ? worth(i, false) : 0u;
-        const bool is_equal = i < n && x == least;
-        const uint32_t equal = __ballot_sync(0xFFFFFFFFu, is_equal);
-        const bool in = (i < n && x > least) || (is_equal && before[w] + __popc(equal & ((1u << lane) - 1u)) < wanted);
-        const uint32_t bits = __ballot_sync(0xFFFFFFFFu, in);
-        const uint32_t below = __ballot_sync(0xFFFFFFFFu, i < keep); // (keep < n: all of them are rows)
-        __syncwarp();
-        if (lane == 0) {
-            stays[w] = bits;
-            before[w] = __popc(below & ~bits) + __popc(bits & ~below); // holes, and rows to be moved
+    int wanted = 0; // of the rows equal to it, from this stretch on
+    if (!exact) {
+        for (int p0 = tid - lane; p0 < pieces; p0 += kThreads) {
+            const int p = p0 + lane;
+            const uint32_t equal = word_of(p < pieces ? bits_of(p, [&](uint32_t x) { return x == least; }) : 0u);
+            if (p < pieces && lane % 8 == 0) stays[p / 8] = equal;
         }
+        __syncthreads();
+        const int ties = scan_words<kThreads>(before, words, sh.scan, [&](int w) { return __popc(stays[w]); });
+        if (tid == 0) for_all([&](auto &&of) { *of(&sh.ties[rank]) = ties; });
+        sync_all();
+        wanted = keep - above;
+        for (int r = 0; r < rank; ++r) wanted -= sh.ties[r];
+    }
+    const uint32_t bound = exact ? least - 1u : least; // (with keep < n rows at or above it, an exact one is not 0)
+    for (int p0 = tid - lane; p0 < pieces; p0 += kThreads) {
+        const int p = p0 + lane;
+        uint32_t bits = 0u;
+        if (p < pieces) {
+            bits = bits_of(p, [&](uint32_t x) { return x > bound; });
+            if (!exact) {
+                const uint32_t equal = stays[p / 8];
+                uint32_t mine = (equal >> (p % 8 * 4)) & 15u;
+                for (int some = wanted - before[p / 8] - __popc(equal & ((1u << (p % 8 * 4)) - 1u)); some > 0 && mine; --some, mine &= mine - 1u) bits |= mine & (0u - mine);
+            }
+        }
+        bits = word_of(bits); // (and behind this all lanes have read the word of the equal rows)
+        if (p < pieces && lane % 8 == 0) stays[p / 8] = bits;
     }
     __syncthreads();
 
     // ---- the j-th row to be moved goes to the j-th hole.  All holes are in front of all rows to be moved ------------
-    const int both = scan_words(before, words, sh.scan);
-    // this stretch's holes: those in the words below keep, and the lower part of the word that keep lies in
-    if (tid == 0) {
-        const int w = keep / 32 - word0;
-        int holes = w < 0 ? 0 : (w >= words ? both : before[w]);
-        if (w >= 0 && w < words) holes += __popc(~stays[w] & ((1u << (keep % 32)) - 1u));
-        sh.holes = holes;
-        sh.movers = both - holes;
-    }
-    cluster.sync();
-    int hole0 = 0, first_mover[kMaxCluster]; // holes in front of the stretch, rows to be moved in front of every stretch
-#pragma unroll
-    for (int r = 0, sum = 0; r < kMaxCluster; ++r) {
-        first_mover[r] = sum;
-        if (r < C) {
-            if (r < rank) hole0 += *cluster.map_shared_rank(&sh.holes, r);
-            sum += *cluster.map_shared_rank(&sh.movers, r);
+    const int keep_word = keep / 32 - word0; // the word that keep lies in (keep < n: the rows below it all exist)
+    const uint32_t keep_mask = (1u << (keep % 32)) - 1u;
+    auto below_of = [&](int w) { return w < keep_word ? ~0u : (w == keep_word ? keep_mask : 0u); };
+    const int both = scan_words<kThreads>(before, words, sh.scan, [&](int w) { return __popc(stays[w] ^ below_of(w)); }); // holes, then rows to be moved
+    __syncthreads();
+    int my_holes = keep_word < 0 ? 0 : (keep_word >= words ? both : before[keep_word]);
+    if (keep_word >= 0 && keep_word < words) my_holes += __popc(~stays[keep_word] & keep_mask);
+    int hole0 = 0, mover0 = 0; // holes, and rows to be moved, in front of this stretch
+    if (C > 1) {
+        if (tid == 0) for_all([&](auto &&of) { *of(&sh.moves[rank]) = make_int2(my_holes, both - my_holes); });
+        cluster.sync();
+        for (int r = 0; r < rank; ++r) {
+            hole0 += sh.moves[r].x;
+            mover0 += sh.moves[r].y;
         }
     }
-    for (int w = warp; w < words; w += kSelectWarps) {
-        const int i = (word0 + w) * 32 + lane;
-        if (i >= keep) continue;
-        const uint32_t bits = stays[w];
-        int from = i;
-        if (!((bits >> lane) & 1u)) {
-            const int j = hole0 + before[w] + __popc(~bits & ((1u << lane) - 1u));
-            int r = 0;
+    // The holes are listed: of a CTA on its own where its rows' worth stood, of several in `source`, from where each takes
+    // those of its rows to its own list before anything else is written there.
+    int *holes_to = C > 1 ? source + hole0 : list;
+    for (int p = tid; p < min(pieces, max(0, (keep - row0 + 3) / 4)); p += kThreads) {
+        const uint32_t bits = ~stays[p / 8];
+        int j = before[p / 8] + __popc(bits & ((1u << (p % 8 * 4)) - 1u));
 #pragma unroll
-            for (int u = 1; u < kMaxCluster; ++u)
-                if (u < C && first_mover[u] <= j) r = u;
-            int at = j;
-#pragma unroll
-            for (int u = 1; u < kMaxCluster; ++u)
-                if (u == r) at = j - first_mover[u];
-            const uint32_t *its_stays = cluster.map_shared_rank(stays, r);
-            const int *its_before = cluster.map_shared_rank(before, r);
-            const int its_holes = *cluster.map_shared_rank(&sh.holes, r);
-            // the last word with at most `at` rows to be moved in front of it
-            int lo = 0, hi = min(all_words, r * each + each) - r * each;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (its_before[mid] - its_holes <= at)
-                    lo = mid;
-                else
-                    hi = mid;
-            }
-            const int word = r * each + lo;
-            uint32_t moved = its_stays[lo];
-            if (word * 32 < keep) moved &= ~((1u << (keep - word * 32)) - 1u); // (keep lies in this word)
-            for (int rest = at - max(0, its_before[lo] - its_holes); rest > 0; --rest) moved &= moved - 1u;
-            from = word * 32 + __ffs(moved) - 1;
-        }
-        source[i] = from;
+        for (int e = 0; e < 4; ++e)
+            if (((bits >> (p % 8 * 4 + e)) & 1u) && row0 + p * 4 + e < keep) holes_to[j++] = row0 + p * 4 + e;
     }
-    cluster.sync(); // (others may still look into this CTA's words)
+    if (C > 1) {
+        __threadfence();
+        cluster.sync();
+        for (int j = tid; j < both - my_holes; j += kThreads) list[j] = __ldcg(source + mover0 + j);
+        cluster.sync();
+    } else {
+        __syncthreads();
+    }
+    for (int i = tid; i < min(rows, keep - row0); i += kThreads)
+        if ((stays[i / 32] >> (i % 32)) & 1u) source[row0 + i] = row0 + i;
+    for (int w = max(0, keep_word) + tid; w < words; w += kThreads) {
+        uint32_t moved = stays[w] & ~below_of(w);
+        for (int j = max(0, before[w] - my_holes); moved; moved &= moved - 1u, ++j) {
+            const int to = list[j];
+            if ((uint32_t)to < (uint32_t)keep) source[to] = row0 + w * 32 + __ffs(moved) - 1; // (always, unless the marks change meanwhile)
+        }
+    }
 }
 
 // Moves row source[i] of every sequence and kv head to row i.  A warp takes 32 rows i at a time, looks at what moves with a
@@ -310,43 +395,55 @@ __global__ void __launch_bounds__(kCompactThreads) kv_compact_kernel(const __gri
     }
 }
 
-} // namespace
+size_t select_smem(int64_t rows, int cluster) { return sizeof(SelectShared) + (size_t)stretch_words(rows, cluster) * (128 + 8); }
+static_assert(sizeof(SelectShared) + kSelectMaxRows / 32 / kMaxCluster * (128 + 8) <= kSelectSmem, "the longest stretch");
 
-cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream)
+template <int C, int kThreads>
+cudaError_t launch_select(const SelectArgs &a, cudaStream_t stream)
 {
-    const int64_t pairs = (int64_t)a.batch.n_seqs * a.cache.kv_heads;
-    // CTAs per (sequence, kv head): more while there are idle SMs and a stretch is long enough to be worth it, and as many as the
-    // bits of the longest sequence need.
-    constexpr size_t kMost = 200 * 1024;
-    auto bytes_of = [&](int c) { return sizeof(SelectShared) + (size_t)stretch_words(a.batch.capacity, c) * 8; };
-    int cluster = 1;
-    while (cluster < kMaxCluster && (bytes_of(cluster) > kMost || (pairs * cluster * 2 <= 2 * sm_count() && a.batch.capacity / cluster > 4096))) cluster *= 2;
-    const size_t smem = bytes_of(cluster);
-    if (smem > kMost) return cudaErrorInvalidValue;
     static bool ready[64] = {false};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev]) {
-        e = cudaFuncSetAttribute(kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
+        e = cudaFuncSetAttribute(kv_select_kernel<C, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSelectSmem);
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
+    const int words = stretch_words(a.batch.capacity, C);
     cudaLaunchAttribute attributes[2];
     attributes[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attributes[0].val.programmaticStreamSerializationAllowed = 1;
     attributes[1].id = cudaLaunchAttributeClusterDimension;
-    attributes[1].val.clusterDim.x = (unsigned)cluster;
+    attributes[1].val.clusterDim.x = (unsigned)C;
     attributes[1].val.clusterDim.y = attributes[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t config = {};
-    config.gridDim = dim3((unsigned)(pairs * cluster));
-    config.blockDim = dim3(kSelectThreads);
-    config.dynamicSmemBytes = smem;
+    config.gridDim = dim3((unsigned)((int64_t)a.batch.n_seqs * a.cache.kv_heads * C));
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = select_smem(a.batch.capacity, C);
     config.stream = stream;
     config.attrs = attributes;
-    config.numAttrs = 2;
-    return cudaLaunchKernelEx(&config, kv_select_kernel, a, stretch_words(a.batch.capacity, cluster));
+    config.numAttrs = C > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&config, kv_select_kernel<C, kThreads>, a, words);
+}
+
+} // namespace
+
+cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream)
+{
+    const int64_t pairs = (int64_t)a.batch.n_seqs * a.cache.kv_heads;
+    // CTAs per (sequence, kv head): as many as the rows of the longest sequence need shared memory of, and more while they all run at
+    // once and a stretch is long enough to be worth the clusters' barriers (8 pairs of 131000 rows, eight CTAs each: 21 us; 32
+    // pairs of 9000: two 15.8 us, one 17; 32 of 2064: two 13.4, one 9.5).
+    int cluster = 1;
+    while (cluster < kMaxCluster && (select_smem(a.batch.capacity, cluster) > kSelectSmem || (pairs * cluster <= sm_count() && a.batch.capacity / cluster > 8192)))
+        cluster *= 2;
+    // Short sequences of many pairs take fewer threads, so that several CTAs share an SM (2560 pairs of 200 to 500 rows: 34 us with 256
+    // threads, 68 with 1024; 32 pairs of 2064 rows: 10.5 and 9.6).
+    if (cluster == 1) return pairs > sm_count() && a.batch.capacity <= 4096 ? launch_select<1, 256>(a, stream) : launch_select<1, 1024>(a, stream);
+    if (cluster == 2) return launch_select<2, 1024>(a, stream);
+    return cluster == 4 ? launch_select<4, 1024>(a, stream) : launch_select<8, 1024>(a, stream);
 }
 
 cudaError_t launch_kv_compact(const CompactArgs &a, cudaStream_t stream)

@@ -112,7 +112,7 @@ def test_arguments_of_evicting_that_are_refused(B):  # noqa: F811
         (dict(source=FAKE + 2), "ERR_ALIGN"), (dict(new_lens=FAKE + 65), "ERR_ALIGN"),
     ]:
         assert select(B, c, s, **changes) == getattr(B, status), changes
-    long = dict(cu_tokens=None, table_pages=(1 << 21) // 16 + 1, table_stride=1 << 20)
+    long = dict(cu_tokens=None, table_pages=(1 << 18) // 16 + 1, table_stride=1 << 20)
     assert select(B, c, batch(B, **long)) == B.ERR_SHAPE
     assert select(B, cache(B, kv_heads=256, n_pages=4), batch(B, cu_tokens=None, n_seqs=(1 << 19) + 1)) == B.ERR_SHAPE
     for changes, status in [
