@@ -569,6 +569,44 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
     uint32_t *counters = reinterpret_cast<uint32_t *>(ws);
     float *parts = reinterpret_cast<float *>(ws + decode_counter_bytes());
     auto part_of = [&](int share, int which) { return parts + (int64_t)(share * kMaxSplits + which) * S::kPartFloats; };
+    // Adds the shared rows' result for four elements of query head `at` (counted over all sequences) to (x, M, L).
+    auto join_shared = [&](int64_t at, int e, float4 &x, float &M, float &L) {
+        if constexpr (kMode == kBehind) {
+            const int2 where = more.where[at];
+            const bool direct = where.x < 0;
+            const int n = direct ? 1 : where.y >> 16, row = where.y & 0xFFFF;
+            const size_t part = direct ? 0 : prompt_part_floats(W);
+            const float *from = more.parts + (direct ? 0 : (size_t)where.x * part);
+            const float2 *ml = direct ? more.ml + at : reinterpret_cast<const float2 *>(from) + row;
+            const float4 *o = direct ? reinterpret_cast<const float4 *>(more.o + at * W + e)
+                                     : reinterpret_cast<const float4 *>(from + 2 * kPromptRows) + (size_t)(e / 4) * kPromptRows + row;
+            constexpr int kAtATime = 4;
+            for (int c = 0; c < n; c += kAtATime) {
+                float2 y[kAtATime];
+                float4 v[kAtATime];
+#pragma unroll
+                for (int u = 0; u < kAtATime; ++u) {
+                    const int p = min(c + u, n - 1);
+                    y[u] = ml[p * part / 2];
+                    v[u] = o[p * part / 4];
+                }
+                float top = M;
+#pragma unroll
+                for (int u = 0; u < kAtATime; ++u) top = fmaxf(top, y[u].x);
+                const float base = top == -INFINITY ? 0.0f : top, keep = exp2_approx(M - base);
+                x = make_float4(x.x * keep, x.y * keep, x.z * keep, x.w * keep);
+                L *= keep;
+                M = top;
+#pragma unroll
+                for (int u = 0; u < kAtATime; ++u)
+                    if (c + u < n) {
+                        const float f = exp2_approx(y[u].x - base);
+                        add_scaled(x, f, v[u]);
+                        L += f * y[u].y;
+                    }
+            }
+        }
+    };
     auto store_out = [&](const Place &p, int q, int e, float4 x, float M, float L) { // four neighbours of a query head's output
         const int head = p.pair / chunks, i = (p.pair % chunks) * chunk_heads + q;
         if (i >= group || e >= D) return;
@@ -576,15 +614,7 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
             if (e == 0) more.sums[(int64_t)p.b * a.heads + head * group + i] = make_float2(M, L);
         }
         if constexpr (kMode == kBehind) {
-            if (start_of(p.b) > 0) {
-                const int64_t at = (int64_t)p.b * a.heads + head * group + i;
-                const float2 ml = more.ml[at];
-                const float top = fmaxf(M, ml.x), base = top == -INFINITY ? 0.0f : top;
-                const float f = exp2_approx(M - base), f2 = exp2_approx(ml.x - base);
-                x = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
-                add_scaled(x, f2, *reinterpret_cast<const float4 *>(more.o + at * W + e));
-                L = L * f + f2 * ml.y;
-            }
+            if (start_of(p.b) > 0) join_shared((int64_t)p.b * a.heads + head * group + i, e, x, M, L);
         }
         const float inv = L == 0.0f ? 0.0f : 1.0f / L;
         *reinterpret_cast<uint2 *>(a.out + (int64_t)p.b * a.out_stride + (int64_t)(head * group + i) * D + e) =
@@ -761,9 +791,10 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
             if (start_of(b) > 0) {
                 for (int i = tid; i < a.heads * D / 4; i += kThreads) {
                     const int h = i / (D / 4), e = i % (D / 4) * 4;
-                    const int64_t at = (int64_t)b * a.heads + h;
-                    const float L = more.ml[at].y, inv = L == 0.0f ? 0.0f : 1.0f / L;
-                    const float4 x = *reinterpret_cast<const float4 *>(more.o + at * W + e);
+                    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    float M = -INFINITY, L = 0.0f;
+                    join_shared((int64_t)b * a.heads + h, e, x, M, L);
+                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
                     *reinterpret_cast<uint2 *>(a.out + (int64_t)b * a.out_stride + (int64_t)h * D + e) =
                         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
                 }

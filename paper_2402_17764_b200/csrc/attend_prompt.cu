@@ -52,6 +52,9 @@
 #include "ptx.cuh"
 #include "tma_host.cuh"
 
+#ifndef SHARED_LEAST
+#define SHARED_LEAST 2
+#endif
 namespace bitlinear {
 namespace {
 
@@ -60,6 +63,7 @@ using namespace ptx;
 constexpr int kTile = 128;               // rows of a query tile, keys of a block
 constexpr int kStep = 64;                // keys of a softmax step
 constexpr int kRows = 2 * kTile;         // rows of a CTA
+static_assert(kRows == kPromptRows, "the parts' layout");
 constexpr int kHalfBytes = kTile * 128;  // 128 rows of 64 bf16 elements, 128-byte swizzle
 constexpr int kTileBytes16 = 2 * kHalfBytes;
 constexpr int kMaxStages = 5;
@@ -72,6 +76,7 @@ constexpr uint32_t kTmemColumns = 512;
 constexpr float kRaise = 8.0f;
 constexpr float kFar = 16777216.0f; // 2^24: references up to here are rounded by at most half a unit (see the header on rounding)
 constexpr int kMaxParts = 16; // of a tile's keys
+constexpr int kMaxSharedParts = 32;
 // kv heads whose tiles follow each other: the keys and values of eight heads stay in the L2 while their tiles are worked on
 // (8192 tokens, 32 heads: 134 MB in all, 590 us with all heads at a time, 576 with eight; at 128k tokens eight heads are
 // 0.5 GB and do not stay there either, and of short prompts all heads would)
@@ -211,8 +216,14 @@ struct Work {
 // (Not inlined: the registers of the main loop are allotted without it, 584 -> 576 us for 8192 tokens, 32 heads.)
 // One row by plain arithmetic, one warp: for tiles in which a non-finite value stands behind keys that some of the rows do not
 // see (0 x NaN would reach them through the MMA), or in which a reference lies beyond kFar.
+// to: the shared form's place for the result, in fp32.
+struct RowResult {
+    float2 *ml;
+    float *o;
+    int step; // between four elements and the next
+};
 template <bool kShared>
-__device__ __noinline__ void attend_row(const AttendArgs &a, const PromptMore<kShared> &more, const Work &w, int r, int lane)
+__device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int r, int lane, int begin, int end, const RowResult &to)
 {
     const int D = a.cache.head_dim, t = w.first_token + r / w.group, h = w.head * w.group + r % w.group;
     const bool mine = 4 * lane < D;
@@ -225,9 +236,8 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const PromptMore<kS
     const float4 q = load(a.q + (int64_t)t * a.q_stride + h * D);
     float m = -INFINITY, l = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const int end = w.sees(r);
     constexpr int kAtATime = 4; // keys (a page holds 16 or more)
-    for (int j = 0; j < end; j += kAtATime) {
+    for (int j = begin; j < end; j += kAtATime) {
         const int page = kv_page(a.cache, a.batch, w.b, j);
         if (page < 0) continue;
         const int64_t row = (int64_t)kv_row(a.cache, page, w.head, j) * a.cache.width;
@@ -262,9 +272,8 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const PromptMore<kS
         m = mn;
     }
     if constexpr (kShared) {
-        const int64_t at = (int64_t)t * a.heads + h;
-        if (lane == 0) more.ml[at] = make_float2(m, l);
-        if (4 * lane < a.cache.width) *reinterpret_cast<float4 *>(more.o + at * a.cache.width + 4 * lane) = o;
+        if (lane == 0) *to.ml = make_float2(m, l);
+        if (4 * lane < a.cache.width) *reinterpret_cast<float4 *>(to.o + lane * to.step) = o;
         return;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -272,10 +281,6 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const PromptMore<kS
         *reinterpret_cast<uint2 *>(a.out + (int64_t)t * a.out_stride + h * D + 4 * lane) =
             make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
 }
-
-// Partial results of the CTAs that share a tile of rows: (reference, sum) of 256 rows, then their outputs as [four elements][row], so
-// that a row per thread writes and reads whole lines.
-__host__ __device__ constexpr size_t part_floats(int width) { return (size_t)kRows * (width + 2); }
 
 template <bool kInt8, bool kShared>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args, const __grid_constant__ PromptMore<kShared> more)
@@ -367,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             int tiles = 0; // (at most one per sequence and kv head, and what the host counted)
 #pragma unroll
             for (int w = 0; w < kThreads / 32; ++w) tiles += (int)sh.scan[w];
-            splits = min(kMaxParts, max(1, args.slots / max(tiles, 1)));
+            splits = min(kShared ? kMaxSharedParts : kMaxParts, max(1, args.slots / max(tiles, 1)));
         }
         const int64_t x = (int)blockIdx.x / splits;
         if (x >= upto - mine && x < upto) {
@@ -411,13 +416,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     // blocks of keys of the two tiles, and this CTA's part of them (a part is at least four blocks, so that joining the parts
     // does not cost more than they save)
     const int most = ((kShared ? w.len : w.sees(min(w.row0 + kRows, w.rows) - 1)) + kTile - 1) / kTile;
-    const int parts = max(1, min(splits, most / 4));
+    // (The parts of the shared form are joined by the kernel behind it, a sequence's rows at a time: two blocks are enough.)
+    const int parts = max(1, min(splits, most / (kShared ? SHARED_LEAST : 4)));
     if (split >= parts) return;
-    const int from = (int)((int64_t)most * split / parts), to = (int)((int64_t)most * (split + 1) / parts);
+    const int from = (int)((int64_t)most * split / parts), to_block = (int)((int64_t)most * (split + 1) / parts);
     int n_steps[2];
     for (int t = 0; t < 2; ++t) {
         const int first = w.row0 + t * kTile, last = min(first + kTile, w.rows) - 1;
-        n_steps[t] = first < w.rows ? max(0, min(((kShared ? w.len : w.sees(last)) + kStep - 1) / kStep, 2 * to) - 2 * from) : 0;
+        n_steps[t] = first < w.rows ? max(0, min(((kShared ? w.len : w.sees(last)) + kStep - 1) / kStep, 2 * to_block) - 2 * from) : 0;
     }
     const int total = (max(n_steps[0], n_steps[1]) + 1) / 2; // blocks
 
@@ -802,8 +808,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
 
         // ---- the result, or this CTA's part of it --------------------------------------------------------------
         float *ws_parts = reinterpret_cast<float *>(reinterpret_cast<char *>(a.workspace) + prompt_counter_bytes());
+        if constexpr (kShared) {
+            ws_parts = more.parts;
+            if (exists && split == 0)
+                more.where[(int64_t)(w.first_token + row / group) * a.heads + w.head * group + row % group] =
+                    parts > 1 ? make_int2(blockIdx.x, parts << 16 | (t * kTile + r)) : make_int2(-1, 0);
+        }
         const int first_part = blockIdx.x - split; // of this tile
-        auto part_of = [&](int p) { return ws_parts + (size_t)(first_part + p) * part_floats(W); };
+        auto part_of = [&](int p) { return ws_parts + (size_t)(first_part + p) * prompt_part_floats(W); };
         if (ok) {
             const float inv = kShared || parts > 1 ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
             __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + row / group) * a.out_stride + (w.head * group + row % group) * D;
@@ -859,7 +871,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                 }
             }
         }
-        if (parts > 1) {
+        if (!kShared && parts > 1) {
             // the CTA that finishes last joins the parts in their order and leaves the counter at zero
             uint32_t *counter = reinterpret_cast<uint32_t *>(a.workspace) + 2 * first_part;
             __threadfence();
@@ -895,8 +907,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                     }
                     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
                     __nv_bfloat16 *dst = a.out + (int64_t)(w.first_token + rr / group) * a.out_stride + (w.head * group + rr % group) * D;
-                    const int64_t at = (int64_t)(w.first_token + rr / group) * a.heads + w.head * group + rr % group; // shared form
-                    if constexpr (kShared) more.ml[at] = make_float2(M, L);
                     for (int e0 = 0; e0 < D; e0 += 16) { // (W is a multiple of 16)
                         float4 x[4];
 #pragma unroll
@@ -911,11 +921,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                                 x[u] = make_float4(x[u].x + f * v.x, x[u].y + f * v.y, x[u].z + f * v.z, x[u].w + f * v.w);
                             }
                         }
-                        if constexpr (kShared) {
-#pragma unroll
-                            for (int u = 0; u < 4; ++u) *reinterpret_cast<float4 *>(more.o + at * W + e0 + 4 * u) = x[u];
-                            continue;
-                        }
 #pragma unroll
                         for (int u = 0; u < 4; ++u)
                             if (e0 + 4 * u < D)
@@ -929,11 +934,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             named_barrier(1, kRows);
             // The next launch may start, unless rows have to be done again: that takes long when they see many keys, and the
             // waits of a matmul that were resident meanwhile would run out.
-            if (tid == 0 && !((parts == 1 || sh.is_last) && (sh.poisoned[0] || sh.poisoned[1]))) griddep_launch_dependents();
-            if (parts == 1 || sh.is_last) {
+            const bool again = kShared || parts == 1 || sh.is_last; // (the shared form's parts are each done again by their own CTA)
+            if (tid == 0 && !(again && (sh.poisoned[0] || sh.poisoned[1]))) griddep_launch_dependents();
+            if (again) {
                 if (sh.poisoned[t])
                     for (int i = warp % 4; i < kTile; i += 4)
-                        if (w.row0 + t * kTile + i < w.rows) attend_row<kShared>(a, more, w, w.row0 + t * kTile + i, lane);
+                        if (const int rr = w.row0 + t * kTile + i; rr < w.rows) {
+                            RowResult to = {};
+                            int begin = 0, end = w.sees(rr);
+                            if constexpr (kShared) {
+                                const int64_t at = (int64_t)(w.first_token + rr / group) * a.heads + w.head * group + rr % group;
+                                begin = from * kTile;
+                                end = min(end, to_block * kTile);
+                                if (parts > 1)
+                                    to = {reinterpret_cast<float2 *>(part_of(split)) + t * kTile + i, part_of(split) + 2 * kRows + 4 * (t * kTile + i), 4 * kRows};
+                                else
+                                    to = {more.ml + at, more.o + at * W, 4};
+                            }
+                            attend_row<kShared>(a, w, rr, lane, begin, end, to);
+                        }
             }
         }
     }
@@ -1006,7 +1025,7 @@ cudaError_t launch_tiles(const AttendArgs &a, const PromptMore<kShared> &more, c
     // empty slots is not split.
     const int slots = std::min(sm_count(), kPromptMaxParts);
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxParts, slots / tiles));
-    p.slots = a.batch.n_seqs > 1 && tiles < slots ? slots : 0;
+    p.slots = (kShared || a.batch.n_seqs > 1) && tiles < slots ? slots : 0;
     const int ctas = p.slots > 0 ? slots : (int)tiles * p.splits;
     return a.cache.k_scale ? launch<true, kShared>(p, more, ctas, stream) : launch<false, kShared>(p, more, ctas, stream);
 }
@@ -1017,7 +1036,7 @@ size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim)
 {
     (void)heads;
     (void)kv_heads;
-    return align_up(prompt_counter_bytes() + kPromptMaxParts * part_floats(kv_row_width(head_dim)) * 4, 256);
+    return align_up(prompt_counter_bytes() + kPromptMaxParts * prompt_part_floats(kv_row_width(head_dim)) * 4, 256);
 }
 
 cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream) { return launch_tiles<false>(a, PromptMore<false>{}, stream); }

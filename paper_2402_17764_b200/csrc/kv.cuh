@@ -149,8 +149,10 @@ struct WeighArgs {
 // What the kernels that attend to shared beginnings hand to each other.
 struct SharedArgs {
     int32_t *starts; // [n_seqs]: rows of the sequence that the shared part has dealt with
+    int2 *where;     // [n_seqs][heads]: where its results stand: (first part, parts * 2^16 + row of the tile), or (-1, 0): in ml and o
     float2 *ml;      // [n_seqs][heads]: reference and sum of the shared part of every softmax
     float *o;        // [n_seqs][heads][width]: its weighted sum of the values
+    float *parts;    // the partial results of tiles whose keys several CTAs share (see prompt_part_floats)
     const int32_t *kv_lens; // of the sequences
 };
 
@@ -171,6 +173,10 @@ cudaError_t launch_attend_decode_behind(const AttendArgs &a, const SharedArgs &s
 constexpr int kPromptMaxParts = 160;
 __host__ __device__ constexpr size_t prompt_counter_bytes() { return 256 * 2 * sizeof(uint32_t); }
 static_assert(kPromptMaxParts * 2 * sizeof(uint32_t) <= prompt_counter_bytes(), "a counter for every part");
+constexpr int kPromptRows = 256; // of a tile
+// A part: (reference, sum) of its rows, then their outputs as [four elements][row], so that a row per thread writes and reads whole
+// lines.
+__host__ __device__ constexpr size_t prompt_part_floats(int width) { return (size_t)kPromptRows * (width + 2); }
 size_t attend_prompt_workspace_bytes(int heads, int kv_heads, int head_dim);
 cudaError_t launch_attend_prompt(const AttendArgs &a, cudaStream_t stream);
 // The part of a decode step that groups of sequences share: a.batch holds the groups (their pages, how many rows they share, which

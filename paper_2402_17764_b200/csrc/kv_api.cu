@@ -282,12 +282,13 @@ namespace {
 
 // Workspace of the attention over shared beginnings: the prompt kernel's, the decode kernel's, then what the one hands to the other.
 struct SharedLayout {
-    size_t decode, starts, ml, o, bytes;
+    size_t decode, starts, where, ml, o, bytes;
     SharedLayout(int heads, int kv_heads, int head_dim, int64_t n_seqs)
     {
         decode = attend_prompt_workspace_bytes(heads, kv_heads, head_dim);
         starts = decode + attend_decode_workspace_bytes(heads, kv_heads, head_dim);
-        ml = starts + align_up((size_t)n_seqs * sizeof(int32_t), 256);
+        where = starts + align_up((size_t)n_seqs * sizeof(int32_t), 256);
+        ml = where + align_up((size_t)n_seqs * heads * sizeof(int2), 256);
         o = ml + align_up((size_t)n_seqs * heads * sizeof(float2), 256);
         bytes = o + align_up((size_t)n_seqs * heads * kv_row_width(head_dim) * sizeof(float), 256);
     }
@@ -322,7 +323,9 @@ bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache,
     a.workspace = ws + at.decode;
     SharedArgs shared;
     shared.starts = reinterpret_cast<int32_t *>(ws + at.starts);
+    shared.where = reinterpret_cast<int2 *>(ws + at.where);
     shared.ml = reinterpret_cast<float2 *>(ws + at.ml);
+    shared.parts = reinterpret_cast<float *>(ws + prompt_counter_bytes());
     shared.o = reinterpret_cast<float *>(ws + at.o);
     shared.kv_lens = a.batch.kv_lens;
     if (groups->n_seqs == 0) return launch_attend_decode(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
