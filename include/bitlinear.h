@@ -492,8 +492,8 @@ bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bit
  * The result is that of bitlinear_attend_decode, up to the rounding of the shared part's weights to bf16 (as in
  * bitlinear_attend_prompt).  `batch` is as there: its page table covers the shared rows too.
  *   groups  n_seqs groups: cu_tokens[g] .. cu_tokens[g + 1] - 1 are the SEQUENCES of group g (not NULL; sequences may belong to
- *           none), kv_lens[g] the number of rows they share, cut to whole pages, and row g of its page_table those pages.  Each
- *           sequence of the group sees them as far as its own length goes.  A group of one sequence shares nothing.  With bounds that
+ *           none), kv_lens[g] the number of rows they share, cut to whole pages, and row g of its page_table those pages.  A group
+ *           of one sequence shares nothing, nor does a sequence that is shorter than what its group shares.  With bounds that
  *           fall or lie outside 0 .. n_seqs of the batch the status is set and all is attended to sequence by sequence.
  *   workspace  >= bitlinear_attend_shared_workspace_bytes(..., n_seqs of the batch), zeroed once
  */

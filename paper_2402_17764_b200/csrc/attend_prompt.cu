@@ -92,7 +92,6 @@ struct Shared {
     uint32_t tmem_base;
     int abort_flag;
     int poisoned[2];
-    int least[2];
     int is_last;
     int found_b;
     int64_t found_local, scan[kThreads / 32];
@@ -123,20 +122,12 @@ struct PromptArgs {
 };
 
 // The shared form: the "sequences" of a.batch are groups of sequences, a group's new tokens are one token of each of its
-// sequences (token row = sequence), and all of them see the rows that the group shares, as far as their own lengths go.  References,
-// sums and outputs stay fp32 and are handed on.
+// sequences (token row = sequence), and all of them see all rows that the group shares (what comes out for a sequence that is
+// shorter is not used).  References, sums and outputs stay fp32 and are handed on.
 template <bool kShared>
 struct PromptMore {};
 template <>
 struct PromptMore<true> : SharedArgs {};
-
-// How many rows group g shares, a whole number of pages; none for a group of a single sequence (nothing is saved).
-__device__ __forceinline__ int shared_rows(const AttendArgs &a, int g, bool &over)
-{
-    const int n = max(0, a.batch.kv_lens[g]) >> a.cache.page_shift << a.cache.page_shift;
-    over = n > a.batch.capacity;
-    return a.batch.cu_tokens[g + 1] - a.batch.cu_tokens[g] < 2 ? 0 : min(n, a.batch.capacity);
-}
 
 __device__ __forceinline__ float exp2_approx(float x)
 {
@@ -204,11 +195,10 @@ struct Work {
     int len;              // keys of the sequence
     int offset;           // position of the first new token (may be negative)
     int group;
-    const int32_t *own_lens; // shared form: the lengths of the group's sequences
     // keys that row r of the sequence sees
     __device__ __forceinline__ int sees(int r) const
     {
-        const int n = own_lens ? own_lens[r / group] : offset + r / group + 1;
+        const int n = offset + r / group + 1;
         return n < 0 ? 0 : (n > len ? len : n);
     }
 };
@@ -285,6 +275,10 @@ __device__ __noinline__ void attend_row(const AttendArgs &a, const Work &w, int 
 template <bool kInt8, bool kShared>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args, const __grid_constant__ PromptMore<kShared> more)
 {
+    if (kShared && !kInt8 && threadIdx.x == 0) {
+        prefetch_tensormap(&args.k_map);
+        prefetch_tensormap(&args.v_map);
+    }
     griddep_wait(); // everything below is read from memory that the launch before this one may have written
     const AttendArgs &a = args.a;
     extern __shared__ uint8_t smem_raw[];
@@ -299,6 +293,48 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     const int D = a.cache.head_dim, W = a.cache.width, group = a.heads / a.cache.kv_heads, n_seqs = a.batch.n_seqs;
     const uint32_t limit = args.hooks.limit_us;
 
+    auto set_up = [&] {
+        if (tid == 0) {
+            for (int t = 0; t < 2; ++t) {
+                mbar_init(smem_u32(&sh.q_full[t]), 4);
+                for (int h = 0; h < 2; ++h) {
+                    mbar_init(smem_u32(&sh.s_full[t][h]), 1);
+                    mbar_init(smem_u32(&sh.p_ready[t][h]), 4);
+                }
+                mbar_init(smem_u32(&sh.o_done[t]), 1);
+                mbar_init(smem_u32(&sh.o_last[t]), 1);
+                sh.poisoned[t] = 0;
+            }
+            for (int s = 0; s < kStages; ++s) {
+                mbar_init(smem_u32(&sh.kv_full[s]), kInt8 ? kConverters : 1);
+                mbar_init(smem_u32(&sh.kv_empty[s]), 2);
+            }
+            for (int s = 0; s < kRaw; ++s) {
+                mbar_init(smem_u32(&sh.raw_full[s]), 1);
+                mbar_init(smem_u32(&sh.raw_empty[s]), kConverters);
+            }
+            sh.abort_flag = 0;
+            fence_mbar_init();
+        }
+        if (warp == kMmaWarp) {
+            tmem_alloc(smem_u32(&sh.tmem_base), kTmemColumns);
+            tmem_relinquish();
+        }
+    };
+    // The shared form: what is set up does not wait for the search for the rows, and a CTA that finds none gives it back.
+    auto leave = [&] {
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+        if (warp == kMmaWarp) tmem_dealloc(sh.tmem_base, kTmemColumns);
+    };
+    bool none = false; // (nothing is shared)
+    auto write_starts = [&] {
+        if constexpr (kShared)
+            for (int b = blockIdx.x * kThreads + tid; b < a.T; b += gridDim.x * kThreads) more.starts[b] = none ? 0 : shared_start(a.cache, a.batch, more.seqs, b);
+    };
+    if (kShared) set_up();
+
     // ---- which rows: tiles are counted sequence by sequence, the longest first, and within a sequence, for every group of kv
     // heads, the last rows (which see most) first, so that the CTAs that start last have the least to do (four chunks of 86
     // to 512 tokens behind 3300 to 12000: 459 -> 383 us) ----
@@ -308,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             const int64_t n = (int64_t)a.batch.cu_tokens[b + 1] - a.batch.cu_tokens[b];
             if constexpr (kShared) {
                 bool over;
-                if (shared_rows(a, b, over) == 0) return 0;
+                if (group_shares(a.cache, a.batch, b, over) == 0) return 0;
             }
             return n <= 0 || n > a.T ? 0 : (n * group + kRows - 1) / kRows * a.cache.kv_heads;
         };
@@ -320,25 +356,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         int64_t mine = 0;
         if constexpr (kShared) { // with bounds that fall, or lie outside the batch, nothing is shared at all
             bool bad = false;
-            for (int b = b0; b < b1; ++b) bad = bad || rows_missing(b);
-            const bool none = __syncthreads_or(bad);
-            for (int b = blockIdx.x * kThreads + tid; b < a.T; b += gridDim.x * kThreads) {
-                int first, count;
-                bool over;
-                const int g = none ? -1 : kv_sequence_of(a.batch, b, first, count);
-                more.starts[b] = g < 0 ? 0 : shared_rows(a, g, over);
+            for (int b = b0; b < b1; ++b) {
+                bad = bad || group_bounds_bad(a.batch, b, a.T);
+                mine += tiles_of(b);
             }
+            none = __syncthreads_or(bad);
             if (none) {
                 if (blockIdx.x == 0 && tid == 0) kv_report(a.cache);
+                write_starts();
+                leave();
                 return;
             }
-        }
-        for (int b = b0; b < b1; ++b) {
-            mine += tiles_of(b);
-            if (blockIdx.x == 0 && rows_missing(b)) kv_report(a.cache);
+        } else {
+            for (int b = b0; b < b1; ++b) {
+                mine += tiles_of(b);
+                if (blockIdx.x == 0 && rows_missing(b)) kv_report(a.cache);
+            }
         }
         int first_b = b0;
-        if (per_thread == 1) { // (longer lists of sequences are taken as they are)
+        if (!kShared && per_thread == 1) { // (longer lists of sequences are taken as they are)
             int64_t *tiles_by_rank = reinterpret_cast<int64_t *>(smem);
             int *lens = reinterpret_cast<int *>(tiles_by_rank + kThreads), *b_by_rank = lens + kThreads;
             const int len = mine > 0 ? a.batch.kv_lens[b0] : 0;
@@ -389,14 +425,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         }
         __syncthreads();
     }
-    if (sh.found_b < 0) return;
+    if (sh.found_b < 0) {
+        if (kShared) {
+            write_starts();
+            leave();
+        }
+        return;
+    }
     const int split = blockIdx.x % splits;
     Work w;
     w.b = sh.found_b;
     w.group = group;
     w.first_token = a.batch.cu_tokens[w.b];
     const int n_tokens = a.batch.cu_tokens[w.b + 1] - w.first_token;
-    if (w.first_token < 0 || (int64_t)w.first_token + n_tokens > a.T) return; // (reported above)
+    if (!kShared && (w.first_token < 0 || (int64_t)w.first_token + n_tokens > a.T)) return; // (reported above)
     w.rows = n_tokens * group;
     {
         const int tiles = (w.rows + kRows - 1) / kRows;
@@ -407,53 +449,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         w.row0 = (tiles - 1 - rest / heads_here) * kRows;
     }
     bool over;
-    w.len = kShared ? shared_rows(a, w.b, over) : kv_length(a.batch, w.b, over);
+    w.len = kShared ? group_shares(a.cache, a.batch, w.b, over) : kv_length(a.batch, w.b, over);
     if (over && tid == 0) kv_report(a.cache);
-    w.offset = a.batch.kv_lens[w.b] - n_tokens;
-    w.own_lens = nullptr;
-    if constexpr (kShared) w.own_lens = more.kv_lens + w.first_token;
+    w.offset = kShared ? w.len : a.batch.kv_lens[w.b] - n_tokens; // (shared form: every row sees all keys)
 
     // blocks of keys of the two tiles, and this CTA's part of them (a part is at least four blocks, so that joining the parts
     // does not cost more than they save)
-    const int most = ((kShared ? w.len : w.sees(min(w.row0 + kRows, w.rows) - 1)) + kTile - 1) / kTile;
+    const int most = (w.sees(min(w.row0 + kRows, w.rows) - 1) + kTile - 1) / kTile;
     // (The parts of the shared form are joined by the kernel behind it, a sequence's rows at a time: two blocks are enough.)
     const int parts = max(1, min(splits, most / (kShared ? SHARED_LEAST : 4)));
-    if (split >= parts) return;
-    const int from = (int)((int64_t)most * split / parts), to_block = (int)((int64_t)most * (split + 1) / parts);
+    if (split >= parts) {
+        if (kShared) {
+            write_starts();
+            leave();
+        }
+        return;
+    }
+    using Product = std::conditional_t<kShared, int, int64_t>; // (blocks are below 2^23, the shared form's parts at most 32)
+    const int from = (int)((Product)most * split / parts), to_block = (int)((Product)most * (split + 1) / parts);
     int n_steps[2];
     for (int t = 0; t < 2; ++t) {
         const int first = w.row0 + t * kTile, last = min(first + kTile, w.rows) - 1;
-        n_steps[t] = first < w.rows ? max(0, min(((kShared ? w.len : w.sees(last)) + kStep - 1) / kStep, 2 * to_block) - 2 * from) : 0;
+        n_steps[t] = first < w.rows ? max(0, min((w.sees(last) + kStep - 1) / kStep, 2 * to_block) - 2 * from) : 0;
     }
     const int total = (max(n_steps[0], n_steps[1]) + 1) / 2; // blocks
 
-    if (tid == 0) {
-        for (int t = 0; t < 2; ++t) {
-            mbar_init(smem_u32(&sh.q_full[t]), 4);
-            for (int h = 0; h < 2; ++h) {
-                mbar_init(smem_u32(&sh.s_full[t][h]), 1);
-                mbar_init(smem_u32(&sh.p_ready[t][h]), 4);
-            }
-            mbar_init(smem_u32(&sh.o_done[t]), 1);
-            mbar_init(smem_u32(&sh.o_last[t]), 1);
-            sh.poisoned[t] = 0;
-            sh.least[t] = w.len;
-        }
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(smem_u32(&sh.kv_full[s]), kInt8 ? kConverters : 1);
-            mbar_init(smem_u32(&sh.kv_empty[s]), 2);
-        }
-        for (int s = 0; s < kRaw; ++s) {
-            mbar_init(smem_u32(&sh.raw_full[s]), 1);
-            mbar_init(smem_u32(&sh.raw_empty[s]), kConverters);
-        }
-        sh.abort_flag = 0;
-        fence_mbar_init();
-    }
-    if (warp == kMmaWarp) {
-        tmem_alloc(smem_u32(&sh.tmem_base), kTmemColumns);
-        tmem_relinquish();
-    }
+    if (!kShared) set_up();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -637,15 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             if (lane == 0) mbar_arrive(smem_u32(&sh.q_full[t]));
         }
         const int sees = exists ? w.sees(row) : 0x7FFFFFFF; // (rows that do not exist: nothing to hide from them)
-        int least; // of the tile's rows
-        if constexpr (kShared) {
-            const int of_warp = __reduce_min_sync(0xFFFFFFFFu, sees);
-            if (lane == 0) atomicMin(&sh.least[t], of_warp);
-            named_barrier(2 + t, kTile);
-            least = sh.least[t];
-        } else {
-            least = w.sees(w.row0 + t * kTile);
-        }
+        const int least = w.sees(w.row0 + t * kTile);       // of the tile's rows
         float m = -INFINITY, l = 0.0f;                      // reference and sum of this row
         bool far = false;                                   // a reference beyond kFar (int8: of any row of the warp, at present)
         bool ok = true;
@@ -956,6 +969,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
             }
         }
     }
+
+    write_starts();
 
     // every thread arrives here, also after an expired wait
     tc_fence_before_sync();

@@ -146,6 +146,29 @@ struct WeighArgs {
     KvMarks marks;
 };
 
+// Groups of sequences that begin with the same rows, as a batch: pages, rows shared, and the bounds of each group's sequences.  With
+// bounds that fall or lie outside the batch nothing is shared.  (Of one group: whether they do.)
+__device__ __forceinline__ bool group_bounds_bad(const KvBatch &groups, int g, int n_seqs)
+{
+    return groups.cu_tokens[g] < 0 || groups.cu_tokens[g] > groups.cu_tokens[g + 1] || groups.cu_tokens[g + 1] > n_seqs;
+}
+// How many rows group g shares, a whole number of pages; none for a group of a single sequence (nothing is saved).
+__device__ __forceinline__ int group_shares(const KvCache &c, const KvBatch &groups, int g, bool &over)
+{
+    const int n = max(0, groups.kv_lens[g]) >> c.page_shift << c.page_shift;
+    over = n > groups.capacity;
+    return groups.cu_tokens[g + 1] - groups.cu_tokens[g] < 2 ? 0 : min(n, groups.capacity);
+}
+// The rows of sequence b that are its group's; none for a sequence that is shorter than them.
+__device__ __forceinline__ int shared_start(const KvCache &c, const KvBatch &groups, const KvBatch &s, int b)
+{
+    int first, count;
+    bool over;
+    const int g = kv_sequence_of(groups, b, first, count);
+    const int n = g < 0 ? 0 : group_shares(c, groups, g, over);
+    return kv_length(s, b, over) >= n ? n : 0;
+}
+
 // What the kernels that attend to shared beginnings hand to each other.
 struct SharedArgs {
     int32_t *starts; // [n_seqs]: rows of the sequence that the shared part has dealt with
@@ -153,7 +176,7 @@ struct SharedArgs {
     float2 *ml;      // [n_seqs][heads]: reference and sum of the shared part of every softmax
     float *o;        // [n_seqs][heads][width]: its weighted sum of the values
     float *parts;    // the partial results of tiles whose keys several CTAs share (see prompt_part_floats)
-    const int32_t *kv_lens; // of the sequences
+    KvBatch seqs;
 };
 
 // Workspace of the decode kernel: a counter per CTA, then the partial results.  The grid has at most kDecodeMaxCtas CTAs.

@@ -327,7 +327,7 @@ bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache,
     shared.ml = reinterpret_cast<float2 *>(ws + at.ml);
     shared.parts = reinterpret_cast<float *>(ws + prompt_counter_bytes());
     shared.o = reinterpret_cast<float *>(ws + at.o);
-    shared.kv_lens = a.batch.kv_lens;
+    shared.seqs = a.batch;
     if (groups->n_seqs == 0) return launch_attend_decode(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
     if (launch_attend_prefix(p, shared, (cudaStream_t)stream) != cudaSuccess) return BITLINEAR_ERR_CUDA;
     return launch_attend_decode_behind(a, shared, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;

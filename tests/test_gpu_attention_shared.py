@@ -46,6 +46,10 @@ CASES = [
     (6, 2, 20, 32, [(100, [100, 101, 102]), (5, [9, 9])], [3]),
     (5, 1, 112, 16, [(10000, [10000, 10001, 16, 0])], []),
     (64, 8, 128, 64, [(8192, [8193 + 7 * i for i in range(20)])], []),
+    (4, 4, 128, 16, [(160, [170, 160, 161, 159] * 30), (64, [64] * 3)], [2]),
+    (32, 2, 64, 32, [(96, [97, 200, 96]), (320, [330, 319])], []),
+    (6, 6, 100, 16, [(640, [700] * 16 + [641])], []),
+    (20, 4, 128, 64, [(1280, [1300, 1290, 1281, 1280, 2000, 1, 0])] * 2, []),
 ]
 
 
@@ -192,10 +196,10 @@ def test_on_a_side_stream_and_in_a_graph():
 
 @pytest.mark.parametrize("bits", [16, 8])
 def test_an_expired_wait_is_reported(bits):
-    s, of = shared([(256, [300, 290])], 1, 64, 16, bits, 15)
-    q = rows(2, 2, 64, 16)
+    s, of = shared([(256, [300, 290] * 20)], 1, 64, 16, bits, 15)
+    q = rows(40, 8, 64, 16)
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
-    ws = B.alloc_attend_shared_workspace(2, 1, 64, 2)
+    ws = B.alloc_attend_shared_workspace(8, 1, 64, 40)
     want = B.attend_decode_shared(cache, batch, of, q, workspace=ws)
     cache.check()
     B.test_expire_next_wait(2000, True)
@@ -205,3 +209,18 @@ def test_an_expired_wait_is_reported(bits):
     assert e.value.status == B.ERR_TIMEOUT
     assert torch.equal(B.attend_decode_shared(cache, batch, of, q, workspace=ws), want)
     cache.check()
+
+
+def test_a_workspace_serves_calls_of_different_sizes():
+    """Calls of more and fewer sequences, share one workspace."""
+    ws = B.alloc_attend_shared_workspace(16, 2, 64, 60)
+    cases = []
+    for n, groups in ((60, [(64, [70 + i for i in range(60)])]), (3, [(64, [100, 64, 90])]), (20, [(48, [50, 49, 60, 70])] * 5)):
+        s, of = shared(groups, 2, 64, 16, 16, 30 + n)
+        q = rows(n, 16, 64, n)
+        cases.append((s, of, q, *R.attend(s, q, [1] * n, **error_of(16))))
+    for _ in range(3):
+        for s, of, q, want, bound in cases:
+            cache = s.cache()
+            check(B.attend_decode_shared(cache, B.KVBatch(s.table, s.kv_lens), of, q, workspace=ws), want, bound)
+            cache.check()
