@@ -14,10 +14,15 @@
 // low bytes of the sums (conversions go through a unit a quarter as wide: 2436 tokens, 40/40 heads: 52 -> 46 us with it).
 //
 // What bounds it: memory (every byte read and written once) for prompts, the launch and one chain of dependent loads
-// (length, page number, row) for a decode step.  Measured: 4096 tokens, 64/8 heads of 128: 32.2 us = 5.3 TB/s (0.80 of a copy's
+// (length, page number, row) for a decode step.  Measured (without the norm): 4096 tokens, 64/8 heads of 128: 32.2 us = 5.3 TB/s (0.80 of a copy's
 // rate); heads of 100, 32/32 of them: 57 us = 2.8 TB/s, held by the 4-byte accesses; single tokens 8.4 us per call, the time the
 // host needs for one; int8, 2436 tokens, 40/40 heads: 46 us = 2.8 TB/s: issue slots 66 % busy (row maxima, quotients and the test
 // that settles each code), not at a limit.  Registers: nothing is spilled but 4 bytes in the rotating int8 form of 4-byte pieces.
+//
+// The form that normalises: y = x g r, r = 1 / sqrt(max(mean x^2 + eps, 2^-126)), the squares summed in fp32 over a group's lanes (four
+// heads of a warp at a time where a head takes all lanes: one root for each, and half the shuffles).  4096 tokens, 64/8 heads of 128:
+// 36.7 us = 4.6 TB/s (0.71 of a copy's rate), 27 million instructions where the form without has 17; heads of 100, 32/32 of them: 87
+// us; int8, 2436 tokens, 40/40 heads: 65 us; single tokens as without it, within 1 us.
 #include <math.h>
 
 #include <algorithm>
@@ -76,6 +81,23 @@ __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const float (&x)[V
     *reinterpret_cast<Piece<VEC> *>(p) = w;
 }
 
+// Two products, or two products and sums, at a time.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
 // The largest magnitude of three, or NaN if one of them is.
 __device__ __forceinline__ float largest(float x, float y, float z)
 {
@@ -125,7 +147,11 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
     const int o0 = kRotate == 2 ? lane * 2 * VEC : lane * VEC;
     const int o1 = kRotate == 2 ? o0 + VEC : half + lane * VEC;
     float2 cs[VEC] = {};
-    if (kRotate != 0 && mine) {
+    // Whether gains and angles are multiplied with each other once: for the few elements of a lane with 4-byte pieces (4096 tokens, 32/32
+    // heads of 100: 109 -> 87 us).  16-byte pieces would hold twice the registers for it, or load the factors as often (64/8 heads of
+    // 128: 36.7 us with gains loaded for every head and four CTAs, 43 with products held and three).
+    constexpr bool kFold = kNorm && VEC == 2 && !kInt8;
+    if (!kFold && kRotate != 0 && mine) {
         const float4 *p = reinterpret_cast<const float4 *>(a.rope + (int64_t)angle_pos * half + lane * VEC);
 #pragma unroll
         for (int i = 0; i < VEC / 2; ++i) {
@@ -152,7 +178,79 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
             next1[u] = *reinterpret_cast<const Piece<VEC> *>(src + o1);
         }
     };
-    auto serve = [&](const int task, const Piece<VEC> &now0, const Piece<VEC> &now1) {
+    // Normalised forms: an element becomes own_factor times itself and other_factor times its partner in the rotation, which are
+    // products of the gain and the angle's cosine and sine, as pairs of neighbours.  They are those of queries or of keys.
+    int held = 0;
+    float2 own_factor[kFold ? VEC : 1], other_factor[kFold && kRotate != 0 ? VEC : 1];
+    auto make_factors = [&](const float *gain) {
+        if constexpr (kFold) {
+            auto gain_at = [&](int e) { return gain ? *reinterpret_cast<const float2 *>(gain + e) : make_float2(1.0f, 1.0f); };
+            const float2 *angles = a.rope + (int64_t)angle_pos * half;
+#pragma unroll
+            for (int p = 0; p < VEC; ++p) {
+                const int e = p < VEC / 2 ? o0 + 2 * p : o1 + 2 * p - VEC; // and its neighbour
+                const float2 g = gain_at(e);
+                if constexpr (kRotate == 0) {
+                    own_factor[p] = g;
+                } else if constexpr (kRotate == 1) {
+                    const int i = lane * VEC + (p < VEC / 2 ? 2 * p : 2 * p - VEC);
+                    const float4 w = *reinterpret_cast<const float4 *>(angles + i); // (c, s) of the two
+                    const float2 of = gain_at(p < VEC / 2 ? o1 + 2 * p : o0 + 2 * p - VEC);
+                    own_factor[p] = make_float2(g.x * w.x, g.y * w.z);
+                    other_factor[p] = p < VEC / 2 ? make_float2(-of.x * w.y, -of.y * w.w) : make_float2(of.x * w.y, of.y * w.w);
+                } else {
+                    const float2 w = angles[e / 2];
+                    own_factor[p] = make_float2(g.x * w.x, g.y * w.x);
+                    other_factor[p] = make_float2(-g.y * w.y, g.x * w.y);
+                }
+            }
+        }
+    };
+    // 1 / rms of the heads that the warp has at hand.
+    auto over_rms_of = [&](const Piece<VEC> (&now0)[kBatch], const Piece<VEC> (&now1)[kBatch], float (&r)[kBatch]) {
+        auto squares_of = [&](float unit) { // of one of the heads per lane: kLanes / kBatch neighbours have the same
+            float s[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                float x0[VEC], x1[VEC];
+                unpack<VEC>(now0[u], x0);
+                unpack<VEC>(now1[u], x1);
+                float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                const float2 unit2 = make_float2(unit, unit);
+#pragma unroll
+                for (int i = 0; i < VEC; i += 2) {
+                    float2 y = make_float2(x0[i], x0[i + 1]), z = make_float2(x1[i], x1[i + 1]);
+                    if (unit != 1.0f) y = mul2(y, unit2), z = mul2(z, unit2);
+                    sum[0] = fma2(y, y, sum[0]);
+                    sum[1] = fma2(z, z, sum[1]);
+                }
+                s[u] = mine ? (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y) : 0.0f;
+            }
+            if constexpr (kBatch == 4) { // each half, then each quarter of the warp keeps the heads that become its own
+                const bool upper = lane & 16, odd = lane & 8;
+                const float y = (upper ? s[2] : s[0]) + __shfl_xor_sync(0xFFFFFFFFu, upper ? s[0] : s[2], 16);
+                const float z = (upper ? s[3] : s[1]) + __shfl_xor_sync(0xFFFFFFFFu, upper ? s[1] : s[3], 16);
+                s[0] = (odd ? z : y) + __shfl_xor_sync(0xFFFFFFFFu, odd ? y : z, 8);
+            }
+#pragma unroll
+            for (int d = kLanes / kBatch / 2; d > 0; d >>= 1) s[0] += __shfl_xor_sync(0xFFFFFFFFu, s[0], d);
+            return s[0];
+        };
+        // (Squares below fp32's range do not matter beside the least mean, 2^-126.  Squares above it: again, in a smaller unit.)
+        float squares = squares_of(1.0f), unit = 1.0f;
+        if (__any_sync(0xFFFFFFFFu, !(squares <= 3e38f))) {
+            const float small = squares_of(0x1p-80f);
+            if (!(squares <= 3e38f)) {
+                squares = small;
+                unit = 0x1p-80f;
+            }
+        }
+        const float mean = squares / (float)D + a.norm_eps * unit * unit;
+        const float own = rsqrtf(mean < 0x1p-126f ? 0x1p-126f : mean) * unit; // (a NaN stays one)
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) r[u] = kBatch > 1 ? __shfl_sync(0xFFFFFFFFu, own, u * (32 / kBatch)) : own;
+    };
+    auto serve = [&](const int task, const Piece<VEC> &now0, const Piece<VEC> &now1, const float over_rms) {
         const bool is_q = task < a.heads, is_k = !is_q && task < a.heads + Hk;
         const int h = is_q ? task : (is_k ? task - a.heads : task - a.heads - Hk);
         const bool work = works(task);
@@ -165,51 +263,59 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
         // the j-th pair of this lane: (x0[j], x1[j]), or two neighbours
         auto first_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j] : x1[2 * j - VEC]) : x0[j]; };
         auto second_of = [&](int j) -> float & { return kRotate == 2 ? (j < VEC / 2 ? x0[2 * j + 1] : x1[2 * j + 1 - VEC]) : x1[j]; };
-        // The norm.  An 8-bit row's factor 1 / rms cancels out of its codes, so its key is only multiplied by the gain here.
-        const float *gain = nullptr;
-        float over_rms = 1.0f;
-        if (kNorm && (a.q_gain || a.k_gain)) {
-            gain = is_q ? a.q_gain : (is_k ? a.k_gain : nullptr);
-            const bool normed = gain != nullptr && task < tasks;
-            float squares = 0.0f;
+        const float *gain = !kNorm ? nullptr : (is_q ? a.q_gain : (is_k ? a.k_gain : nullptr));
+        const bool rotate = kRotate != 0 && (is_q || is_k);
+        if (kFold) {
+            if (work && (is_q || is_k)) {
+                const int kind = is_q ? 1 : 2;
+                if (kind != held) {
+                    held = kind;
+                    make_factors(gain);
+                }
+                const float r = gain ? over_rms : 1.0f;
+                float2 x[VEC];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) squares = fmaf(x1[i], x1[i], fmaf(x0[i], x0[i], squares));
+                for (int p = 0; p < VEC; ++p)
+                    x[p] = mul2(p < VEC / 2 ? make_float2(x0[2 * p], x0[2 * p + 1]) : make_float2(x1[2 * p - VEC], x1[2 * p + 1 - VEC]), make_float2(r, r));
 #pragma unroll
-            for (int d = 1; d < kLanes; d <<= 1) squares += __shfl_xor_sync(0xFFFFFFFFu, squares, d);
-            float mean = squares / (float)D + a.norm_eps;
-            // squares near the ends of fp32's range (or of a row that is not finite, or all zero): again in double
-            if (__any_sync(0xFFFFFFFFu, normed && !(squares >= 1e-30f && squares <= 1e37f))) {
-                double wide = 0.0;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) wide += (double)x0[i] * x0[i] + (double)x1[i] * x1[i];
-#pragma unroll
-                for (int d = 1; d < kLanes; d <<= 1) wide += __shfl_xor_sync(0xFFFFFFFFu, wide, d);
-                wide = wide / D + (double)a.norm_eps;
-                if (!(squares >= 1e-30f && squares <= 1e37f)) {
-                    mean = 1.0f;
-                    over_rms = (float)(1.0 / sqrt(wide < 0x1p-126 ? 0x1p-126 : wide)); // (a NaN stays one)
+                for (int p = 0; p < VEC; ++p) {
+                    // (the partner's product is rounded first, as the form without a norm does it)
+                    const float2 y = kRotate == 0 ? mul2(x[p], own_factor[p])
+                                                  : fma2(x[p], own_factor[p],
+                                                         mul2(kRotate == 1 ? x[p < VEC / 2 ? p + VEC / 2 : p - VEC / 2] : make_float2(x[p].y, x[p].x), other_factor[p]));
+                    (p < VEC / 2 ? x0[2 * p] : x1[2 * p - VEC]) = y.x;
+                    (p < VEC / 2 ? x0[2 * p + 1] : x1[2 * p + 1 - VEC]) = y.y;
                 }
             }
-            if (squares >= 1e-30f && squares <= 1e37f) over_rms = 1.0f / sqrtf(mean < 0x1p-126f ? 0x1p-126f : mean);
-            if (normed && work) {
+        } else {
+            if (kNorm && gain && work) {
+                // (An 8-bit row's factor 1 / rms cancels out of its codes: it enters the scale alone.)
                 const float f = kInt8 && !is_q ? 1.0f : over_rms;
 #pragma unroll
                 for (int i = 0; i < VEC; i += 2) {
                     const float2 g0 = *reinterpret_cast<const float2 *>(gain + o0 + i), g1 = *reinterpret_cast<const float2 *>(gain + o1 + i);
-                    x0[i] = x0[i] * f * g0.x;
-                    x0[i + 1] = x0[i + 1] * f * g0.y;
-                    x1[i] = x1[i] * f * g1.x;
-                    x1[i + 1] = x1[i + 1] * f * g1.y;
+                    const float2 y = mul2(mul2(make_float2(x0[i], x0[i + 1]), make_float2(f, f)), g0);
+                    const float2 z = mul2(mul2(make_float2(x1[i], x1[i + 1]), make_float2(f, f)), g1);
+                    x0[i] = y.x, x0[i + 1] = y.y;
+                    x1[i] = z.x, x1[i + 1] = z.y;
                 }
             }
-        }
-        const bool rotate = kRotate != 0 && (is_q || is_k);
-        if (rotate) {
+            if (kNorm && kRotate == 1 && rotate) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float p = first_of(j), r = second_of(j);
-                first_of(j) = p * cs[j].x - r * cs[j].y;
-                second_of(j) = r * cs[j].x + p * cs[j].y;
+                for (int j = 0; j < VEC; j += 2) {
+                    const float2 y = make_float2(x0[j], x0[j + 1]), z = make_float2(x1[j], x1[j + 1]);
+                    const float2 c = make_float2(cs[j].x, cs[j + 1].x), n = make_float2(cs[j].y, cs[j + 1].y);
+                    const float2 u = mul2(z, n), lo = fma2(y, c, make_float2(-u.x, -u.y)), hi = fma2(z, c, mul2(y, n));
+                    x0[j] = lo.x, x0[j + 1] = lo.y;
+                    x1[j] = hi.x, x1[j + 1] = hi.y;
+                }
+            } else if (rotate) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float p = first_of(j), r = second_of(j);
+                    first_of(j) = p * cs[j].x - r * cs[j].y;
+                    second_of(j) = r * cs[j].x + p * cs[j].y;
+                }
             }
         }
         const int64_t row = is_q || page < 0 ? 0 : kv_row(a.cache, page, h, pos);
@@ -355,8 +461,12 @@ __global__ void __launch_bounds__(256, kInt8 && VEC == 8 ? 3 : 4) kv_append_kern
             now1[u] = next1[u];
         }
         prefetch(round + step + group);
+        float factor[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) serve(round + u * kGroups + group, now0[u], now1[u]);
+        for (int u = 0; u < kBatch; ++u) factor[u] = 1.0f;
+        if (kNorm && (a.q_gain || a.k_gain)) over_rms_of(now0, now1, factor);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) serve(round + u * kGroups + group, now0[u], now1[u], factor[u]);
     }
 }
 
