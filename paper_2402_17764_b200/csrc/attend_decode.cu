@@ -73,6 +73,18 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// The same for what is to leave the L2 first.
+__device__ __forceinline__ uint64_t leave_first()
+{
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
+}
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, bool real, uint64_t policy)
+{
+    const int n = real ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(n), "l"(policy) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -290,6 +302,14 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
         }
         return page;
     };
+    // (kWeigh: the keys and values make room in the L2 for the scores, which the launch behind this one reads)
+    const uint64_t policy = kMode == kWeigh ? leave_first() : 0;
+    auto copy = [&](uint32_t dst, const void *src, bool real) {
+        if (kMode == kWeigh)
+            cp_async_16(dst, src, real, policy);
+        else
+            cp_async_16(dst, src, real);
+    };
     auto fetch = [&](const Place &p, int pages, int stage) {
         const uint32_t at = ring_addr + stage * S::kStage;
         const int key0 = p.blk * kBlock + warp * kKeys;
@@ -314,8 +334,13 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
 #pragma unroll
                 for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
                     const uint32_t dst = at + piece<kRB>(q * 16 + i * kRowsAtOnce + r0, c);
-                    cp_async_16(dst, kp + i * 512);
-                    cp_async_16(dst + kStageBytes / 2, vp + i * 512);
+                    if (kMode == kWeigh) {
+                        copy(dst, kp + i * 512, true);
+                        copy(dst + kStageBytes / 2, vp + i * 512, true);
+                    } else {
+                        cp_async_16(dst, kp + i * 512);
+                        cp_async_16(dst + kStageBytes / 2, vp + i * 512);
+                    }
                 }
             } else {
                 const int64_t offset = row * W * kElement;
@@ -327,8 +352,8 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
                     const bool real = have && real_c && q * 16 + r < n;
                     const int skip = real ? r * W * kElement + c * 16 : 0; // (an address that exists in any case)
                     const uint32_t dst = at + piece<kRB>(q * 16 + r, c);
-                    cp_async_16(dst, kp + skip, real);
-                    cp_async_16(dst + kStageBytes / 2, vp + skip, real);
+                    copy(dst, kp + skip, real);
+                    copy(dst + kStageBytes / 2, vp + skip, real);
                 }
             }
             if (kInt8 && lane < 8) { // 4 pieces of 4 scales for the keys, 4 for the values
@@ -477,9 +502,15 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int column = t * 8 + 2 * tq + c % 2;
-                            if (column < chunk_heads) to[(q * 16 + c / 2 * 8 + g) * chunk_heads + column] = s[q][t][c];
+                        for (int h = 0; h < 2; ++h) {
+                            const int column = t * 8 + 2 * tq;
+                            float *at = to + (q * 16 + h * 8 + g) * chunk_heads + column;
+                            if (chunk_heads % 2 == 0) {
+                                if (column < chunk_heads) *reinterpret_cast<float2 *>(at) = make_float2(s[q][t][2 * h], s[q][t][2 * h + 1]);
+                            } else {
+                                if (column < chunk_heads) at[0] = s[q][t][2 * h];
+                                if (column + 1 < chunk_heads) at[1] = s[q][t][2 * h + 1];
+                            }
                         }
             }
         }
@@ -815,8 +846,8 @@ template <int kBlock>
 __global__ void __launch_bounds__(kWeighWarps * 32, kWeighCtas)
 add_weights_kernel(const __grid_constant__ AttendArgs a, const int chunks, const int chunk_heads, const __grid_constant__ WeighArgs more)
 {
-    griddep_wait();
-    griddep_launch_dependents();
+    // (What is looked at before the wait, lengths and pages, the launch before this one has only read, and its CTAs let this one in
+    // when what came before them was complete.)
     constexpr int kThreads = kWeighWarps * 32;
     __shared__ int upto_of[kThreads];
     __shared__ int scan[kWeighWarps];
@@ -869,6 +900,8 @@ add_weights_kernel(const __grid_constant__ AttendArgs a, const int chunks, const
         rest -= units;
     }
     int pair = rest / (nblk + kPairCost), blk = rest - pair * (nblk + kPairCost);
+    griddep_wait();
+    griddep_launch_dependents();
     while (unit < end) {
         const int chunk = pair % chunks, head = pair / chunks;
         if (chunk != 0 || blk >= nblk) { // (the other chunks are added to the first one's keys; the end of a pair)
@@ -888,11 +921,24 @@ add_weights_kernel(const __grid_constant__ AttendArgs a, const int chunks, const
                 if (lane < heads_here) ml = more.sums[(int64_t)b * a.heads + head * group + c * chunk_heads + lane];
                 const float m = ml.x == -INFINITY ? 0.0f : ml.x, inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
                 const float *from = more.scores + (int64_t)u * kBlock * chunk_heads;
-                for (int q = 0; q < heads_here; ++q) {
+                auto add = [&](int q, int i, float s) {
                     const float mq = __shfl_sync(0xFFFFFFFFu, m, q), iq = __shfl_sync(0xFFFFFFFFu, inv, q);
+                    sum[i] += exp2_approx(s - mq) * iq;
+                };
+                if (chunk_heads % 4 == 0 && heads_here == chunk_heads) {
+                    for (int q = 0; q < heads_here; q += 4)
 #pragma unroll
-                    for (int i = 0; i < kBlock / 32; ++i)
-                        if (blk * kBlock + i * 32 + lane < len) sum[i] += exp2_approx(from[(i * 32 + lane) * chunk_heads + q] - mq) * iq;
+                        for (int i = 0; i < kBlock / 32; ++i) { // (what stands behind the last key goes into sums that nobody stores)
+                            const float4 s = *reinterpret_cast<const float4 *>(from + (i * 32 + lane) * chunk_heads + q);
+                            add(q, i, s.x);
+                            add(q + 1, i, s.y);
+                            add(q + 2, i, s.z);
+                            add(q + 3, i, s.w);
+                        }
+                } else {
+                    for (int q = 0; q < heads_here; ++q)
+#pragma unroll
+                        for (int i = 0; i < kBlock / 32; ++i) add(q, i, from[(i * 32 + lane) * chunk_heads + q]);
                 }
             }
             if (!room && lane == 0) kv_report(a.cache);
