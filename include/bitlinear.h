@@ -495,13 +495,17 @@ bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bit
  *           none), kv_lens[g] the number of rows they share, cut to whole pages, and row g of its page_table those pages.  A group
  *           of one sequence shares nothing, nor does a sequence that is shorter than what its group shares.  With bounds that
  *           fall or lie outside 0 .. n_seqs of the batch the status is set and all is attended to sequence by sequence.
+ *   share_from  sharing has a cost of its own: rows are shared when the sequences of all groups would read at least this many elements
+ *           of keys without it (sequences of the group * rows shared * kv_heads * head_dim, over the groups).  < 0: the library's
+ *           measured bound, 40 * 2^20;  0: always.  (Where not even lengths that fill the groups' page table would reach it the
+ *           groups are not looked at.)
  *   workspace  >= bitlinear_attend_shared_workspace_bytes(..., n_seqs of the batch), zeroed once
  */
 size_t bitlinear_attend_shared_workspace_bytes(int heads, int kv_heads, int head_dim, int64_t n_seqs);
 bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,
                                                 const bitlinear_kv_batch *groups, const void *q, int64_t q_stride, int heads,
-                                                float softmax_scale, void *out, int64_t out_stride, void *workspace,
-                                                size_t workspace_bytes, void *stream);
+                                                float softmax_scale, int64_t share_from, void *out, int64_t out_stride,
+                                                void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Test hooks.

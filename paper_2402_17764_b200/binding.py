@@ -189,7 +189,7 @@ def load_library() -> ctypes.CDLL:
     L.bitlinear_kv_compact.argtypes = [vp, vp, vp, i64, vp, vp]
     L.bitlinear_attend_shared_workspace_bytes.argtypes = [ci, ci, ci, i64]
     L.bitlinear_attend_shared_workspace_bytes.restype = sz
-    L.bitlinear_attend_decode_shared.argtypes = [vp, vp, vp, vp, i64, ci, cf, vp, i64, vp, sz, vp]
+    L.bitlinear_attend_decode_shared.argtypes = [vp, vp, vp, vp, i64, ci, cf, i64, vp, i64, vp, sz, vp]
     _lib = L
     return L
 
@@ -906,17 +906,17 @@ def alloc_attend_shared_workspace(heads: int, kv_heads: int, head_dim: int, n_se
     return _zeroed(attend_shared_workspace_bytes(heads, kv_heads, head_dim, n_seqs), "bitlinear_attend_shared_workspace_bytes", device)
 
 
-def _attend_more(where: str, call, cache: KVCache, batch: KVBatch, other, q, scale, out, workspace, stream):
-    """What attend_decode_weigh and attend_decode_shared have in common: call(.., address of `other` (marks or groups), ..)."""
+def _attend_more(where: str, call, cache: KVCache, batch: KVBatch, other, q, scale, more: tuple, out, workspace, stream):
+    """What attend_decode_weigh and attend_decode_shared have in common: call(.., address of `other` (marks or groups), .., *more, ..)."""
     index = cache.index
     if batch.index != index or other.index != index:
         _refuse(where, f"not everything is on {cache.device}")
     if _current_device() != index:
         with torch.cuda.device(index):
-            return _attend_more(where, call, cache, batch, other, q, scale, out, workspace, stream)
+            return _attend_more(where, call, cache, batch, other, q, scale, more, out, workspace, stream)
     if stream is not None and out is None:
         with _allocating_on(stream, cache.device):
-            return _attend_more(where, call, cache, batch, other, q, scale, out, workspace, None)
+            return _attend_more(where, call, cache, batch, other, q, scale, more, out, workspace, None)
     if q.dim() != 3:
         _refuse(where, "q is [tokens, heads, head_dim]", ERR_SHAPE)
     T, heads, _ = q.shape
@@ -931,7 +931,7 @@ def _attend_more(where: str, call, cache: KVCache, batch: KVBatch, other, q, sca
     if workspace.get_device() != index or not workspace.is_contiguous():
         _refuse(where, f"the workspace is contiguous and on {cache.device}")
     st = call(cache._address, batch._address, other._address, q.data_ptr(), qs, heads, D ** -0.5 if scale is None else float(scale),
-              out.data_ptr(), os_, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+              *more, out.data_ptr(), os_, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
               _raw_stream(index) if stream is None else _stream(stream))
     if st != OK:
         _check(st, where)
@@ -946,21 +946,22 @@ def attend_decode_weigh(cache: KVCache, batch: KVBatch, marks: KVMarks, q: torch
     if workspace is None:
         _refuse(where, "a workspace is needed (alloc_attend_weigh_workspace)", ERR_WORKSPACE)
     _marks_of(cache, marks, where)
-    return _attend_more(where, (_lib or load_library()).bitlinear_attend_decode_weigh, cache, batch, marks, q, scale, out, workspace, stream)
+    return _attend_more(where, (_lib or load_library()).bitlinear_attend_decode_weigh, cache, batch, marks, q, scale, (), out, workspace, stream)
 
 
 def attend_decode_shared(cache: KVCache, batch: KVBatch, groups: KVBatch, q: torch.Tensor, scale: float | None = None,
-                         out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+                         out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None, share_from: int = -1) -> torch.Tensor:
     """bitlinear_attend_decode_shared: attend_decode for sequences that begin with the same rows.  groups: KVBatch(page_table [groups,
-    pages] of the shared rows, kv_lens [groups] how many they are, cu_tokens [groups + 1] the bounds of each group's sequences)."""
+    pages] of the shared rows, kv_lens [groups] how many they are, cu_tokens [groups + 1] the bounds of each group's sequences).
+    share_from: elements of keys from which on sharing is worth its cost; negative: the measured bound, 0: always."""
     where = "bitlinear_attend_decode_shared"
     if workspace is None:
         if stream is not None:
             with _allocating_on(stream, cache.device):
-                return attend_decode_shared(cache, batch, groups, q, scale, out)
+                return attend_decode_shared(cache, batch, groups, q, scale, out, share_from=share_from)
         workspace = torch.zeros(max(1, attend_shared_workspace_bytes(q.shape[1] if q.dim() == 3 else 0, cache.kv_heads, cache.head_dim, batch.n_seqs)),
                                 dtype=torch.uint8, device=cache.device)
-    return _attend_more(where, (_lib or load_library()).bitlinear_attend_decode_shared, cache, batch, groups, q, scale, out, workspace, stream)
+    return _attend_more(where, (_lib or load_library()).bitlinear_attend_decode_shared, cache, batch, groups, q, scale, (share_from,), out, workspace, stream)
 
 
 def _int32(t: torch.Tensor, shape: tuple, index: int, where: str, name: str) -> int:

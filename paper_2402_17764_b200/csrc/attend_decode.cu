@@ -910,6 +910,12 @@ add_weights_kernel(const __grid_constant__ AttendArgs a, const int chunks, const
             blk += step;
         } else {
             float sum[kBlock / 32] = {};
+            int row[kBlock / 32]; // of the marks; -1: no key, or on a bad page
+#pragma unroll
+            for (int i = 0; i < kBlock / 32; ++i) {
+                const int pos = blk * kBlock + i * 32 + lane, page = pos < len ? kv_page(a.cache, a.batch, b, pos) : -1;
+                row[i] = page < 0 ? -1 : kv_row(a.cache, page, head, pos);
+            }
             bool room = true;
             for (int c = 0; c < chunks; ++c) {
                 const int u = unit + c * (nblk + kPairCost), heads_here = min(chunk_heads, group - c * chunk_heads);
@@ -921,34 +927,38 @@ add_weights_kernel(const __grid_constant__ AttendArgs a, const int chunks, const
                 if (lane < heads_here) ml = more.sums[(int64_t)b * a.heads + head * group + c * chunk_heads + lane];
                 const float m = ml.x == -INFINITY ? 0.0f : ml.x, inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
                 const float *from = more.scores + (int64_t)u * kBlock * chunk_heads;
-                auto add = [&](int q, int i, float s) {
-                    const float mq = __shfl_sync(0xFFFFFFFFu, m, q), iq = __shfl_sync(0xFFFFFFFFu, inv, q);
-                    sum[i] += exp2_approx(s - mq) * iq;
-                };
+                // (what stands behind the last key goes into sums that nobody stores)
                 if (chunk_heads % 4 == 0 && heads_here == chunk_heads) {
-                    for (int q = 0; q < heads_here; q += 4)
+                    for (int q = 0; q < heads_here; q += 4) {
+                        float4 s[kBlock / 32];
 #pragma unroll
-                        for (int i = 0; i < kBlock / 32; ++i) { // (what stands behind the last key goes into sums that nobody stores)
-                            const float4 s = *reinterpret_cast<const float4 *>(from + (i * 32 + lane) * chunk_heads + q);
-                            add(q, i, s.x);
-                            add(q + 1, i, s.y);
-                            add(q + 2, i, s.z);
-                            add(q + 3, i, s.w);
+                        for (int i = 0; i < kBlock / 32; ++i) s[i] = *reinterpret_cast<const float4 *>(from + (i * 32 + lane) * chunk_heads + q);
+                        float mq[4], iq[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            mq[u] = __shfl_sync(0xFFFFFFFFu, m, q + u);
+                            iq[u] = __shfl_sync(0xFFFFFFFFu, inv, q + u);
                         }
-                } else {
-                    for (int q = 0; q < heads_here; ++q)
 #pragma unroll
-                        for (int i = 0; i < kBlock / 32; ++i) add(q, i, from[(i * 32 + lane) * chunk_heads + q]);
+                        for (int i = 0; i < kBlock / 32; ++i) {
+                            sum[i] += exp2_approx(s[i].x - mq[0]) * iq[0];
+                            sum[i] += exp2_approx(s[i].y - mq[1]) * iq[1];
+                            sum[i] += exp2_approx(s[i].z - mq[2]) * iq[2];
+                            sum[i] += exp2_approx(s[i].w - mq[3]) * iq[3];
+                        }
+                    }
+                } else {
+                    for (int q = 0; q < heads_here; ++q) {
+                        const float mq = __shfl_sync(0xFFFFFFFFu, m, q), iq = __shfl_sync(0xFFFFFFFFu, inv, q);
+#pragma unroll
+                        for (int i = 0; i < kBlock / 32; ++i) sum[i] += exp2_approx(from[(i * 32 + lane) * chunk_heads + q] - mq) * iq;
+                    }
                 }
             }
             if (!room && lane == 0) kv_report(a.cache);
 #pragma unroll
-            for (int i = 0; i < kBlock / 32; ++i) {
-                const int pos = blk * kBlock + i * 32 + lane;
-                if (!room || pos >= len) continue;
-                const int page = kv_page(a.cache, a.batch, b, pos);
-                if (page >= 0) atomicAdd(more.marks.mass + kv_row(a.cache, page, head, pos), sum[i]);
-            }
+            for (int i = 0; i < kBlock / 32; ++i)
+                if (room && row[i] >= 0) atomicAdd(more.marks.mass + row[i], sum[i]);
             ++unit;
             ++blk;
         }

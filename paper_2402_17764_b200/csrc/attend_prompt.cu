@@ -356,13 +356,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
         int64_t mine = 0;
         if constexpr (kShared) { // with bounds that fall, or lie outside the batch, nothing is shared at all
             bool bad = false;
+            int64_t rows_again = 0; // what the groups' sequences would read where nothing is shared
             for (int b = b0; b < b1; ++b) {
+                bool over;
                 bad = bad || group_bounds_bad(a.batch, b, a.T);
                 mine += tiles_of(b);
+                rows_again += (int64_t)(a.batch.cu_tokens[b + 1] - a.batch.cu_tokens[b]) * group_shares(a.cache, a.batch, b, over);
             }
-            none = __syncthreads_or(bad);
+#pragma unroll
+            for (int d = 16; d; d >>= 1) rows_again += __shfl_xor_sync(0xFFFFFFFFu, rows_again, d);
+            if (lane == 0) sh.scan[warp] = rows_again;
+            bad = __syncthreads_or(bad);
+            rows_again = 0;
+#pragma unroll
+            for (int w = 0; w < kThreads / 32; ++w) rows_again += sh.scan[w];
+            __syncthreads(); // (the sums are written to below)
+            none = bad || rows_again * a.cache.kv_heads * D < more.share_from;
             if (none) {
-                if (blockIdx.x == 0 && tid == 0) kv_report(a.cache);
+                if (bad && blockIdx.x == 0 && tid == 0) kv_report(a.cache);
                 write_starts();
                 leave();
                 return;

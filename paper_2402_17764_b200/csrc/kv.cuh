@@ -177,7 +177,13 @@ struct SharedArgs {
     float *o;        // [n_seqs][heads][width]: its weighted sum of the values
     float *parts;    // the partial results of tiles whose keys several CTAs share (see prompt_part_floats)
     KvBatch seqs;
+    int64_t share_from; // elements of keys that the sequences read again where nothing is shared: from here on it is
 };
+// Sharing costs a launch and 9 us of beginnings and ends; reading a shared row again for every sequence, mostly from the L2, goes at 7
+// TB/s of keys and values.  Both meet near 40 M elements of keys (bf16, 32/32 heads of 128, 4 sequences sharing 1000 rows: 20 us shared,
+// 16 apart; 4000 rows: 32 and 40; 64/8 heads, 8 sequences sharing 2000: 23 and 17; 28/4 heads, 16 sharing 4000: 27 and 24; 24/8 heads
+// of 64, 32 in two groups sharing 8000: 30 and 70).
+constexpr int64_t kShareFrom = (int64_t)40 << 20;
 
 // Workspace of the decode kernel: a counter per CTA, then the partial results.  The grid has at most kDecodeMaxCtas CTAs.
 constexpr int kDecodeMaxCtas = 512;

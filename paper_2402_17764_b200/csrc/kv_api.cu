@@ -304,7 +304,7 @@ size_t bitlinear_attend_shared_workspace_bytes(int heads, int kv_heads, int head
 
 bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,
                                                 const bitlinear_kv_batch *groups, const void *q, int64_t q_stride, int heads,
-                                                float softmax_scale, void *out, int64_t out_stride, void *workspace,
+                                                float softmax_scale, int64_t share_from, void *out, int64_t out_stride, void *workspace,
                                                 size_t workspace_bytes, void *stream)
 {
     AttendArgs a{}, p{};
@@ -328,7 +328,10 @@ bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache,
     shared.parts = reinterpret_cast<float *>(ws + prompt_counter_bytes());
     shared.o = reinterpret_cast<float *>(ws + at.o);
     shared.seqs = a.batch;
-    if (groups->n_seqs == 0) return launch_attend_decode(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+    shared.share_from = share_from < 0 ? kShareFrom : share_from;
+    // (or where no lengths that the groups' page table has room for make it worth while)
+    if (groups->n_seqs == 0 || (double)T * p.batch.capacity * a.cache.kv_heads * a.cache.head_dim < (double)shared.share_from)
+        return launch_attend_decode(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
     if (launch_attend_prefix(p, shared, (cudaStream_t)stream) != cudaSuccess) return BITLINEAR_ERR_CUDA;
     return launch_attend_decode_behind(a, shared, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }

@@ -63,16 +63,16 @@ def test_shared_against_64_bits(heads, kv_heads, head_dim, page, groups, alone, 
     edge = guard[:, heads * head_dim:].clone()
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
     ws = B.alloc_attend_shared_workspace(heads, kv_heads, head_dim, n)
-    B.attend_decode_shared(cache, batch, of, q, out=out, workspace=ws)
+    B.attend_decode_shared(cache, batch, of, q, out=out, workspace=ws, share_from=0)
     cache.check()
     want, bound = R.attend(s, q, [1] * n, **error_of(bits))
     check(out, want, bound)
     assert torch.equal(guard[:, heads * head_dim:], edge)
     first = out.clone()
     out.fill_(0.5)
-    B.attend_decode_shared(cache, batch, of, q, out=out, workspace=ws)  # on the workspace as the first call left it
+    B.attend_decode_shared(cache, batch, of, q, out=out, workspace=ws, share_from=0)  # on the workspace as the first call left it
     assert torch.equal(out, first)
-    assert torch.equal(B.attend_decode_shared(cache, batch, of, q), first)
+    assert torch.equal(B.attend_decode_shared(cache, batch, of, q, share_from=0), first)
 
 
 def test_without_groups_it_is_the_plain_attention():
@@ -81,14 +81,14 @@ def test_without_groups_it_is_the_plain_attention():
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
     want = B.attend_decode(cache, batch, q)
     none = B.KVBatch(of.page_table[:0], of.kv_lens[:0], of.cu_tokens[:1])
-    assert torch.equal(B.attend_decode_shared(cache, batch, none, q), want)
+    assert torch.equal(B.attend_decode_shared(cache, batch, none, q, share_from=0), want)
     of.kv_lens.zero_()
-    assert torch.equal(B.attend_decode_shared(cache, batch, of, q), want)
+    assert torch.equal(B.attend_decode_shared(cache, batch, of, q, share_from=0), want)
     of.kv_lens.fill_(15)  # less than a page
-    assert torch.equal(B.attend_decode_shared(cache, batch, of, q), want)
+    assert torch.equal(B.attend_decode_shared(cache, batch, of, q, share_from=0), want)
     of.kv_lens.fill_(64)
     of.cu_tokens.copy_(torch.tensor([1, 2], dtype=torch.int32))  # a group of one
-    assert torch.equal(B.attend_decode_shared(cache, batch, of, q), want)
+    assert torch.equal(B.attend_decode_shared(cache, batch, of, q, share_from=0), want)
     cache.check()
 
 
@@ -100,7 +100,7 @@ def test_bounds_that_make_no_sense(bounds):
     q = rows(4, 8, 64, 6)
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
     want = B.attend_decode(cache, batch, q)
-    got = B.attend_decode_shared(cache, batch, of, q)
+    got = B.attend_decode_shared(cache, batch, of, q, share_from=0)
     with pytest.raises(B.BitLinearError) as e:
         cache.check()
     assert e.value.status == B.ERR_PAGE and torch.equal(got, want)
@@ -114,7 +114,7 @@ def test_bad_pages_and_lengths(bits):
     q = rows(3, 8, 64, 8)
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
     of.page_table[0, 2] = s.n_pages
-    got = B.attend_decode_shared(cache, batch, of, q)
+    got = B.attend_decode_shared(cache, batch, of, q, share_from=0)
     with pytest.raises(B.BitLinearError) as e:
         cache.check()
     assert e.value.status == B.ERR_PAGE
@@ -126,7 +126,7 @@ def test_bad_pages_and_lengths(bits):
     check(got, want, bound)
     of.page_table[0, 2] = s.table[0, 2]
     cut = B.KVBatch(of.page_table[:, :4].contiguous(), torch.tensor([1000], dtype=torch.int32, device="cuda"), of.cu_tokens)
-    got = B.attend_decode_shared(cache, batch, cut, q)
+    got = B.attend_decode_shared(cache, batch, cut, q, share_from=0)
     with pytest.raises(B.BitLinearError):
         cache.check()
     want, bound = R.attend(s, q, [1] * 3, **error_of(bits))
@@ -142,7 +142,7 @@ def test_values_that_are_not_finite_reach_those_that_see_them():
     v[row[0], 7], v[row[1], 9] = float("nan"), float("inf")
     q = rows(4, 4, 64, 10, size=0.3)
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
-    got = B.attend_decode_shared(cache, batch, of, q)
+    got = B.attend_decode_shared(cache, batch, of, q, share_from=0)
     cache.check()
     see = torch.tensor([0, 1, 3], device="cuda")
     assert torch.all(torch.isnan(got[see][..., 7])) and torch.all(got[see][..., 9] == float("inf"))
@@ -164,7 +164,7 @@ def test_scores_of_any_size(bits):
                 z *= 4.0
         q = rows(3, 4, 64, 12, size=size)
         cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
-        got = B.attend_decode_shared(cache, batch, of, q)
+        got = B.attend_decode_shared(cache, batch, of, q, share_from=0)
         cache.check()
         want, bound = R.attend(s, q, [1] * 3, **error_of(bits))
         check(got, want, bound)
@@ -175,15 +175,15 @@ def test_on_a_side_stream_and_in_a_graph():
     q = rows(5, 8, 128, 14)
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
     ws = B.alloc_attend_shared_workspace(8, 2, 128, 5)
-    want = B.attend_decode_shared(cache, batch, of, q, workspace=ws)
+    want = B.attend_decode_shared(cache, batch, of, q, workspace=ws, share_from=0)
     side = torch.cuda.Stream()
     torch.cuda.synchronize()
-    got = B.attend_decode_shared(cache, batch, of, q, stream=side)
+    got = B.attend_decode_shared(cache, batch, of, q, stream=side, share_from=0)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
     graph, out = torch.cuda.CUDAGraph(), torch.empty_like(want)
     with torch.cuda.graph(graph):
-        B.attend_decode_shared(cache, batch, of, q, out=out, workspace=ws)
+        B.attend_decode_shared(cache, batch, of, q, out=out, workspace=ws, share_from=0)
     s.kv_lens.copy_(torch.tensor([257, 0, 256, 91, 66], dtype=torch.int32))
     s.lens = [257, 0, 256, 91, 66]
     of.kv_lens.copy_(torch.tensor([128, 48], dtype=torch.int32))
@@ -200,14 +200,14 @@ def test_an_expired_wait_is_reported(bits):
     q = rows(40, 8, 64, 16)
     cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
     ws = B.alloc_attend_shared_workspace(8, 1, 64, 40)
-    want = B.attend_decode_shared(cache, batch, of, q, workspace=ws)
+    want = B.attend_decode_shared(cache, batch, of, q, workspace=ws, share_from=0)
     cache.check()
     B.test_expire_next_wait(2000, True)
-    B.attend_decode_shared(cache, batch, of, q, workspace=ws)
+    B.attend_decode_shared(cache, batch, of, q, workspace=ws, share_from=0)
     with pytest.raises(B.BitLinearError) as e:
         cache.check()
     assert e.value.status == B.ERR_TIMEOUT
-    assert torch.equal(B.attend_decode_shared(cache, batch, of, q, workspace=ws), want)
+    assert torch.equal(B.attend_decode_shared(cache, batch, of, q, workspace=ws, share_from=0), want)
     cache.check()
 
 
@@ -222,5 +222,32 @@ def test_a_workspace_serves_calls_of_different_sizes():
     for _ in range(3):
         for s, of, q, want, bound in cases:
             cache = s.cache()
-            check(B.attend_decode_shared(cache, B.KVBatch(s.table, s.kv_lens), of, q, workspace=ws), want, bound)
+            check(B.attend_decode_shared(cache, B.KVBatch(s.table, s.kv_lens), of, q, workspace=ws, share_from=0), want, bound)
             cache.check()
+
+
+def test_sharing_that_is_not_worth_its_cost():
+    """Below the bound the call is the plain attention, whether the page table alone says so or the lengths; above it rows are shared."""
+    s, of = shared([(256, [300, 290, 280]), (64, [100, 90])], 2, 128, 16, 16, 40)
+    q = rows(5, 8, 128, 41)
+    cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
+    plain, split = B.attend_decode(cache, batch, q), B.attend_decode_shared(cache, batch, of, q, share_from=0)
+    assert not torch.equal(plain, split)
+    elements = (3 * 256 + 2 * 64) * 2 * 128
+    room = 5 * of.page_table.shape[1] * 16 * 2 * 128
+    assert elements + 1 < room
+    for share_from, want in ((-1, plain), (room + 1, plain), (elements + 1, plain), (elements, split), (1, split)):
+        assert torch.equal(B.attend_decode_shared(cache, batch, of, q, share_from=share_from), want), share_from
+    cache.check()
+
+
+def test_the_measured_bound():
+    """130 sequences of 320 shared rows at 8 heads of 128: 42.6 M elements, above the bound."""
+    s, of = shared([(320, [321 + i % 5 for i in range(130)])], 8, 128, 64, 16, 42)
+    q = rows(130, 16, 128, 43)
+    cache, batch = s.cache(), B.KVBatch(s.table, s.kv_lens)
+    got = B.attend_decode_shared(cache, batch, of, q)
+    assert torch.equal(got, B.attend_decode_shared(cache, batch, of, q, share_from=0)) and not torch.equal(got, B.attend_decode(cache, batch, q))
+    want, bound = R.attend(s, q, [1] * 130, **error_of(16))
+    check(got, want, bound)
+    cache.check()

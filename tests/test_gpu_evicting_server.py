@@ -145,7 +145,7 @@ def test_users_of_one_instruction(bits):
         lens += 1
         q, k, v = (rows(users, n, head_dim, 10 * step + i + 5, size=2.0) for i, n in enumerate((heads, kv_heads, kv_heads)))
         q = B.kv_append_rmsnorm(cache, batch, k, v, q=q, q_gain=gain, k_gain=gain, rope=rope)
-        out = B.attend_decode_shared(cache, batch, groups, q, workspace=ws)
+        out = B.attend_decode_shared(cache, batch, groups, q, workspace=ws, share_from=0)
         s.lens = lens.tolist()
         want, bound = R.attend(s, q, [1] * users, weight_rounding=2.0 ** -8, query_rounding=2.0 ** -22)
         check(out, want, bound)

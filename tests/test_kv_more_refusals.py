@@ -24,8 +24,10 @@ def append(B, c, s, **changes):
 
 
 def attend(B, c, s, which, **changes):
-    d = dict(other=marks(B) if which == "weigh" else batch(B, cu_tokens=FAKE), q=FAKE, q_stride=256, heads=4, scale=0.125, out=FAKE + 4096,
+    d = dict(other=marks(B) if which == "weigh" else batch(B, cu_tokens=FAKE), q=FAKE, q_stride=256, heads=4, scale=0.125, share_from=0, out=FAKE + 4096,
              out_stride=256, workspace=FAKE, bytes=1 << 40, stream=None)
+    if which == "weigh":
+        d.pop("share_from")
     d.update(changes)
     held = d["other"]  # (alive until the call returns)
     d["other"] = address(held)
