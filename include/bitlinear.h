@@ -469,7 +469,7 @@ bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, 
  *   source    out  int32 [n_seqs][kv_heads][keep]: the place that row i's new contents come from: i itself where the row at i
  *                  stays; the j-th of the rows at or behind `keep` that stay, for the j-th place below `keep` whose row goes;
  *                  -1 behind the end of a sequence of fewer rows
- *   new_lens  out  int32 [n_seqs]: min(kv_lens[b], keep); must not be kv_lens itself
+ *   new_lens  out  int32 [n_seqs]: min(kv_lens[b], keep); must not overlap kv_lens
  *   0 <= recent <= keep, 1 <= keep <= 2^30;  table_pages * page_size <= 2^18;  n_seqs * kv_heads <= 2^27
  * cu_tokens is not looked at.
  */

@@ -29,6 +29,14 @@
 // 32 heads: 46.5 us = 5.2 TB/s; int8, 128 sequences of 256 to 8192 tokens, 64/8 heads: 157-159 us = 4.5 TB/s (issue slots 57 %
 // busy, so not at a limit; what they wait for is the chain from a stage's codes to its output); one sequence of 777 tokens, 32
 // heads of 100: 9.5 us per call, a chain of dependent loads and the join of its parts.
+//
+// Two more forms.  The one that weighs keeps all scores (4 bytes for each query head and key, 6 % of the traffic with 8 heads per kv
+// head) and every softmax's reference and sum, and a second launch adds up 2^(s - m) / l over a kv head's queries: the references are
+// known at the end only, and reading the keys again would cost half as much once more.  128k tokens of one sequence, 64/8 heads:
+// 116 us (92 without); int8, 24 sequences of 100 to 4096 tokens, 40/40 heads: 87 us (75); one sequence of 777, 32 heads of 100: 11.5 us
+// (9.2).  What they add: the scores' way to the L2 and back, and a launch.  The form behind shared rows starts behind them and joins
+// what attend_prompt.cu found for those (up to 32 parts of a row) when a pair is stored: 64 sequences of 1 to 801 keys, 64/8 heads, 26 us
+// with nine parts to join each, 21 without any.
 #include <algorithm>
 
 #include "internal.cuh"

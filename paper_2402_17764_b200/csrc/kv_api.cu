@@ -345,7 +345,10 @@ bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitl
     if ((st = take_marks(marks, a.marks)) != BITLINEAR_OK) return st;
     if (keep < 1 || keep > ((int64_t)1 << 30) || recent < 0 || recent > keep) return BITLINEAR_ERR_SHAPE;
     if (a.batch.capacity > kSelectMaxRows || batch->n_seqs * a.cache.kv_heads > (1 << 27)) return BITLINEAR_ERR_SHAPE;
-    if (batch->n_seqs > 0 && (!source || !new_lens || new_lens == batch->kv_lens)) return BITLINEAR_ERR_ARG;
+    if (batch->n_seqs > 0 && (!source || !new_lens)) return BITLINEAR_ERR_ARG;
+    // (the lengths are read by every head's CTAs while one of them writes the new ones)
+    const uintptr_t from = reinterpret_cast<uintptr_t>(batch->kv_lens), to = reinterpret_cast<uintptr_t>(new_lens), bytes = (uintptr_t)batch->n_seqs * 4;
+    if (batch->n_seqs > 0 && from < to + bytes && to < from + bytes) return BITLINEAR_ERR_ARG;
     if (!aligned(source, 4) || !aligned(new_lens, 4)) return BITLINEAR_ERR_ALIGN;
     if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
     if (batch->n_seqs == 0) return BITLINEAR_OK;

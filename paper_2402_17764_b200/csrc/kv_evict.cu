@@ -330,6 +330,9 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
 // Moves row source[i] of every sequence and kv head to row i.  A warp takes 32 rows i at a time, looks at what moves with a
 // lane each, and copies rows with all of its lanes: keys with one half, values with the other.  Rows that are copied from lie at or behind
 // `keep`, rows that are copied to below it, so no row is both and all may be copied at once.
+//
+// What bounds it: memory, in pieces of a row (256 bytes of bf16).  64 sequences of 1500 to 8191 rows cut to 1024, 8 heads of 128: 66.6 us
+// = 5.5 TB/s (0.84 of a copy's rate; two rows at a time 80 us, eight 67).  32 heads, 16 rows of 2064 each: 2.7 us, the launch.
 constexpr int kCompactThreads = 256;
 constexpr int kRowsAtATime = 4;
 
@@ -449,7 +452,7 @@ cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream)
 cudaError_t launch_kv_compact(const CompactArgs &a, cudaStream_t stream)
 {
     const int64_t items = (int64_t)a.batch.n_seqs * a.cache.kv_heads * ((a.keep + 31) / 32);
-    const int64_t blocks = std::min<int64_t>((items + kCompactThreads / 32 - 1) / (kCompactThreads / 32), 8 * sm_count());
+    const int64_t blocks = std::min<int64_t>((items + kCompactThreads / 32 - 1) / (kCompactThreads / 32), 16 * sm_count());
     return launch_dependent(kv_compact_kernel, (unsigned)blocks, kCompactThreads, 0, stream, a, items);
 }
 

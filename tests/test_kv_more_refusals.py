@@ -111,6 +111,7 @@ def test_arguments_of_evicting_that_are_refused(B):  # noqa: F811
         (dict(marks=None), "ERR_ARG"), (dict(marks=marks(B, mass=None)), "ERR_ARG"), (dict(marks=marks(B, pos=FAKE + 2)), "ERR_ALIGN"),
         (dict(keep=0), "ERR_SHAPE"), (dict(keep=(1 << 30) + 1), "ERR_SHAPE"), (dict(recent=-1), "ERR_SHAPE"), (dict(recent=9), "ERR_SHAPE"),
         (dict(source=None), "ERR_ARG"), (dict(new_lens=None), "ERR_ARG"), (dict(new_lens=FAKE), "ERR_ARG"),  # (kv_lens itself)
+        (dict(new_lens=FAKE + 8), "ERR_ARG"), (dict(new_lens=FAKE - 8), "ERR_ARG"),
         (dict(source=FAKE + 2), "ERR_ALIGN"), (dict(new_lens=FAKE + 65), "ERR_ALIGN"),
     ]:
         assert select(B, c, s, **changes) == getattr(B, status), changes
