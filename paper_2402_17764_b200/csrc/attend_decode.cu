@@ -663,6 +663,11 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
     // comes after this); element e of query q stands at e ^ 8 (q / 2 % 4), so that the lanes of a store hit 32 banks.
     auto laid = [](int q, int e) { return q * WT + (e ^ (((q >> 1) & 3) << 3)); };
     auto end_pair = [&](const Place &p, int stage) { // p: the last block of the pair that this CTA has
+        // A thread's item, four elements of a query: neighbouring threads take neighbouring elements, or, where the shared rows' parts
+        // are joined, in which neighbouring rows lie side by side, neighbouring queries (64 sequences, nine parts each: 79 -> 76 us).
+        const bool by_query = kMode == kBehind && start_of(p.b) > 0;
+        auto item_query = [&](int i) { return by_query ? i % chunk_heads : i / (WT / 4); };
+        auto item_element = [&](int i) { return by_query ? i / chunk_heads * 4 : i % (WT / 4) * 4; };
         __syncwarp();
         float *own = reinterpret_cast<float *>(ring + stage * S::kStage);
 #pragma unroll
@@ -689,7 +694,7 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
         // the four warps' results, in warp order
         float *part = whole ? nullptr : part_of(blockIdx.x, pair_begin < share_begin ? 0 : 1);
         for (int i = tid; i < items; i += kThreads) {
-            const int q = i / (WT / 4), e = i % (WT / 4) * 4;
+            const int q = item_query(i), e = item_element(i);
             float2 ml[kWarps];
             float M = -INFINITY;
 #pragma unroll
@@ -732,7 +737,7 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
                 while (items * lanes * 2 <= kThreads) lanes *= 2;
                 const int n = to - from + 1, stretch = (n + lanes - 1) / lanes;
                 for (int i0 = 0; i0 < items; i0 += kThreads / lanes) {
-                    const int i = i0 + tid / lanes, q = i / (WT / 4), e = i % (WT / 4) * 4;
+                    const int i = i0 + tid / lanes, q = item_query(i), e = item_element(i);
                     const int c0 = from + min(n, tid % lanes * stretch), c1 = from + min(n, (tid % lanes + 1) * stretch);
                     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     float M = -INFINITY, L = 0.0f;
