@@ -897,7 +897,10 @@ add_weights_kernel(const __grid_constant__ AttendArgs a, const int chunks, const
     __syncthreads();
     const Plan plan(total, (int)gridDim.x * kWeighWarps);
     const int share = (int)blockIdx.x * kWeighWarps + warp;
-    if (share >= plan.shares) return;
+    if (share >= plan.shares) {
+        griddep_wait(); // (nor may this launch be over before the one in front of it)
+        return;
+    }
     int unit = plan.begin_of(share);
     const int end = plan.begin_of(share + 1);
     // the thread whose sequences the first unit lies in, then the sequence

@@ -45,8 +45,8 @@
 //
 // The form for rows that sequences share (single tokens of many sequences over the same keys) has the queries of a group's sequences
 // as rows, no masks, and leaves its parts, in fp32, to be joined by the decode kernel behind it, a sequence's rows at a time: joined by
-// the last CTA of a tile, as above, nine parts of 133 KB took 10 us.  64 sequences over 16384 shared rows, 64/8 heads: about 50 of the
-// 79 us of both launches, 28 steps of 1960 cycles and 18000 for the beginning (search, queries, first scores) and the end (parts).
+// the last CTA of a tile, as above, nine parts of 133 KB took 10 us.  64 sequences over 16384 shared rows, 64/8 heads: about 48 of the
+// 77 us of both launches, 28 steps of 1960 cycles and 18000 for the beginning (search, queries, first scores) and the end (parts).
 #include <cuda.h>
 
 #include <algorithm>
@@ -57,9 +57,6 @@
 #include "ptx.cuh"
 #include "tma_host.cuh"
 
-#ifndef SHARED_LEAST
-#define SHARED_LEAST 2
-#endif
 namespace bitlinear {
 namespace {
 
@@ -376,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
 #pragma unroll
             for (int w = 0; w < kThreads / 32; ++w) rows_again += sh.scan[w];
             __syncthreads(); // (the sums are written to below)
-            none = bad || rows_again * a.cache.kv_heads * D < more.share_from;
+            none = bad || rows_again < more.share_from;
             if (none) {
                 if (bad && blockIdx.x == 0 && tid == 0) kv_report(a.cache);
                 write_starts();
@@ -473,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     // does not cost more than they save)
     const int most = (w.sees(min(w.row0 + kRows, w.rows) - 1) + kTile - 1) / kTile;
     // (The parts of the shared form are joined by the kernel behind it, a sequence's rows at a time: two blocks are enough.)
-    const int parts = max(1, min(splits, most / (kShared ? SHARED_LEAST : 4)));
+    const int parts = max(1, min(splits, most / (kShared ? 2 : 4)));
     if (split >= parts) {
         if (kShared) {
             write_starts();

@@ -177,7 +177,7 @@ struct SharedArgs {
     float *o;        // [n_seqs][heads][width]: its weighted sum of the values
     float *parts;    // the partial results of tiles whose keys several CTAs share (see prompt_part_floats)
     KvBatch seqs;
-    int64_t share_from; // elements of keys that the sequences read again where nothing is shared: from here on it is
+    int64_t share_from; // rows that the groups' sequences read in all where nothing is shared: from here on it is
 };
 // Sharing costs a launch and 9 us of beginnings and ends; reading a shared row again for every sequence, mostly from the L2, goes at 7
 // TB/s of keys and values.  Both meet near 40 M elements of keys (bf16, 32/32 heads of 128, 4 sequences sharing 1000 rows: 20 us shared,

@@ -328,9 +328,10 @@ bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache,
     shared.parts = reinterpret_cast<float *>(ws + prompt_counter_bytes());
     shared.o = reinterpret_cast<float *>(ws + at.o);
     shared.seqs = a.batch;
-    shared.share_from = share_from < 0 ? kShareFrom : share_from;
+    const int64_t row = (int64_t)a.cache.kv_heads * a.cache.head_dim, least = share_from < 0 ? kShareFrom : share_from;
+    shared.share_from = least / row + (least % row != 0);
     // (or where no lengths that the groups' page table has room for make it worth while)
-    if (groups->n_seqs == 0 || (double)T * p.batch.capacity * a.cache.kv_heads * a.cache.head_dim < (double)shared.share_from)
+    if (groups->n_seqs == 0 || T * p.batch.capacity < shared.share_from)
         return launch_attend_decode(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
     if (launch_attend_prefix(p, shared, (cudaStream_t)stream) != cudaSuccess) return BITLINEAR_ERR_CUDA;
     return launch_attend_decode_behind(a, shared, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;

@@ -237,3 +237,62 @@ def test_without_sequences():
     source, lens = B.kv_select(cache, batch, marks, 5)
     B.kv_compact(cache, batch, source, marks)
     assert source.shape == (0, 2, 5) and lens.shape == (0,)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_caches_beyond_32_bit_offsets(bits):
+    """Keys (and values) of more than 4 GB, the sequences in the last pages: appended, weighed, chosen and moved there."""
+    page, kv_heads, head_dim = 64, 8, 128
+    n_pages = 2 ** 32 // (kv_heads * page * head_dim * bits // 8) + 40
+    dtype = torch.bfloat16 if bits == 16 else torch.int8
+    pools = [torch.zeros(n_pages, kv_heads, page, head_dim, dtype=dtype, device="cuda") for _ in range(2)]
+    scales = [None if bits == 16 else torch.zeros(n_pages, kv_heads, page, device="cuda") for _ in range(2)]
+    cache = B.KVCache.from_tensors(*pools, head_dim, *scales)
+    marks = B.KVMarks(cache)
+    lens, keep = [300, 129], 128
+    s = R.Setup.__new__(R.Setup)
+    s.lens, s.kv_heads, s.head_dim, s.page_size, s.bits, s.pools, s.scales = lens, kv_heads, head_dim, page, bits, pools, scales
+    s.table = torch.arange(n_pages - 10, n_pages, dtype=torch.int32, device="cuda").flip(0).view(2, 5).contiguous()
+    kv_lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(16)
+    k, v = (torch.randn(sum(lens), kv_heads, head_dim, generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    cu = torch.tensor([0, lens[0], sum(lens)], dtype=torch.int32, device="cuda")
+    B.kv_append_rmsnorm(cache, B.KVBatch(s.table, kv_lens, cu), k, v, marks=marks)
+    want = [torch.cat([s.rows(which, b, n).transpose(0, 1) for b, n in enumerate(lens)]) for which in (0, 1)]
+    for got, x in zip(want, (k, v)):
+        size = x.double().abs().amax(-1, keepdim=True)
+        assert torch.all((got - x.double()).abs() <= (0.0 if bits == 16 else (0.5 / 127 + 2.0 ** -20) * size))
+    batch = B.KVBatch(s.table, kv_lens)
+    q = torch.randn(2, 16, head_dim, generator=g).to(torch.bfloat16).cuda()
+    B.attend_decode_weigh(cache, batch, marks, q, workspace=B.alloc_attend_weigh_workspace(16, kv_heads, head_dim, bits, 2, sum(lens)))
+    assert abs(marks.mass.sum(dtype=torch.float64).item() - 32) < 1e-4
+    source, _ = B.kv_select(cache, batch, marks, keep, 20)
+    assert torch.equal(source, select(s, marks, keep, 20)[0])
+    B.kv_compact(cache, batch, source, marks)
+    cache.check()
+    for b, n in enumerate(lens):
+        at = sum(lens[:b])
+        for which in (0, 1):
+            now = s.rows(which, b, keep)
+            for h in range(kv_heads):
+                assert torch.equal(now[h], want[which][at + source[b, h].long(), h])
+
+
+def test_small_launches_behind_each_other_with_nothing_to_weigh():
+    """All slots empty: the attention's zeros are there when the next launch of the stream reads them."""
+    s = R.Setup([40] * 300, 4, 64, 16, 16, seed=17)
+    cache, marks = marked(s, 18)
+    s.kv_lens.zero_()
+    batch, q = B.KVBatch(s.table, s.kv_lens), torch.ones(300, 32, 64, dtype=torch.bfloat16, device="cuda")
+    ws, mass = B.alloc_attend_weigh_workspace(32, 4, 64, 16, 300, 0), marks.mass.clone()
+    out, seen = torch.empty_like(q), torch.empty_like(q)
+    cu, empty = torch.arange(301, dtype=torch.int32, device="cuda"), torch.empty(300, 4, 64, dtype=torch.bfloat16, device="cuda")
+    later = B.KVBatch(s.table, torch.ones(300, dtype=torch.int32, device="cuda"), cu)
+    other = R.Setup([40] * 300, 4, 64, 16, 16, seed=17).cache()
+    for _ in range(20):
+        out.fill_(3.0)
+        B.attend_decode_weigh(cache, batch, marks, q, out=out, workspace=ws)
+        B.kv_append(other, later, empty, empty, q=out, q_out=seen)  # (a dependent launch that copies what it finds)
+        assert torch.all(seen == 0)
+    assert torch.equal(marks.mass, mass)
+    cache.check()
