@@ -454,7 +454,8 @@ bitlinear_status bitlinear_kv_append_rmsnorm(const bitlinear_kv_cache *cache, co
  *              zeroed as there, where max_keys is the most keys that a call's sequences have in all (the sum of kv_lens).
  *              The weights of keys that there is no room for are not added, and the status is set.
  * Weights are added in fp32, one addition per row and call; a row that several sequences of the call share gets one for each, in an
- * order that is not fixed.  Rows on a bad page get nothing, and where a result is NaN the weights are.
+ * order that is not fixed.  Rows on a bad page get nothing, and where a result is NaN the weights are.  The rows of a prompt get their
+ * first weights from its last tokens, as sequences of their own over its pages: token t with kv_lens = t + 1.
  */
 size_t bitlinear_attend_weigh_workspace_bytes(int heads, int kv_heads, int head_dim, int bits, int64_t n_seqs, int64_t max_keys);
 bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,
@@ -471,7 +472,7 @@ bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, 
  *                  -1 behind the end of a sequence of fewer rows
  *   new_lens  out  int32 [n_seqs]: min(kv_lens[b], keep); must not overlap kv_lens
  *   0 <= recent <= keep, 1 <= keep <= 2^30;  table_pages * page_size <= 2^18;  n_seqs * kv_heads <= 2^27
- * cu_tokens is not looked at.
+ * cu_tokens is not looked at.  (A wider page table: its first columns make a batch of their own, table_pages <= table_stride.)
  */
 bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
                                      int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream);

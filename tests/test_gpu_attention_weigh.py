@@ -219,3 +219,46 @@ def test_on_a_side_stream_and_in_a_graph():
     want, bound = R.attend(s, q, [1, 1], **decode_error(8))
     check(held, want, bound)
     check_mass(marks.mass, before, weights(s, q))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_the_last_tokens_of_a_prompt_as_sequences_of_their_own(bits):
+    """A window of 16 tokens at the end of one sequence of 300: every row gets what those of the tokens that see it give."""
+    n, window = 300, 16
+    one = R.Setup([n], 2, 128, 32, bits, seed=24)
+    q = rows(window, 8, 128, 25)
+    cache = one.cache()
+    marks = marks_of(cache, 26)
+    before = marks.mass.clone()
+    s = R.Setup.__new__(R.Setup)
+    s.__dict__.update(one.__dict__)
+    s.lens = list(range(n - window + 1, n + 1))
+    s.table, s.kv_lens = one.table.expand(window, -1).contiguous(), torch.tensor(s.lens, dtype=torch.int32, device="cuda")
+    out = B.attend_decode_weigh(cache, B.KVBatch(s.table, s.kv_lens), marks, q, workspace=B.alloc_attend_weigh_workspace(8, 2, 128, bits, window, sum(s.lens)))
+    cache.check()
+    cu = torch.tensor([0, window], dtype=torch.int32, device="cuda")
+    want, bound = R.attend(one, q, [window], **decode_error(bits))
+    check(out, want, bound)
+    check(B.attend_prompt(cache, B.KVBatch(one.table, one.kv_lens, cu), q), *R.attend(one, q, [window], weight_rounding=2.0 ** -8))
+    expected = weights(s, q)
+    want, bound = before.double().flatten(), torch.zeros(before.numel(), dtype=torch.float64, device="cuda")
+    for number, p, off in expected:
+        want.index_add_(0, number.flatten(), p.flatten())
+        bound.index_add_(0, number.flatten(), off.flatten())
+    bound += window * 2.0 ** -24 * want.abs() * (bound > 0)  # (one rounding for each addition)
+    assert torch.all((marks.mass.double().flatten() - want).abs() <= bound)
+
+
+def test_a_page_table_cut_to_its_first_columns():
+    """The rows of the table keep their distance; selection takes the narrow one, whatever the wide one could hold."""
+    s = R.Setup([200, 150], 1, 64, 16, 16, seed=27, table_extra=20000)
+    cache = s.cache()
+    marks = marks_of(cache, 28)
+    with pytest.raises(B.BitLinearError) as e:
+        B.kv_select(cache, B.KVBatch(s.table, s.kv_lens), marks, 64)
+    assert e.value.status == B.ERR_SHAPE
+    narrow = B.KVBatch(s.table[:, :13], s.kv_lens)
+    source, lens = B.kv_select(cache, narrow, marks, 64)
+    B.kv_compact(cache, narrow, source, marks)
+    cache.check()
+    assert lens.tolist() == [64, 64] and torch.all(source.sort(-1).values.diff() > 0)
