@@ -10,12 +10,13 @@
 //
 // A cluster of CTAs shares a (sequence, kv head), each of them a contiguous stretch of the rows, whose marks are read once and
 // kept in shared memory.  Histograms are added up by atomics into every CTA's shared memory (of the few bins that hold anything: reading
-// all bins of the others took 1000 cycles for each of them); the list of holes goes by way of the output array (gathering it from
-// another CTA's shared memory took 2 cycles a row).
+// all bins of the others took 1000 cycles for each of them); a hole is written to the list of the CTA whose row is moved there (by way of
+// the output array it took 4000 cycles longer).
 //
-// What bounds it: latency.  1 x 32 heads of 2064 rows: 9.5 us, 17000 cycles, of which 2400 load the marks and the rest are barriers and
-// chains of a few dependent accesses in ten steps.  16 sequences of 6000 to 65535 rows, 8 heads: 42-45 us where the marks' 28 MB take
-// 4.4: two waves of CTAs, each 40000 cycles, 12000 of them (at 5.7 TB/s) loading.
+// What bounds it: latency.  1 x 32 heads of 2064 rows: 8.4 us, 15000 cycles, of which 2300 load the marks and the rest are barriers and
+// chains of a few dependent accesses in ten steps.  16 sequences of 6000 to 65535 rows, 8 heads: 32 us where the marks' 28 MB take
+// 4.4: two waves of CTAs, the longest of 40000 cycles, 12000 of them (at 5.7 TB/s) loading.  Keys of 15 bits, with which 65536 rows fit into one
+// CTA, and weights read again for those that agree in them: 30 us, and the short sequences 12 instead of 8.4.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -31,6 +32,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kMaxCluster = 8;
 constexpr size_t kSelectSmem = 220 * 1024;
+constexpr int kSorted = 128; // sequences that are taken in the order of their lengths
 constexpr int kDigits = 3;    // of 10, 11 and 11 bits
 constexpr int kBins = 2048;
 constexpr int kFirstBins = 1024, kCopies = 4; // the first digit's bins, exponents above all, are few, and so are kept four times
@@ -47,6 +49,8 @@ struct alignas(16) SelectShared {
     int4 found;           // the digit, how many rows are above it, and how many have it
     int ties[kMaxCluster]; // of every CTA's stretch
     int2 moves[kMaxCluster]; // the same: holes, and rows to be moved
+    int lens[kSorted];
+    int4 taken;              // (the sequence of this CTA)
 };
 
 // Sum over the CTA of x of the threads in front of this one; total: of all of them.
@@ -95,10 +99,8 @@ int stretch_words(int64_t rows, int cluster) { return (int)(((rows + 31) / 32 + 
 
 // C: CTAs that share a (sequence, kv head).
 template <int C, int kThreads>
-__global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_constant__ SelectArgs a, const int max_words)
+__global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_constant__ SelectArgs a, const int max_words, const bool sorted)
 {
-    ptx::griddep_wait(); // everything below is read from memory that the launch before this one may have written
-    ptx::griddep_launch_dependents();
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = C > 1 ? (int)cluster.block_rank() : 0;
     auto sync_all = [&] {
@@ -118,17 +120,38 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
     uint32_t *stays = reinterpret_cast<uint32_t *>(cached + max_words * 8);  // a bit per row of the stretch
     int *before = reinterpret_cast<int *>(stays + max_words);                // per word: what is in front of it in the stretch
     const int tid = threadIdx.x;
+    for (int i = tid; i < (kFirstBins * (kCopies + 1) + (kDigits - 1) * kBins) / 4; i += kThreads) reinterpret_cast<uint4 *>(&sh)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 0) sh.found = make_int4(0, 0, 0, 0);
+    __syncthreads();
+    if (C > 1) cluster.barrier_arrive(); // (the others may add to these bins)
+    ptx::griddep_wait(); // what follows is read from memory that the launch before this one may have written
+    ptx::griddep_launch_dependents();
     const int Hk = a.cache.kv_heads, keep = a.keep;
-    const int pair = (int)blockIdx.x / C, b = pair / Hk, h = pair - b * Hk;
+    const int turn = (int)blockIdx.x / C / Hk, h = (int)blockIdx.x / C - turn * Hk;
     bool over;
+    int b = turn;
+    if (sorted) { // the longest sequences first
+        const int seqs = a.batch.n_seqs;
+        if (tid < seqs) sh.lens[tid] = kv_length(a.batch, tid, over);
+        __syncthreads();
+        if (tid < seqs) {
+            const int mine = sh.lens[tid];
+            int longer = 0;
+            for (int i = 0; i < seqs; ++i) longer += sh.lens[i] > mine || (sh.lens[i] == mine && i < tid);
+            if (longer == turn) sh.taken.x = tid;
+        }
+        __syncthreads();
+        b = sh.taken.x;
+    }
     const int n = kv_length(a.batch, b, over);
     if (tid == 0 && rank == 0 && h == 0) {
         if (over) kv_report(a.cache);
         a.new_lens[b] = min(n, keep);
     }
-    int32_t *source = a.source + (int64_t)pair * keep;
+    int32_t *source = a.source + ((int64_t)b * Hk + h) * keep;
     if (n <= keep) { // (the whole cluster)
         for (int i = rank * kThreads + tid; i < keep; i += C * kThreads) source[i] = i < n ? i : -1;
+        if (C > 1) cluster.barrier_wait();
         return;
     }
     auto row_of = [&](int i) {
@@ -166,10 +189,6 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
     };
 
     // ---- the keep-th largest worth, and how many rows are above it -----------------------------------------
-    for (int i = tid; i < (kFirstBins * (kCopies + 1) + (kDigits - 1) * kBins) / 4; i += kThreads) reinterpret_cast<uint4 *>(&sh)[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (tid == 0) sh.found = make_int4(0, 0, 0, 0);
-    __syncthreads();
-    if (C > 1) cluster.barrier_arrive(); // (the others may add to these bins)
     constexpr int kInFlight = 4; // pieces of a thread whose marks are being loaded
     for (int i0 = tid * 4; i0 < rows; i0 += kInFlight * kThreads * 4) {
         int row[kInFlight];
@@ -196,7 +215,9 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
     uint32_t least = 0u; // its digits found so far, zeros behind them
     int above = 0;
     bool exact = false;  // the rows with a worth of `least` or more are `keep` in all
-    for (int d = 0; d < kDigits && !exact; ++d) {
+#pragma unroll
+    for (int d = 0; d < kDigits; ++d) {
+        if (exact) break;
         const int shift = digit_shift(d);
         if (d > 0) {
             const uint32_t span = 1u << digit_shift(d - 1); // (least begins with the digits found: those that agree are less than this above it)
@@ -289,38 +310,34 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
     __syncthreads();
     int my_holes = keep_word < 0 ? 0 : (keep_word >= words ? both : before[keep_word]);
     if (keep_word >= 0 && keep_word < words) my_holes += __popc(~stays[keep_word] & keep_mask);
-    int hole0 = 0, mover0 = 0; // holes, and rows to be moved, in front of this stretch
+    int hole0 = 0; // holes in front of this stretch
     if (C > 1) {
         if (tid == 0) for_all([&](auto &&of) { *of(&sh.moves[rank]) = make_int2(my_holes, both - my_holes); });
-        cluster.sync();
-        for (int r = 0; r < rank; ++r) {
-            hole0 += sh.moves[r].x;
-            mover0 += sh.moves[r].y;
-        }
+        cluster.sync(); // (and behind this no CTA looks at its rows' worth)
+        for (int r = 0; r < rank; ++r) hole0 += sh.moves[r].x;
     }
-    // The holes are listed: of a CTA on its own where its rows' worth stood, of several in `source`, from where each takes
-    // those of its rows to its own list before anything else is written there.
-    int *holes_to = C > 1 ? source + hole0 : list;
+    // The holes are listed where their rows' worth stood, each with the CTA whose row is moved there.
     for (int p = tid; p < min(pieces, max(0, (keep - row0 + 3) / 4)); p += kThreads) {
         const uint32_t bits = ~stays[p / 8];
-        int j = before[p / 8] + __popc(bits & ((1u << (p % 8 * 4)) - 1u));
+        int j = hole0 + before[p / 8] + __popc(bits & ((1u << (p % 8 * 4)) - 1u));
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (((bits >> (p % 8 * 4 + e)) & 1u) && row0 + p * 4 + e < keep) holes_to[j++] = row0 + p * 4 + e;
+        for (int e = 0; e < 4; ++e) {
+            if (!((bits >> (p % 8 * 4 + e)) & 1u) || row0 + p * 4 + e >= keep) continue;
+            int k = j++, r = 0;
+            if (C > 1)
+                while (r < C && k >= sh.moves[r].y) k -= sh.moves[r++].y;
+            if (r < C) *(C > 1 ? cluster.map_shared_rank(&list[k], r) : &list[k]) = row0 + p * 4 + e;
+        }
     }
-    if (C > 1) {
-        __threadfence();
-        cluster.sync();
-        for (int j = tid; j < both - my_holes; j += kThreads) list[j] = __ldcg(source + mover0 + j);
-        cluster.sync();
-    } else {
-        __syncthreads();
-    }
+    sync_all();
     for (int i = tid; i < min(rows, keep - row0); i += kThreads)
         if ((stays[i / 32] >> (i % 32)) & 1u) source[row0 + i] = row0 + i;
-    for (int w = max(0, keep_word) + tid; w < words; w += kThreads) {
-        uint32_t moved = stays[w] & ~below_of(w);
-        for (int j = max(0, before[w] - my_holes); moved; moved &= moved - 1u, ++j) {
+    constexpr int kGroup = 4; // rows of a thread (the newest are neighbours and all of them moved: with a word each 1 to 3 us more)
+    for (int g = max(0, keep_word) * (32 / kGroup) + tid; g < words * (32 / kGroup); g += kThreads) {
+        const int w = g / (32 / kGroup), e = g % (32 / kGroup) * kGroup;
+        const uint32_t all = stays[w] & ~below_of(w);
+        int j = max(0, before[w] - my_holes) + __popc(all & ((1u << e) - 1u));
+        for (uint32_t moved = all & (((1u << kGroup) - 1u) << e); moved; moved &= moved - 1u, ++j) {
             const int to = list[j];
             if ((uint32_t)to < (uint32_t)keep) source[to] = row0 + w * 32 + __ffs(moved) - 1; // (always, unless the marks change meanwhile)
         }
@@ -422,13 +439,17 @@ cudaError_t launch_select(const SelectArgs &a, cudaStream_t stream)
     attributes[1].val.clusterDim.x = (unsigned)C;
     attributes[1].val.clusterDim.y = attributes[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t config = {};
-    config.gridDim = dim3((unsigned)((int64_t)a.batch.n_seqs * a.cache.kv_heads * C));
+    const int64_t ctas = (int64_t)a.batch.n_seqs * a.cache.kv_heads * C;
+    config.gridDim = dim3((unsigned)ctas);
     config.blockDim = dim3(kThreads);
     config.dynamicSmemBytes = select_smem(a.batch.capacity, C);
     config.stream = stream;
     config.attrs = attributes;
     config.numAttrs = C > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&config, kv_select_kernel<C, kThreads>, a, words);
+    // With a few waves of CTAs a long sequence that comes last is waited for (16 sequences of 6000 to 65535 rows, 8 heads: 41 us in the
+    // order of the batch, 32 sorted); with many waves it is not, and every CTA's sorting costs (2560 pairs: 28, 31).
+    const bool sorted = a.batch.n_seqs > 1 && a.batch.n_seqs <= kSorted && ctas > sm_count() && ctas <= 4 * sm_count();
+    return cudaLaunchKernelEx(&config, kv_select_kernel<C, kThreads>, a, words, sorted);
 }
 
 } // namespace
@@ -436,15 +457,20 @@ cudaError_t launch_select(const SelectArgs &a, cudaStream_t stream)
 cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream)
 {
     const int64_t pairs = (int64_t)a.batch.n_seqs * a.cache.kv_heads;
-    // CTAs per (sequence, kv head): as many as the rows of the longest sequence need shared memory of, and more while they all run at
-    // once and a stretch is long enough to be worth the clusters' barriers (8 pairs of 131000 rows, eight CTAs each: 21 us; 32
-    // pairs of 9000: two 15.8 us, one 17; 32 of 2064: two 13.4, one 9.5).
+    // CTAs per (sequence, kv head): as many as the rows of the longest sequence need shared memory of, and more where a stretch is long
+    // enough to be worth the clusters' barriers (us with 1, 2, 4 and 8 CTAs: 32 pairs of 9000 rows 10.5, 12.3, 11.0; of 12000 11.3, 12.2; of
+    // 20000 14.8, 13.8, 12.8; 8 pairs of 40000 17.9 with 2, 14.1, 13.3; of 131000 23.8 with 4, 19.5) and all clusters run at once, of which the
+    // parts of the GPU that hold a cluster each have room for few (16 pairs of 131000: 8 CTAs 35.7, 4 25.4; 128 of 16000: 2 25, 1 13.3).
     int cluster = 1;
-    while (cluster < kMaxCluster && (select_smem(a.batch.capacity, cluster) > kSelectSmem || (pairs * cluster <= sm_count() && a.batch.capacity / cluster > 8192)))
+    auto all_run = [&](int ctas) { return pairs * ctas <= sm_count() * (ctas == 8 ? 3 : 4) / 4; };
+    while (cluster < kMaxCluster && (select_smem(a.batch.capacity, cluster) > kSelectSmem || (a.batch.capacity > 12288 && a.batch.capacity / cluster > 8192 && all_run(2 * cluster))))
         cluster *= 2;
-    // Short sequences of many pairs take fewer threads, so that several CTAs share an SM (2560 pairs of 200 to 500 rows: 34 us with 256
-    // threads, 68 with 1024; 32 pairs of 2064 rows: 10.5 and 9.6).
-    if (cluster == 1) return pairs > sm_count() && a.batch.capacity <= 4096 ? launch_select<1, 256>(a, stream) : launch_select<1, 1024>(a, stream);
+    // Many pairs take fewer threads, where several CTAs fit on an SM (2560 pairs of 200 to 500 rows: 28 us with 256 threads, 38 with 512, 61
+    // with 1024; 512 pairs of 1500 to 8191: 18.3, 17.7, 21.3; 256 of 10000 to 20000, whose marks fill an SM's shared memory: 48, 31, 25).
+    if (cluster == 1) {
+        if (pairs <= sm_count() || select_smem(a.batch.capacity, 1) > kSelectSmem / 2) return launch_select<1, 1024>(a, stream);
+        return a.batch.capacity <= 4096 ? launch_select<1, 256>(a, stream) : launch_select<1, 512>(a, stream);
+    }
     if (cluster == 2) return launch_select<2, 1024>(a, stream);
     return cluster == 4 ? launch_select<4, 1024>(a, stream) : launch_select<8, 1024>(a, stream);
 }

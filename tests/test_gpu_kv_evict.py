@@ -296,3 +296,21 @@ def test_small_launches_behind_each_other_with_nothing_to_weigh():
         assert torch.all(seen == 0)
     assert torch.equal(marks.mass, mass)
     cache.check()
+
+
+@pytest.mark.parametrize("kv_heads,page,seqs,longest,keep,extra", [
+    (8, 16, 30, 400, 100, 0), (2, 16, 128, 300, 64, 0), (2, 16, 129, 300, 64, 0), (8, 64, 10, 2000, 500, 700), (5, 32, 32, 64, 1, 0),
+    (2, 16, 4, 900, 100, 850), (2, 16, 4, 900, 100, 1200), (1, 16, 4, 20000, 3000, 0), (3, 64, 4, 14000, 7001, 0), (8, 16, 19, 700, 90, 3000),
+])
+def test_select_from_sequences_of_many_lengths(kv_heads, page, seqs, longest, keep, extra):
+    """A few waves of CTAs take the longest sequences first, and the page table's size decides how many share one; what they find does
+    not depend on it.  Some are equally long, one is empty, one of the length that stays."""
+    g = torch.Generator().manual_seed(seqs)
+    lens = torch.randint(1, longest + 1, (seqs,), generator=g).tolist()
+    lens[1], lens[2], lens[-1], lens[seqs // 2] = 0, keep, longest, longest
+    s = R.Setup(lens, kv_heads, 16, page, 16, seed=seqs, table_extra=extra)
+    cache, marks = marked(s, 21)
+    want, new_lens = select(s, marks, keep, keep // 3)
+    source, got = B.kv_select(cache, B.KVBatch(s.table, s.kv_lens), marks, keep, keep // 3)
+    cache.check()
+    assert torch.equal(source, want) and torch.equal(got, new_lens)
