@@ -490,8 +490,8 @@ bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bit
 /*
  * bitlinear_attend_decode for sequences that begin with the same rows: what a group of sequences shares is read once for all of them
  * (tcgen05, the queries of all its sequences as rows of one tile), the rest sequence by sequence, and the two are joined.
- * The result is that of bitlinear_attend_decode, up to the rounding of the shared part's weights to bf16 (as in
- * bitlinear_attend_prompt).  `batch` is as there: its page table covers the shared rows too.
+ * The result is that of bitlinear_attend_decode, within the same roundings (of the shared part, the weights are split into two bf16
+ * parts as there; over an 8-bit cache its queries stay bf16).  `batch` is as there: its page table covers the shared rows too.
  *   groups  n_seqs groups: cu_tokens[g] .. cu_tokens[g + 1] - 1 are the SEQUENCES of group g (not NULL; sequences may belong to
  *           none), kv_lens[g] the number of rows they share, cut to whole pages, and row g of its page_table those pages.  A group
  *           of one sequence shares nothing, nor does a sequence that is shorter than what its group shares.  With bounds that

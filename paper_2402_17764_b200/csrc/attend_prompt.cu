@@ -45,8 +45,11 @@
 //
 // The form for rows that sequences share (single tokens of many sequences over the same keys) has the queries of a group's sequences
 // as rows, no masks, and leaves its parts, in fp32, to be joined by the decode kernel behind it, a sequence's rows at a time: joined by
-// the last CTA of a tile, as above, nine parts of 133 KB took 10 us.  64 sequences over 16384 shared rows, 64/8 heads: about 48 of the
-// 77 us of both launches, 28 steps of 1960 cycles and 18000 for the beginning (search, queries, first scores) and the end (parts).
+// the last CTA of a tile, as above, nine parts of 133 KB took 10 us.  Its weights enter as two bf16 parts (value and remainder, 16 bits
+// together), as the decode kernel's do, so that a result is as exact with rows shared as without; the second parts stand behind the first
+// ones, in the other half of the scores' columns, and meet the same values (64 sequences over 16384 shared rows, 64/8 heads: 77 us with
+// one part and an error of 0.0023 against 64 bits, 82-83 with two and 0.0017, that of results rounded to bf16).  Of these 82 about 54
+// are the tiles, 28 steps of some 2300 cycles and 18000 for the beginning (search, queries, first scores) and the end (parts).
 #include <cuda.h>
 
 #include <algorithm>
@@ -622,6 +625,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
 #pragma unroll
                     for (int i = 0; i < 4; ++i) // O += P V, 16 keys each
                         mma_f16_ts(o_tmem, s_tmem + (k & 1) * kStep + i * 8, v_desc + ((i * 16 * 128) >> 4), idesc_o, k > 0 || i > 0);
+                    if (kShared) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) // (the weights' second parts)
+                            mma_f16_ts(o_tmem, s_tmem + (k & 1) * kStep + kStep / 2 + i * 8, v_desc + ((i * 16 * 128) >> 4), idesc_o, true);
+                    }
                     mma_commit(smem_u32(&sh.o_done[t]));
                     if (k + 1 == n) mma_commit(smem_u32(&sh.o_last[t]));
                     if ((k & 1) || k + 1 == n) mma_commit(smem_u32(&sh.kv_empty[stage]));
@@ -792,6 +800,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t p[16];
+                    [[maybe_unused]] uint32_t rest[kShared ? 16 : 1];
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
                         float4 f = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
@@ -808,10 +817,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                                 // (0 times the scale of a row that is not finite)
                                 if (decltype(hidden)::value) y = make_float2(u0 == 0xFF800000u ? 0.0f : y.x, u1 == 0xFF800000u ? 0.0f : y.y);
                             }
-                            p[e / 2 + h] = pack_bf16(y.x, y.y);
+                            if constexpr (kShared) {
+                                // (as in attend_decode.cu: bf16 values may be infinite, so the first part is cut off and the second one positive)
+                                const uint32_t x = kInt8 ? pack_bf16(y.x, y.y) : __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x7632);
+                                float2 z = fma2(make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u)), make_float2(-1.0f, -1.0f), y);
+                                if (!kInt8) {
+                                    const float2 least = mul2(y, make_float2(0x1p-24f, 0x1p-24f));
+                                    z = make_float2(fmaxf(z.x, least.x), fmaxf(z.y, least.y));
+                                }
+                                p[e / 2 + h] = x;
+                                rest[e / 2 + h] = pack_bf16(z.x, z.y);
+                            } else {
+                                p[e / 2 + h] = pack_bf16(y.x, y.y);
+                            }
                         }
                     }
                     tmem_st_32x16(s_half + c * 16, p); // (the scores have been read)
+                    if constexpr (kShared) tmem_st_32x16(s_half + kStep / 2 + c * 16, rest);
                 }
             };
             if (kInt8 && masked)
