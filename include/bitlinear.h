@@ -399,8 +399,9 @@ size_t bitlinear_attend_workspace_bytes(int heads, int kv_heads, int head_dim, i
  *              prompt: T * heads / kv_heads <= 2^30
  *   softmax_scale  > 0 and finite; usually 1 / sqrt(head_dim)
  *   workspace  >= bitlinear_attend_workspace_bytes(...), 256-byte aligned, filled with zeros by the caller once before its
- *              first use; every call leaves it fit for the next.  Two calls that may run at the same time must not
- *              share a workspace.
+ *              first use; every call leaves it fit for the next, which may be of another kind (decode, prompt, and the weighing
+ *              and sharing forms below), batch, head count and width, as long as it is large enough for each.  Two calls that
+ *              may run at the same time must not share a workspace.
  * Sums, maxima and the softmax's denominators are fp32.  Roundings to fewer bits: the prompt kernel rounds the weights to
  * bf16 before they meet the values; the decode kernel splits them into two bf16 parts (16 bits) and, over an 8-bit cache, takes
  * the queries to integers of 22 bits relative to the row's largest element; the results are rounded to bf16.  A token that

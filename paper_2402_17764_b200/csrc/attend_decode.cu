@@ -604,10 +604,8 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
     };
 
     // ---- the end of a pair, or of this CTA's part of it -----------------------------------------------------
-    char *ws = reinterpret_cast<char *>(a.workspace);
-    uint32_t *counters = reinterpret_cast<uint32_t *>(ws);
-    float *parts = reinterpret_cast<float *>(ws + decode_counter_bytes());
-    auto part_of = [&](int share, int which) { return parts + (int64_t)(share * kMaxSplits + which) * S::kPartFloats; };
+    uint32_t *counters = reinterpret_cast<uint32_t *>(a.workspace);
+    auto part_of = [&](int share, int which) { return a.parts + (int64_t)(share * kMaxSplits + which) * S::kPartFloats; };
     // Adds the shared rows' result for four elements of query head `at` (counted over all sequences) to (x, M, L).
     auto join_shared = [&](int64_t at, int e, float4 &x, float &M, float &L) {
         if constexpr (kMode == kBehind) {

@@ -135,7 +135,8 @@ struct AttendArgs {
     int64_t q_stride, out_stride;
     int32_t T, heads;
     float scale; // of the scores, times log2(e): the kernels work with powers of two
-    void *workspace;
+    void *workspace; // begins with the counters, of every kind of call and for any heads: they alone have to be zero between calls
+    float *parts;    // in it: the decode kernel's partial results
 };
 
 // What the decode kernel that passes its weights on (to the marks) has besides.
@@ -185,7 +186,8 @@ struct SharedArgs {
 // of 64, 32 in two groups sharing 8000: 30 and 70).
 constexpr int64_t kShareFrom = (int64_t)40 << 20;
 
-// Workspace of the decode kernel: a counter per CTA, then the partial results.  The grid has at most kDecodeMaxCtas CTAs.
+// Workspace of the decode kernel: a counter per CTA, then the partial results (of the shared form elsewhere).  The grid has at most
+// kDecodeMaxCtas CTAs.
 constexpr int kDecodeMaxCtas = 512;
 __host__ __device__ constexpr size_t decode_counter_bytes() { return kDecodeMaxCtas * sizeof(uint32_t); }
 size_t attend_decode_workspace_bytes(int heads, int kv_heads, int head_dim);
@@ -202,6 +204,7 @@ cudaError_t launch_attend_decode_behind(const AttendArgs &a, const SharedArgs &s
 constexpr int kPromptMaxParts = 160;
 __host__ __device__ constexpr size_t prompt_counter_bytes() { return 256 * 2 * sizeof(uint32_t); }
 static_assert(kPromptMaxParts * 2 * sizeof(uint32_t) <= prompt_counter_bytes(), "a counter for every part");
+static_assert(decode_counter_bytes() == prompt_counter_bytes(), "calls of both kinds may take turns in one workspace");
 constexpr int kPromptRows = 256; // of a tile
 // A part: (reference, sum) of its rows, then their outputs as [four elements][row], so that a row per thread writes and reads whole
 // lines.

@@ -213,6 +213,7 @@ bitlinear_status take_attend(AttendArgs &a, const bitlinear_kv_cache *cache, con
     a.out_stride = out_stride;
     a.T = (int32_t)T;
     a.workspace = workspace;
+    a.parts = reinterpret_cast<float *>(reinterpret_cast<char *>(workspace) + decode_counter_bytes());
     return BITLINEAR_OK;
 }
 
@@ -280,13 +281,14 @@ bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, 
 
 namespace {
 
-// Workspace of the attention over shared beginnings: the prompt kernel's, the decode kernel's, then what the one hands to the other.
+// Workspace of the attention over shared beginnings: the prompt kernel's, whose counters are the decode kernel's (the shared form needs
+// none), the decode kernel's partial results, then what the one hands to the other.
 struct SharedLayout {
-    size_t decode, starts, where, ml, o, bytes;
+    size_t decode_parts, starts, where, ml, o, bytes;
     SharedLayout(int heads, int kv_heads, int head_dim, int64_t n_seqs)
     {
-        decode = attend_prompt_workspace_bytes(heads, kv_heads, head_dim);
-        starts = decode + attend_decode_workspace_bytes(heads, kv_heads, head_dim);
+        decode_parts = attend_prompt_workspace_bytes(heads, kv_heads, head_dim);
+        starts = decode_parts + attend_decode_workspace_bytes(heads, kv_heads, head_dim) - decode_counter_bytes();
         where = starts + align_up((size_t)n_seqs * sizeof(int32_t), 256);
         ml = where + align_up((size_t)n_seqs * heads * sizeof(int2), 256);
         o = ml + align_up((size_t)n_seqs * heads * sizeof(float2), 256);
@@ -320,7 +322,7 @@ bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache,
     if (!device_is_sm100()) return BITLINEAR_ERR_ARCH;
     if (T == 0) return BITLINEAR_OK;
     char *ws = reinterpret_cast<char *>(workspace);
-    a.workspace = ws + at.decode;
+    a.parts = reinterpret_cast<float *>(ws + at.decode_parts);
     SharedArgs shared;
     shared.starts = reinterpret_cast<int32_t *>(ws + at.starts);
     shared.where = reinterpret_cast<int2 *>(ws + at.where);
