@@ -159,9 +159,9 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
         return page < 0 ? -1 : kv_row(a.cache, page, h, i);
     };
     const int last = row_of(n - 1);
-    const int64_t after = last < 0 ? INT32_MAX : (int64_t)a.marks.pos[last] - a.recent + 1;
-    const int newest = (int)(after < INT32_MIN ? INT32_MIN : (after > INT32_MAX ? INT32_MAX : after)); // what is as new as this stays
-    const bool some_new = last >= 0;
+    const int64_t after = last < 0 ? INT64_MAX : (int64_t)a.marks.pos[last] - a.recent + 1;
+    const bool some_new = after <= INT32_MAX;
+    const int newest = (int)(after < INT32_MIN ? INT32_MIN : after); // what is as new as this stays
     const int all_words = (n + 31) / 32, each = (all_words + C - 1) / C;
     const int word0 = min(all_words, rank * each), words = min(all_words, word0 + each) - word0; // of this stretch
     const int row0 = word0 * 32, rows = min(n, row0 + words * 32) - row0;
