@@ -466,8 +466,14 @@ bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, 
 
 /*
  * Which rows stay when the sequences of a batch are cut to `keep` rows: for every sequence longer than that and every kv head, the
- * rows whose position is among the `recent` newest (above pos of the sequence's last row - recent) and, for the rest, the
- * rows of the largest mass; of equal ones the first (a negative mass or NaN counts as 0, as does a row on a bad page, which sets the status).
+ * rows whose position is above (the newest position - recent) and, for the rest, the rows of the largest mass; of equal ones the
+ * first (a negative mass or NaN counts as 0, as does a row on a bad page, which sets the status).
+ *   bitlinear_kv_select            takes the position of the sequence's LAST row for the newest.  So it is behind an append, as in a step
+ *                                  that appends, attends, selects and moves.  It need not be where rows were moved since, by
+ *                                  bitlinear_kv_compact, which fills the holes with the newest rows: a second cut before the next
+ *                                  append would count older rows as new, in place of the newest.
+ *   bitlinear_kv_select_any_order  takes the largest position of the sequence's rows, of each kv head: right for rows in any order, and
+ *                                  the same where the last row is the newest.  It reads the positions once more.
  *   source    out  int32 [n_seqs][kv_heads][keep]: the place that row i's new contents come from: i itself where the row at i
  *                  stays; the j-th of the rows at or behind `keep` that stay, for the j-th place below `keep` whose row goes;
  *                  -1 behind the end of a sequence of fewer rows
@@ -477,6 +483,8 @@ bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, 
  */
 bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
                                      int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream);
+bitlinear_status bitlinear_kv_select_any_order(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
+                                               int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream);
 
 /*
  * Moves the rows that `source` (as bitlinear_kv_select writes it, or the caller's own) names: keys, values, scales and marks (if not

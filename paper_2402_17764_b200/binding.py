@@ -60,6 +60,7 @@ EXPORTS = [
     "bitlinear_attend_weigh_workspace_bytes",
     "bitlinear_attend_decode_weigh",
     "bitlinear_kv_select",
+    "bitlinear_kv_select_any_order",
     "bitlinear_kv_compact",
     "bitlinear_attend_shared_workspace_bytes",
     "bitlinear_attend_decode_shared",
@@ -186,6 +187,7 @@ def load_library() -> ctypes.CDLL:
     L.bitlinear_attend_weigh_workspace_bytes.restype = sz
     L.bitlinear_attend_decode_weigh.argtypes = [vp, vp, vp, vp, i64, ci, cf, vp, i64, vp, sz, vp]
     L.bitlinear_kv_select.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp]
+    L.bitlinear_kv_select_any_order.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp]
     L.bitlinear_kv_compact.argtypes = [vp, vp, vp, i64, vp, vp]
     L.bitlinear_attend_shared_workspace_bytes.argtypes = [ci, ci, ci, i64]
     L.bitlinear_attend_shared_workspace_bytes.restype = sz
@@ -971,19 +973,21 @@ def _int32(t: torch.Tensor, shape: tuple, index: int, where: str, name: str) -> 
 
 
 def kv_select(cache: KVCache, batch: KVBatch, marks: KVMarks, keep: int, recent: int = 0, source: torch.Tensor | None = None,
-              new_lens: torch.Tensor | None = None, stream=None):
+              new_lens: torch.Tensor | None = None, stream=None, any_order: bool = False):
     """bitlinear_kv_select: -> (source int32 [n_seqs, kv_heads, keep], new_lens int32 [n_seqs]), which rows stay when the sequences are
-    cut to `keep` rows: those of the `recent` newest positions, then those of the largest mass."""
-    where = "bitlinear_kv_select"
+    cut to `keep` rows: those of the `recent` newest positions, then those of the largest mass.  The last row of a sequence has to be its
+    newest, as it is behind an append; any_order (bitlinear_kv_select_any_order): rows may stand in any order, as they do when they
+    were moved (kv_compact) and nothing was appended since."""
+    where = "bitlinear_kv_select_any_order" if any_order else "bitlinear_kv_select"
     index = cache.index
     if batch.index != index:
         _refuse(where, f"the cache is on {cache.device}, the batch on {batch.device}")
     if _current_device() != index:
         with torch.cuda.device(index):
-            return kv_select(cache, batch, marks, keep, recent, source, new_lens, stream)
+            return kv_select(cache, batch, marks, keep, recent, source, new_lens, stream, any_order)
     if stream is not None and (source is None or new_lens is None):
         with _allocating_on(stream, cache.device):
-            return kv_select(cache, batch, marks, keep, recent, source, new_lens)
+            return kv_select(cache, batch, marks, keep, recent, source, new_lens, any_order=any_order)
     if not 1 <= keep <= 1 << 30:
         _refuse(where, "keep is 1 .. 2^30", ERR_SHAPE)
     shape = (batch.n_seqs, cache.kv_heads, keep)
@@ -991,7 +995,8 @@ def kv_select(cache: KVCache, batch: KVBatch, marks: KVMarks, keep: int, recent:
         source = torch.empty(shape, dtype=torch.int32, device=cache.device)
     if new_lens is None:
         new_lens = torch.empty(shape[:1], dtype=torch.int32, device=cache.device)
-    st = (_lib or load_library()).bitlinear_kv_select(
+    L = _lib or load_library()
+    st = (L.bitlinear_kv_select_any_order if any_order else L.bitlinear_kv_select)(
         cache._address, batch._address, _marks_of(cache, marks, where), keep, recent, _int32(source, shape, index, where, "source"),
         _int32(new_lens, shape[:1], index, where, "new_lens"), _raw_stream(index) if stream is None else _stream(stream))
     if st != OK:

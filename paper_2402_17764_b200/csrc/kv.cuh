@@ -221,6 +221,7 @@ struct SelectArgs {
     KvMarks marks;
     int32_t *source, *new_lens;
     int32_t keep, recent;
+    bool any_order; // the newest position is the largest of the rows', not the last row's
 };
 constexpr int64_t kSelectMaxRows = (int64_t)1 << 18; // of a sequence
 cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream);

@@ -339,8 +339,10 @@ bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache,
     return launch_attend_decode_behind(a, shared, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
 }
 
-bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
-                                     int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream)
+namespace {
+
+bitlinear_status select_rows(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks, int64_t keep,
+                             int64_t recent, bool any_order, int32_t *source, int32_t *new_lens, void *stream)
 {
     SelectArgs a{};
     bitlinear_status st = take_views(cache, batch, a.cache, a.batch);
@@ -359,7 +361,22 @@ bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitl
     a.new_lens = new_lens;
     a.keep = (int32_t)keep;
     a.recent = (int32_t)recent;
+    a.any_order = any_order;
     return launch_kv_select(a, (cudaStream_t)stream) == cudaSuccess ? BITLINEAR_OK : BITLINEAR_ERR_CUDA;
+}
+
+} // namespace
+
+bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
+                                     int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream)
+{
+    return select_rows(cache, batch, marks, keep, recent, false, source, new_lens, stream);
+}
+
+bitlinear_status bitlinear_kv_select_any_order(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
+                                               int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream)
+{
+    return select_rows(cache, batch, marks, keep, recent, true, source, new_lens, stream);
 }
 
 bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const int32_t *source,

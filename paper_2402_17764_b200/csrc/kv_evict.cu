@@ -8,6 +8,9 @@
 // or behind `keep`) in front of every word; the j-th row to be moved takes its hole from a list of the holes in order.  Nothing
 // depends on the order in which threads run.
 //
+// The newest position is the last row's, or, for rows in any order, the largest, found by a pass over the positions in front of the
+// others (1 x 32 heads of 2064 rows: 0.1 us more; 16 sequences of 6000 to 65535 rows: 32 -> 37 us).
+//
 // A cluster of CTAs shares a (sequence, kv head), each of them a contiguous stretch of the rows, whose marks are read once and
 // kept in shared memory.  Histograms are added up by atomics into every CTA's shared memory (of the few bins that hold anything: reading
 // all bins of the others took 1000 cycles for each of them); a hole is written to the list of the CTA whose row is moved there (by way of
@@ -49,6 +52,7 @@ struct alignas(16) SelectShared {
     int4 found;           // the digit, how many rows are above it, and how many have it
     int ties[kMaxCluster]; // of every CTA's stretch
     int2 moves[kMaxCluster]; // the same: holes, and rows to be moved
+    int newest[kMaxCluster]; // the same: the largest position
     int lens[kSorted];
     int4 taken;              // (the sequence of this CTA)
 };
@@ -158,13 +162,39 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
         const int page = kv_page(a.cache, a.batch, b, i);
         return page < 0 ? -1 : kv_row(a.cache, page, h, i);
     };
-    const int last = row_of(n - 1);
-    const int64_t after = last < 0 ? INT64_MAX : (int64_t)a.marks.pos[last] - a.recent + 1;
-    const bool some_new = after <= INT32_MAX;
-    const int newest = (int)(after < INT32_MIN ? INT32_MIN : after); // what is as new as this stays
     const int all_words = (n + 31) / 32, each = (all_words + C - 1) / C;
     const int word0 = min(all_words, rank * each), words = min(all_words, word0 + each) - word0; // of this stretch
     const int row0 = word0 * 32, rows = min(n, row0 + words * 32) - row0;
+    int64_t after = INT64_MAX; // what is as new as this stays
+    if (!a.any_order) {
+        const int last = row_of(n - 1);
+        if (last >= 0) after = (int64_t)a.marks.pos[last] - a.recent + 1;
+    } else { // the largest position of the stretch, then of all stretches (no row of it on a page that exists: the smallest there is)
+        int top = INT32_MIN;
+        for (int i = tid * 4; i < rows; i += kThreads * 4) {
+            const int row = row_of(row0 + i);
+            if (row < 0) continue;
+            const int4 p = *reinterpret_cast<const int4 *>(a.marks.pos + row);
+            const int y[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < rows) top = max(top, y[e]);
+        }
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+        if (tid % 32 == 0) sh.scan[tid / 32] = top;
+        __syncthreads();
+        top = __reduce_max_sync(0xFFFFFFFFu, tid % 32 < kThreads / 32 ? sh.scan[tid % 32] : INT32_MIN);
+        if (C > 1) {
+            cluster.barrier_wait(); // (all CTAs have begun)
+            if (tid == 0) for_all([&](auto &&of) { *of(&sh.newest[rank]) = top; });
+            cluster.sync();
+            for (int r = 0; r < C; ++r) top = max(top, sh.newest[r]);
+            cluster.barrier_arrive(); // (as in front of this)
+        }
+        after = (int64_t)top - a.recent + 1;
+    }
+    const bool some_new = after <= INT32_MAX;
+    const int newest = (int)(after < INT32_MIN ? INT32_MIN : after);
     auto worth_of = [&](float mass, int pos) { // (nothing, or not a number: 0)
         return some_new && pos >= newest ? 0xFFFFFFFFu : (mass > 0.0f ? __float_as_uint(mass) : 0u);
     };
