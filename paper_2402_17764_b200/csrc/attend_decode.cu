@@ -557,12 +557,13 @@ attend_decode_kernel(const __grid_constant__ AttendArgs a, const int chunks, con
                         if (kInt8) w[j] *= vs;
                     }
                     // bf16 values may be infinite: the first part is cut off, not rounded, and the second one positive where the weight
-                    // is, or infinity times the two would be NaN (with a second part of 0 or below)
+                    // is, or infinity times the two would be NaN (with a second part of 0 or below): at least 2^-24 of the weight, and a
+                    // normal number
                     const uint32_t x = kInt8 ? pack_bf16(w[0], w[1]) : __byte_perm(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632);
                     rest[0] = w[0] - __uint_as_float(x << 16);
                     rest[1] = w[1] - __uint_as_float(x & 0xFFFF0000u);
                     if (!kInt8)
-                        for (int j = 0; j < 2; ++j) rest[j] = fmaxf(rest[j], w[j] * 0x1p-24f);
+                        for (int j = 0; j < 2; ++j) rest[j] = fmaxf(rest[j], fminf(w[j], fmaf(w[j], 0x1p-24f, 0x1p-126f)));
                     hi[t][h] = movmatrix(x);
                     lo[t][h] = movmatrix(pack_bf16(rest[0], rest[1]));
                 }

@@ -818,11 +818,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
                                 if (decltype(hidden)::value) y = make_float2(u0 == 0xFF800000u ? 0.0f : y.x, u1 == 0xFF800000u ? 0.0f : y.y);
                             }
                             if constexpr (kShared) {
-                                // (as in attend_decode.cu: bf16 values may be infinite, so the first part is cut off and the second one positive)
+                                // (as in attend_decode.cu: bf16 values may be infinite, so the first part is cut off and the second one positive; here
+                                // of a weight of 0 too, which may count as 2^-126: keys that do not exist have values of 0)
                                 const uint32_t x = kInt8 ? pack_bf16(y.x, y.y) : __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x7632);
                                 float2 z = fma2(make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u)), make_float2(-1.0f, -1.0f), y);
                                 if (!kInt8) {
-                                    const float2 least = mul2(y, make_float2(0x1p-24f, 0x1p-24f));
+                                    const float2 least = fma2(y, make_float2(0x1p-24f, 0x1p-24f), make_float2(0x1p-126f, 0x1p-126f));
                                     z = make_float2(fmaxf(z.x, least.x), fmaxf(z.y, least.y));
                                 }
                                 p[e / 2 + h] = x;
