@@ -507,7 +507,7 @@ bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bit
  *           fall or lie outside 0 .. n_seqs of the batch the status is set and all is attended to sequence by sequence.
  *   share_from  sharing has a cost of its own: rows are shared when the sequences of all groups would read at least this many elements
  *           of keys without it (sequences of the group * rows shared * kv_heads * head_dim, over the groups).  < 0: the library's
- *           measured bound, 40 * 2^20;  0: always.  (Where not even lengths that fill the groups' page table would reach it the
+ *           measured bound, 40 * 2^20, or 64 * 2^20 over an 8-bit cache;  0: always.  (Where not even lengths that fill the groups' page table would reach it the
  *           groups are not looked at.)
  *   workspace  >= bitlinear_attend_shared_workspace_bytes(..., n_seqs of the batch), zeroed once
  */

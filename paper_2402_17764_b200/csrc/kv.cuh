@@ -181,10 +181,15 @@ struct SharedArgs {
     int64_t share_from; // rows that the groups' sequences read in all where nothing is shared: from here on it is
 };
 // Sharing costs a launch and 9 us of beginnings and ends; reading a shared row again for every sequence, mostly from the L2, goes at 7
-// TB/s of keys and values.  Both meet near 40 M elements of keys (bf16, 32/32 heads of 128, 4 sequences sharing 1000 rows: 20 us shared,
-// 16 apart; 4000 rows: 32 and 40; 64/8 heads, 8 sequences sharing 2000: 23 and 17; 28/4 heads, 16 sharing 4000: 27 and 24; 24/8 heads
-// of 64, 32 in two groups sharing 8000: 30 and 70).
+// TB/s of keys and values.  Both meet near 40 M elements of keys (32/32 heads of 128, 4 sequences sharing 1000 rows: 22 us shared, 16
+// apart; 2500 rows, 41 M: 29.6 and 29.2; 4000 rows: 32 and 42; 64/8 heads, 8 sequences sharing 2000: 21 and 17; 5000, 41 M: 28.7 and 28.8;
+// 28/4 heads, 16 sharing 4000: 22 and 24; 24/8 heads of 64, 32 in two groups sharing 8000: 29 and 73).
 constexpr int64_t kShareFrom = (int64_t)40 << 20;
+// Codes are half as long to read apart, and have to become bf16 in the tiles: they meet near 64 M elements (64/8 heads, 8 sequences sharing
+// 5000 rows, 41 M: 29.9 us shared, 24.4 apart; 8000, 65 M: 33.1 and 32.9; 10000: 35.8 and 38.5; 28/4 heads, 16 sharing 4000: 27 and 22; 8000,
+// 65 M: 31.7 and 32.7; 24/8 heads of 64, 16 sharing 5000, 41 M: 26.3 and 24.9; 32 in two groups sharing 8000: 36 and 56).  Where few
+// sequences share rows under many kv heads, later (32/32 heads, 4 sequences sharing 5000, 82 M: 45 and 39; 8000: 59 and 55).
+constexpr int64_t kShareFromCodes = (int64_t)64 << 20;
 
 // Workspace of the decode kernel: a counter per CTA, then the partial results (of the shared form elsewhere).  The grid has at most
 // kDecodeMaxCtas CTAs.

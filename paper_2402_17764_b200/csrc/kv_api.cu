@@ -330,7 +330,8 @@ bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache,
     shared.parts = reinterpret_cast<float *>(ws + prompt_counter_bytes());
     shared.o = reinterpret_cast<float *>(ws + at.o);
     shared.seqs = a.batch;
-    const int64_t row = (int64_t)a.cache.kv_heads * a.cache.head_dim, least = share_from < 0 ? kShareFrom : share_from;
+    const int64_t row = (int64_t)a.cache.kv_heads * a.cache.head_dim, own_bound = a.cache.k_scale ? kShareFromCodes : kShareFrom,
+                  least = share_from < 0 ? own_bound : share_from;
     shared.share_from = least / row + (least % row != 0);
     // (or where no lengths that the groups' page table has room for make it worth while)
     if (groups->n_seqs == 0 || T * p.batch.capacity < shared.share_from)
