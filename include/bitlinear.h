@@ -479,7 +479,8 @@ bitlinear_status bitlinear_attend_decode_weigh(const bitlinear_kv_cache *cache, 
  *                  -1 behind the end of a sequence of fewer rows
  *   new_lens  out  int32 [n_seqs]: min(kv_lens[b], keep); must not overlap kv_lens
  *   0 <= recent <= keep, 1 <= keep <= 2^30;  table_pages * page_size <= 2^18;  n_seqs * kv_heads <= 2^27
- * cu_tokens is not looked at.  (A wider page table: its first columns make a batch of their own, table_pages <= table_stride.)
+ * cu_tokens is not looked at.  The time goes by table_pages, not by the lengths alone: a table much wider than the sequences is better
+ * given by its first columns, as a batch of their own (table_pages <= table_stride), and so is one beyond 2^18 positions.
  */
 bitlinear_status bitlinear_kv_select(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch, const bitlinear_kv_marks *marks,
                                      int64_t keep, int64_t recent, int32_t *source, int32_t *new_lens, void *stream);
@@ -510,6 +511,9 @@ bitlinear_status bitlinear_kv_compact(const bitlinear_kv_cache *cache, const bit
  *           measured bound, 40 * 2^20, or 64 * 2^20 over an 8-bit cache;  0: always.  (Where not even lengths that fill the groups' page table would reach it the
  *           groups are not looked at.)
  *   workspace  >= bitlinear_attend_shared_workspace_bytes(..., n_seqs of the batch), zeroed once
+ * How the shared keys are split among CTAs goes by the number of groups: min(groups, sequences) counts as so many tiles of rows per kv
+ * head, and where these are as many as the SMs, every tile is one CTA's.  So empty groups, as a captured graph may have them, cost time,
+ * and so does one long group beside many short ones, since all tiles get the same number of CTAs.
  */
 size_t bitlinear_attend_shared_workspace_bytes(int heads, int kv_heads, int head_dim, int64_t n_seqs);
 bitlinear_status bitlinear_attend_decode_shared(const bitlinear_kv_cache *cache, const bitlinear_kv_batch *batch,

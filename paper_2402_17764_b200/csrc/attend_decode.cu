@@ -33,8 +33,8 @@
 // Two more forms.  The one that weighs keeps all scores (4 bytes for each query head and key, 6 % of the traffic with 8 heads per kv
 // head) and every softmax's reference and sum, and a second launch adds up 2^(s - m) / l over a kv head's queries: the references are
 // known at the end only, and reading the keys again would cost half as much once more.  128k tokens of one sequence, 64/8 heads:
-// 116 us (92 without); int8, 24 sequences of 100 to 4096 tokens, 40/40 heads: 87 us (75); one sequence of 777, 32 heads of 100: 11.5 us
-// (9.2).  What they add: the scores' way to the L2 and back, and a launch.  The form behind shared rows starts behind them and joins
+// 117 us (93 without); int8, 24 sequences of 100 to 4096 tokens, 40/40 heads: 86 us (75); one sequence of 777, 32 heads of 100: 11.8 us
+// (9.2) on the GPU, 12.4 per call.  What they add: the scores' way to the L2 and back, and a launch.  The form behind shared rows starts behind them and joins
 // what attend_prompt.cu found for those (up to 32 parts of a row) when a pair is stored: 64 sequences of 1 to 801 keys, 64/8 heads, 26 us
 // with nine parts to join each, 21 without any.
 #include <algorithm>

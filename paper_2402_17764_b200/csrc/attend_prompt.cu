@@ -41,7 +41,7 @@
 // (the same launch takes about 930 000 cycles at any clock).  int8: the converters' shared-memory traffic and arithmetic come on
 // top, 57 % of the issue slots (chunks of 86 to 512 tokens behind 3300 to 12000, 64/8 heads: 393-405 us = 0.73 PFLOP/s).
 // Prompts of few hundred tokens: half the time is each tile's beginning and end (pages, queries, first scores; results).
-// Registers: the bf16 form spills 4 bytes (12 loaded), the int8 form none.
+// Registers: the bf16 form spills 4 bytes (12 loaded; for shared rows 12, 28 loaded), the int8 form none.
 //
 // The form for rows that sequences share (single tokens of many sequences over the same keys) has the queries of a group's sequences
 // as rows, no masks, and leaves its parts, in fp32, to be joined by the decode kernel behind it, a sequence's rows at a time: joined by

@@ -22,7 +22,8 @@
 // The form that normalises: y = x g r, r = 1 / sqrt(max(mean x^2 + eps, 2^-126)), the squares summed in fp32 over a group's lanes (four
 // heads of a warp at a time where a head takes all lanes: one root for each, and half the shuffles).  4096 tokens, 64/8 heads of 128:
 // 36.7 us = 4.6 TB/s (0.71 of a copy's rate), 27 million instructions where the form without has 17; heads of 100, 32/32 of them: 87
-// us; int8, 2436 tokens, 40/40 heads: 65 us; single tokens as without it, within 1 us.
+// us (56 without), 76 million instructions where 50 are without, issue slots 78 % busy; int8, 2436 tokens, 40/40 heads: 65 us (48),
+// 41 million for 31, issue slots 66 % busy with three CTAs; a single token, 32/32 heads of 100: 5.0 us on the GPU (3.7), 10.7 per call (8.4).
 #include <math.h>
 
 #include <algorithm>

@@ -379,7 +379,8 @@ __global__ void __launch_bounds__(kThreads) kv_select_kernel(const __grid_consta
 // `keep`, rows that are copied to below it, so no row is both and all may be copied at once.
 //
 // What bounds it: memory, in pieces of a row (256 bytes of bf16).  64 sequences of 1500 to 8191 rows cut to 1024, 8 heads of 128: 66.6 us
-// = 5.5 TB/s (0.84 of a copy's rate; two rows at a time 80 us, eight 67).  32 heads, 16 rows of 2064 each: 2.7 us, the launch.
+// = 5.5 TB/s (0.84 of a copy's rate; two rows at a time 80 us, eight 67).  Pieces of 128 bytes, for which half of the lanes copy: the same
+// rows in 8 bits 49 us (0.60), heads of 64 in bf16 44 (0.64).  32 heads, 16 rows of 2064 each: 2.7 us, the launch.
 constexpr int kCompactThreads = 256;
 constexpr int kRowsAtATime = 4;
 
@@ -487,6 +488,9 @@ cudaError_t launch_select(const SelectArgs &a, cudaStream_t stream)
 cudaError_t launch_kv_select(const SelectArgs &a, cudaStream_t stream)
 {
     const int64_t pairs = (int64_t)a.batch.n_seqs * a.cache.kv_heads;
+    // (The lengths are known on the device alone, so "rows" here are those that a row of the page table has room for: a table far wider than
+    // the sequences costs time.  64 sequences of 100 to 900 rows, 8 heads, none of them to be cut: 2.5 us behind a table of 960 positions, 22
+    // behind one of 131072; of 1100 to 2000 rows, cut to 1024: 10.7 and 129.)
     // CTAs per (sequence, kv head): as many as the rows of the longest sequence need shared memory of, and more where a stretch is long
     // enough to be worth the clusters' barriers (us with 1, 2, 4 and 8 CTAs: 32 pairs of 9000 rows 10.5, 12.3, 11.0; of 12000 11.3, 12.2; of
     // 20000 14.8, 13.8, 12.8; 8 pairs of 40000 17.9 with 2, 14.1, 13.3; of 131000 23.8 with 4, 19.5) and all clusters run at once, of which the
